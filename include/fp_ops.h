@@ -225,6 +225,84 @@ int fp_op_attention_decode_noalloc(const uint16_t* q, int q_stride, int B, int n
 int fp_op_attention_prefill(const uint16_t* q, int q_stride, int B, int S, int n_heads,
                             const fp_kv_view* kv, uint16_t* out, int32_t* err, void* stream);
 
+/* ---- Chunks of new tokens over a cache that already holds something: the next
+ * piece of each prompt (chunked prefill), drafted tokens to be verified, or one
+ * token a sequence, mixed as they come.  The batch is ragged: cu int32 [B + 1]
+ * does not decrease, sequence b's rows are cu[b] .. cu[b+1]-1 of the packed
+ * buffers (none is allowed), and its row i sits at position pos[b] + i (pos
+ * int32 [B]: what the cache held before the chunk).  n_tokens rows are in the
+ * buffers; rows that no sequence owns (behind cu[B], before cu[0]) are left as
+ * they were.  cu and pos are read on the device, so one captured launch serves
+ * other lengths within the same bounds.  A cu that decreases or leaves
+ * [0, n_tokens] sets *err = 1 (err may be NULL) and no row outside the buffers is
+ * touched.  All buffers 16-byte aligned and strides multiples of 8 elements, else
+ * FP_ERR_UNSUPPORTED; pools of fewer than 2^31 rows. */
+
+/* RoPE + KV-cache append of a chunk: as fp_op_rope_kv, for a ragged batch and
+ * with the rotated queries to q_out bf16 [n_tokens][q_out_stride] (head h at
+ * h*head_dim; q_out == qkv with the same stride rotates in place).  qkv bf16
+ * [n_tokens][row_stride]: H query heads, Hkv key heads, Hkv value heads.
+ * Positions outside the cache set *err = 1 and skip the row, a page id outside
+ * the pool sets *err = 1 and skips the row's cache writes.  Two rows must not
+ * write the same cache position. */
+int fp_op_rope_kv_chunk(const uint16_t* qkv, int row_stride, int n_tokens, int B, int n_heads, const fp_kv_view* kv,
+                        const int32_t* cu, const int32_t* pos, const float* rope_cs, uint16_t* q_out, int q_out_stride,
+                        int32_t* err, void* stream);
+
+/* Cached positions read back: row cu[b] + i of k_out and v_out (bf16
+ * [n_tokens][out_stride], KV head h at h*head_dim) is position pos[b] + i of
+ * sequence b, an int8 cache as bf16(code * scale).  A position outside the cache
+ * or a page id outside the pool gives a row of zeros and sets *err = 1. */
+int fp_op_kv_read(const fp_kv_view* kv, int n_tokens, int B, const int32_t* cu, const int32_t* pos, uint16_t* k_out,
+                  uint16_t* v_out, int out_stride, int32_t* err, void* stream);
+
+/* Attention of a chunk: row i of sequence b attends over cache positions
+ * 0 .. pos[b] + i (the chunk's own keys included: append them first);
+ * softmax(q K^T / sqrt(hd)) V, query head j reads KV head j / (H/Hkv), H/Hkv <=
+ * 128.  q bf16 [n_tokens][q_stride] (head h at h*head_dim), out bf16
+ * [n_tokens][n_heads*head_dim].
+ * max_new: at least every sequence's number of rows; max_len: at least every
+ * pos[b] + rows.  A sequence beyond either sets *err = 1: its rows behind the
+ * first max_new are left as they were, keys behind max_len are not read.  A row at
+ * a negative position has no keys: zeros, and *err = 1.  A page id outside the
+ * pool reads as zero keys and values and sets *err = 1.
+ * workspace: 256-byte aligned, at least
+ * fp_op_attention_chunk_workspace_bytes(B, n_heads, n_kv_heads, head_dim, max_new)
+ * bytes (0: a shape that is refused), of any content; calls that overlap on the GPU need separate ones. */
+int fp_op_attention_chunk(const uint16_t* q, int q_stride, int n_tokens, int B, int n_heads, const fp_kv_view* kv,
+                          const int32_t* cu, const int32_t* pos, int max_new, int max_len, uint16_t* out,
+                          void* workspace, size_t workspace_bytes, int32_t* err, void* stream);
+size_t fp_op_attention_chunk_workspace_bytes(int B, int n_heads, int n_kv_heads, int head_dim, int max_new);
+
+/* Probabilities of logits fp32 [M][V]: probs[m] = softmax(logits[m] / T),
+ * T = temperature[m] (fp32 [M]; NULL: 1).  T = 0 is the greedy choice: 1 at the
+ * lowest index of the largest logit, else 0.  -inf masks a token; a row that
+ * masks all of them gives zeros.  A NaN or +inf in a row with T > 0 gives NaN
+ * throughout.  A T that is negative, infinite or NaN gives a row of zeros and
+ * sets *err = 1 (err may be NULL).  probs may be logits. */
+int fp_op_softmax(const float* logits, int M, int V, const float* temperature, float* probs, int32_t* err,
+                  void* stream);
+
+/* Verification of drafted tokens against the target's probabilities, from given
+ * random numbers.  Sequence b's rows cu[b] .. cu[b+1]-1 are its last accepted
+ * token and the k drafted after it (tokens int32 [n_tokens]; the first one's id is
+ * not read); row i of p fp32 [n_tokens][V] is the target's distribution of the
+ * token after row i, row i < k of q that which draft i + 1 was drawn from (q NULL:
+ * drafts without one, taken as certain).  In order, the draft t after row i is
+ * accepted if u_accept[cu[b] + i] * q_i(t) < p_i(t); a is the number accepted.
+ * Then one token is drawn: a < k from max(0, p_a - q_a) (q NULL: from p_a without
+ * the refused token), a = k from p_k; it is the lowest t whose running sum exceeds
+ * u_draw[b] times the whole sum (u in [0, 1); the weights need not add up to 1).
+ * If that distribution is all zero, p_a itself is drawn from.
+ * out_tokens int32 [n_tokens]: rows 0 .. a-1 of the sequence the accepted drafts,
+ * row a the drawn token, -1 behind it; n_out int32 [B]: a + 1 (0: a sequence
+ * without rows).  A sum that is zero or not finite draws nothing: row a is -1,
+ * n_out a, *err = 1 (err may be NULL).  A draft outside [0, V) is refused and sets *err = 1.
+ * Sums and borders are as in fp64, whatever V. */
+int fp_op_verify_draft(const float* p, const float* q, int V, int n_tokens, int B, const int32_t* cu,
+                       const int32_t* tokens, const float* u_accept, const float* u_draw, int32_t* out_tokens,
+                       int32_t* n_out, int32_t* err, void* stream);
+
 /* Test hook for the failure path of the pipelined tensor-core kernels (the
  * paper has no counterpart).  Every wait of those kernels is bounded; a role
  * whose wait runs out stops, the CTA drains its copies and MMAs in flight,

@@ -149,6 +149,12 @@ _PROTOS = {
     "fp_op_attention_decode_noalloc": (_I, [_P, _I, _I, _I, C.POINTER(fp_kv_view), _P, _I, _P, _P, _P]),
     "fp_op_attention_prefill": (_I, [_P, _I, _I, _I, _I, C.POINTER(fp_kv_view), _P, _P, _P]),
     "fp_op_argmax": (_I, [_P, _I, _I, _P, _P]),
+    "fp_op_rope_kv_chunk": (_I, [_P, _I, _I, _I, _I, C.POINTER(fp_kv_view), _P, _P, _P, _P, _I, _P, _P]),
+    "fp_op_kv_read": (_I, [C.POINTER(fp_kv_view), _I, _I, _P, _P, _P, _P, _I, _P, _P]),
+    "fp_op_attention_chunk": (_I, [_P, _I, _I, _I, _I, C.POINTER(fp_kv_view), _P, _P, _I, _I, _P, _P, _SZ, _P, _P]),
+    "fp_op_attention_chunk_workspace_bytes": (_SZ, [_I, _I, _I, _I, _I]),
+    "fp_op_softmax": (_I, [_P, _I, _I, _P, _P, _P, _P]),
+    "fp_op_verify_draft": (_I, [_P, _P, _I, _I, _I, _P, _P, _P, _P, _P, _P, _P, _P]),
     "fp_debug_set_wait_limit": (_I, [_LL]),
     "fp_solve_eq1": (_I, [_I, C.c_double, _I, C.c_double, C.POINTER(fp_eq1_fit)]),
     "fp_solve_eq23": (_I, [_I, C.POINTER(fp_eq1_fit), _I, C.POINTER(fp_eq1_fit), C.POINTER(fp_l2_terms)]),
@@ -357,6 +363,35 @@ def fp_op_attention_prefill(q, q_stride, B, S, n_heads, kv: fp_kv_view, out, err
 
 def fp_op_argmax(logits, M, V, out, stream=None):
     return _check(_lib.fp_op_argmax(logits, M, V, out, stream))
+
+
+def fp_op_rope_kv_chunk(qkv, row_stride, n_tokens, B, n_heads, kv: fp_kv_view, cu, pos, rope_cs, q_out, q_out_stride,
+                        err=None, stream=None):
+    return _check(_lib.fp_op_rope_kv_chunk(qkv, row_stride, n_tokens, B, n_heads, C.byref(kv), cu, pos, rope_cs, q_out,
+                                           q_out_stride, err, stream))
+
+
+def fp_op_kv_read(kv: fp_kv_view, n_tokens, B, cu, pos, k_out, v_out, out_stride, err=None, stream=None):
+    return _check(_lib.fp_op_kv_read(C.byref(kv), n_tokens, B, cu, pos, k_out, v_out, out_stride, err, stream))
+
+
+def fp_op_attention_chunk_workspace_bytes(B, n_heads, n_kv_heads, head_dim, max_new):
+    return _lib.fp_op_attention_chunk_workspace_bytes(B, n_heads, n_kv_heads, head_dim, max_new)
+
+
+def fp_op_attention_chunk(q, q_stride, n_tokens, B, n_heads, kv: fp_kv_view, cu, pos, max_new, max_len, out, workspace,
+                          workspace_bytes, err=None, stream=None):
+    return _check(_lib.fp_op_attention_chunk(q, q_stride, n_tokens, B, n_heads, C.byref(kv), cu, pos, max_new, max_len,
+                                             out, workspace, workspace_bytes, err, stream))
+
+
+def fp_op_softmax(logits, M, V, temperature, probs, err=None, stream=None):
+    return _check(_lib.fp_op_softmax(logits, M, V, temperature, probs, err, stream))
+
+
+def fp_op_verify_draft(p, q, V, n_tokens, B, cu, tokens, u_accept, u_draw, out_tokens, n_out, err=None, stream=None):
+    return _check(_lib.fp_op_verify_draft(p, q, V, n_tokens, B, cu, tokens, u_accept, u_draw, out_tokens, n_out, err,
+                                          stream))
 
 
 def fp_debug_set_wait_limit(rounds):

@@ -189,4 +189,86 @@ int fp_op_argmax(const float* logits, int M, int V, int32_t* out, void* stream) 
   return cuda_status(launch_argmax(logits, M, V, out, (cudaStream_t)stream));
 }
 
+static bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+
+// What the chunk operators share: counts, the ragged batch, a view whose pools
+// take 16-byte accesses.
+static int check_chunk(const fp_kv_view* kv, int n_tokens, int B, const int32_t* cu, const int32_t* pos) {
+  int st = fpk_check_kv(kv);
+  if (st) return st;
+  if (n_tokens < 0 || B < 0 || !cu || !pos) return FP_ERR_INVALID_ARG;
+  if ((long long)kv->n_pages * kv->n_kv_heads * kv->page_size >= (1LL << 31)) return FP_ERR_UNSUPPORTED;
+  if (kv->pages_per_seq > (1 << 26) || n_tokens > (1 << 30) || B > (1 << 26)) return FP_ERR_UNSUPPORTED;
+  if (!aligned16(kv->k_pool) || !aligned16(kv->v_pool)) return FP_ERR_UNSUPPORTED;
+  return FP_OK;
+}
+
+int fp_op_rope_kv_chunk(const uint16_t* qkv, int row_stride, int n_tokens, int B, int n_heads, const fp_kv_view* kv,
+                        const int32_t* cu, const int32_t* pos, const float* rope_cs, uint16_t* q_out, int q_out_stride,
+                        int32_t* err, void* stream) {
+  int st = check_chunk(kv, n_tokens, B, cu, pos);
+  if (st) return st;
+  if (!qkv || !rope_cs || !q_out || n_heads <= 0 || n_heads % kv->n_kv_heads != 0) return FP_ERR_INVALID_ARG;
+  if (row_stride < (n_heads + 2LL * kv->n_kv_heads) * kv->head_dim || q_out_stride < (long long)n_heads * kv->head_dim)
+    return FP_ERR_INVALID_ARG;
+  if (row_stride % 8 || q_out_stride % 8 || !aligned16(qkv) || !aligned16(q_out) || !aligned16(rope_cs))
+    return FP_ERR_UNSUPPORTED;
+  return cuda_status(launch_rope_kv_chunk(qkv, row_stride, n_tokens, B, n_heads, *kv, cu, pos, rope_cs, q_out,
+                                          q_out_stride, err, (cudaStream_t)stream));
+}
+
+int fp_op_kv_read(const fp_kv_view* kv, int n_tokens, int B, const int32_t* cu, const int32_t* pos, uint16_t* k_out,
+                  uint16_t* v_out, int out_stride, int32_t* err, void* stream) {
+  int st = check_chunk(kv, n_tokens, B, cu, pos);
+  if (st) return st;
+  if (!k_out || !v_out || out_stride < (long long)kv->n_kv_heads * kv->head_dim) return FP_ERR_INVALID_ARG;
+  if (out_stride % 8 || !aligned16(k_out) || !aligned16(v_out)) return FP_ERR_UNSUPPORTED;
+  return cuda_status(
+      launch_kv_read(*kv, n_tokens, B, cu, pos, k_out, v_out, out_stride, err, (cudaStream_t)stream));
+}
+
+// Query heads a KV head that one tile of 128 rows takes.
+static bool chunk_group_ok(int n_heads, int n_kv_heads) { return n_heads / n_kv_heads <= 128; }
+
+size_t fp_op_attention_chunk_workspace_bytes(int B, int n_heads, int n_kv_heads, int head_dim, int max_new) {
+  if (B <= 0 || n_heads <= 0 || n_kv_heads <= 0 || max_new <= 0) return 0;
+  if ((head_dim != 64 && head_dim != 128) || n_heads % n_kv_heads != 0 || !chunk_group_ok(n_heads, n_kv_heads)) return 0;
+  return attention_chunk_ws_bytes(B, n_heads, n_kv_heads, head_dim, max_new);
+}
+
+int fp_op_attention_chunk(const uint16_t* q, int q_stride, int n_tokens, int B, int n_heads, const fp_kv_view* kv,
+                          const int32_t* cu, const int32_t* pos, int max_new, int max_len, uint16_t* out,
+                          void* workspace, size_t workspace_bytes, int32_t* err, void* stream) {
+  int st = check_chunk(kv, n_tokens, B, cu, pos);
+  if (st) return st;
+  if (!q || !out || n_heads <= 0 || n_heads % kv->n_kv_heads != 0 || max_new < 0 || max_len < 0)
+    return FP_ERR_INVALID_ARG;
+  if (q_stride < (long long)n_heads * kv->head_dim) return FP_ERR_INVALID_ARG;
+  if (!chunk_group_ok(n_heads, kv->n_kv_heads)) return FP_ERR_UNSUPPORTED;
+  if (q_stride % 8 || !aligned16(q) || !aligned16(out)) return FP_ERR_UNSUPPORTED;
+  if (max_len > (long long)kv->pages_per_seq * kv->page_size) return FP_ERR_CAPACITY;
+  if (n_tokens == 0 || B == 0 || max_new == 0 || max_len == 0) return FP_OK;
+  if (!workspace || ((uintptr_t)workspace & 255) ||
+      workspace_bytes < attention_chunk_ws_bytes(B, n_heads, kv->n_kv_heads, kv->head_dim, max_new))
+    return FP_ERR_INVALID_ARG;
+  return cuda_status(launch_attention_chunk(q, q_stride, n_tokens, B, n_heads, *kv, cu, pos, max_new, max_len, out,
+                                            workspace, err, (cudaStream_t)stream));
+}
+
+int fp_op_softmax(const float* logits, int M, int V, const float* temperature, float* probs, int32_t* err,
+                  void* stream) {
+  if (!logits || !probs || M < 0 || V <= 0) return FP_ERR_INVALID_ARG;
+  return cuda_status(launch_softmax(logits, M, V, temperature, probs, err, (cudaStream_t)stream));
+}
+
+int fp_op_verify_draft(const float* p, const float* q, int V, int n_tokens, int B, const int32_t* cu,
+                       const int32_t* tokens, const float* u_accept, const float* u_draw, int32_t* out_tokens,
+                       int32_t* n_out, int32_t* err, void* stream) {
+  if (!p || V <= 0 || n_tokens < 0 || B < 0 || !cu || !tokens || !u_accept || !u_draw || !out_tokens || !n_out)
+    return FP_ERR_INVALID_ARG;
+  if (V > (1 << 30) || B > (1 << 27)) return FP_ERR_UNSUPPORTED;
+  return cuda_status(launch_verify_draft(p, q, V, n_tokens, B, cu, tokens, u_accept, u_draw, out_tokens, n_out, err,
+                                         (cudaStream_t)stream));
+}
+
 }  // extern "C"

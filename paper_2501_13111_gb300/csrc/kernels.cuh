@@ -53,6 +53,24 @@ cudaError_t launch_attention_prefill_tc(const uint16_t* q, int q_stride, int B, 
 cudaError_t launch_attention_prefill(const uint16_t* q, int q_stride, int B, int S, int n_heads,
                                      const fp_kv_view& kv, uint16_t* out, int32_t* err, cudaStream_t s);
 
+// ---- ragged chunks of new tokens (fp_chunk.cu, fp_attn_chunk.cu)
+cudaError_t launch_rope_kv_chunk(const uint16_t* qkv, int row_stride, int n_tokens, int B, int n_heads,
+                                 const fp_kv_view& kv, const int32_t* cu, const int32_t* pos, const float* rope_cs,
+                                 uint16_t* q_out, int q_out_stride, int32_t* err, cudaStream_t s);
+cudaError_t launch_kv_read(const fp_kv_view& kv, int n_tokens, int B, const int32_t* cu, const int32_t* pos,
+                           uint16_t* k_out, uint16_t* v_out, int out_stride, int32_t* err, cudaStream_t s);
+size_t attention_chunk_ws_bytes(int B, int n_heads, int n_kv_heads, int head_dim, int max_new);
+cudaError_t launch_attention_chunk(const uint16_t* q, int q_stride, int n_tokens, int B, int n_heads,
+                                   const fp_kv_view& kv, const int32_t* cu, const int32_t* pos, int max_new, int max_len,
+                                   uint16_t* out, void* ws, int32_t* err, cudaStream_t s);
+
+// ---- probabilities and draft verification (fp_verify.cu)
+cudaError_t launch_softmax(const float* logits, int M, int V, const float* temp, float* probs, int32_t* err,
+                           cudaStream_t s);
+cudaError_t launch_verify_draft(const float* p, const float* q, int V, int n_tokens, int B, const int32_t* cu,
+                                const int32_t* tokens, const float* u, const float* r, int32_t* out, int32_t* n_out,
+                                int32_t* err, cudaStream_t s);
+
 // ---- weight-only linear (fp_linear.cu)
 // Split-K ticket counters at the head of a linear's workspace (zero at rest).
 constexpr int kLinTicketSlots = 4096;
