@@ -1,0 +1,105 @@
+// How the attention of a chunk is cut up (fp_attn_chunk.cu).  Host and device.
+//
+// The G query heads of a KV head read the same keys, so their rows are packed:
+// row r of a query tile is token r / G, head r % G; a tile holds the largest power of
+// two of tokens with at most 128 rows, a unit up to two tiles of one (sequence, KV
+// head).  The units, sequence by sequence, KV head by KV head, lie on a line, each
+// with kCkStart + (its key tiles) places: what starting it costs beside a key tile,
+// and its key tiles.  CTA c of g takes an equal stretch of that line, so every SM
+// reads as many keys whatever the lengths are; a unit that a border cuts leaves a
+// partial result with every CTA, and a second kernel adds them.
+#pragma once
+
+#include <algorithm>
+#include <cstdint>
+
+#ifdef __CUDACC__
+#define FP_CK __host__ __device__ __forceinline__
+#else
+#define FP_CK inline
+#endif
+
+namespace fpk {
+
+constexpr int kCkKeys = 128;  // keys a tile, and rows a query tile
+constexpr int kCkStart = 2;
+constexpr int kCkSnap = 2;      // key tiles at a unit's ends that a border does not cut off
+constexpr int kCkLeast = 4;     // places a CTA takes at least
+
+// Tokens of a query tile.
+FP_CK int ck_tile_tokens(int G) {
+  int t = 128;
+  while (t * G > 128) t >>= 1;
+  return t;
+}
+
+// One sequence's chunk, after its lengths have been looked over.
+struct CkSeq {
+  int row0, n;  // first row, rows
+  int pos;      // position of the first row
+  int end;      // cached positions that it reads (its last row's, at most max_len)
+  int units;
+  bool bad;     // lengths beyond the bounds: every unit is given all key tiles
+
+  // first and count as in cu, position p; false: a bound is broken
+  FP_CK bool set(int first, int count, int p, int tile_tokens, int max_new, int max_len) {
+    row0 = first;
+    n = count < max_new ? count : max_new;
+    pos = p;
+    const long long e = (long long)p + n;
+    end = (int)(e < 0 ? 0 : e > max_len ? max_len : e);
+    bad = n > 0 && (p < 0 || e > max_len);
+    units = (n + 2 * tile_tokens - 1) / (2 * tile_tokens);
+    return !bad && count <= max_new;
+  }
+  FP_CK int all_tiles() const { return (end + kCkKeys - 1) / kCkKeys; }
+  // key tiles of unit u (T: tokens a unit)
+  FP_CK int tiles(int u, int T) const {
+    return bad || u == units - 1 ? all_tiles() : (pos + (u + 1) * T + kCkKeys - 1) / kCkKeys;
+  }
+  // key tiles of units 0 .. u-1, u < units
+  FP_CK long long tiles_before(int u, int T) const {
+    if (bad) return (long long)u * all_tiles();
+    if (T > kCkKeys)  // 256
+      return (long long)u * ((pos + kCkKeys - 1) / kCkKeys) + (long long)u * (u + 1);
+    // ceil((pos + i T) / 128) = ceil((ceil(pos / T) + i) / r), r = 128 / T
+    const int r = kCkKeys / T;
+    const long long a = (pos + T - 1) / T;
+    return upto(a + u, r) - upto(a, r);
+  }
+  static FP_CK long long upto(long long m, int r) {  // sum of ceil(j / r), j = 1 .. m
+    const long long q = m / r, rem = m % r;
+    return r * q * (q + 1) / 2 + rem * (q + 1);
+  }
+  FP_CK long long before(int u, int T) const { return (long long)u * kCkStart + tiles_before(u, T); }
+  // places of one KV head's units
+  FP_CK long long cost(int T) const {
+    return units == 0 ? 0 : before(units - 1, T) + kCkStart + all_tiles();
+  }
+  // the unit that holds place x < cost
+  FP_CK int unit_at(long long x, int T) const {
+    int lo = 0, hi = units;  // before(lo) <= x
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (before(mid, T) <= x) lo = mid;
+      else hi = mid;
+    }
+    return lo;
+  }
+};
+
+// A border at place `off` of a unit of nt key tiles, moved off its ends: the place to
+// cut at, 0 (before the unit) or kCkStart + nt (behind it).
+FP_CK int ck_snap(int off, int nt) {
+  if (off < kCkStart + kCkSnap) return 0;
+  if (off > kCkStart + nt - kCkSnap) return kCkStart + nt;
+  return off;
+}
+
+// CTAs that take part of W places.
+FP_CK int ck_ctas(long long W, int grid) {
+  const long long most = W / kCkLeast > 1 ? W / kCkLeast : 1;
+  return most < grid ? (int)most : grid;
+}
+
+}  // namespace fpk
