@@ -53,31 +53,31 @@ struct CkSeq {
     return !bad && count <= max_new;
   }
   FP_CK int all_tiles() const { return (end + kCkKeys - 1) / kCkKeys; }
-  // key tiles of unit u (T: tokens a unit)
+  // key tiles of unit u (T: tokens a unit, a power of two)
   FP_CK int tiles(int u, int T) const {
     return bad || u == units - 1 ? all_tiles() : (pos + (u + 1) * T + kCkKeys - 1) / kCkKeys;
   }
   // key tiles of units 0 .. u-1, u < units
-  FP_CK long long tiles_before(int u, int T) const {
-    if (bad) return (long long)u * all_tiles();
-    if (T > kCkKeys)  // 256
-      return (long long)u * ((pos + kCkKeys - 1) / kCkKeys) + (long long)u * (u + 1);
-    // ceil((pos + i T) / 128) = ceil((ceil(pos / T) + i) / r), r = 128 / T
-    const int r = kCkKeys / T;
-    const long long a = (pos + T - 1) / T;
-    return upto(a + u, r) - upto(a, r);
+  FP_CK int tiles_before(int u, int T) const {
+    if (bad) return u * all_tiles();
+    const int a0 = (pos + kCkKeys - 1) / kCkKeys;
+    if (T > kCkKeys) return u * a0 + u * (u + 1);  // 256
+    // ceil((pos + i T) / 128): the first unit ends in tile a0 or the next, and every
+    // 128 / T = 2^lg units move on by one tile
+    int lg = 0;
+    while ((T << lg) < kCkKeys) ++lg;
+    const int k = (a0 * kCkKeys - pos) >> (7 - lg);  // units that end within tile a0's keys
+    if (u <= k) return u * a0;
+    const int v = u - k, q = v >> lg, rem = v & ((1 << lg) - 1);
+    return u * a0 + (((q * (q + 1)) >> 1) << lg) + rem * (q + 1);
   }
-  static FP_CK long long upto(long long m, int r) {  // sum of ceil(j / r), j = 1 .. m
-    const long long q = m / r, rem = m % r;
-    return r * q * (q + 1) / 2 + rem * (q + 1);
-  }
-  FP_CK long long before(int u, int T) const { return (long long)u * kCkStart + tiles_before(u, T); }
-  // places of one KV head's units
-  FP_CK long long cost(int T) const {
+  FP_CK int before(int u, int T) const { return u * kCkStart + tiles_before(u, T); }
+  // places of one KV head's units (ck_fits: below 2^31)
+  FP_CK int cost(int T) const {
     return units == 0 ? 0 : before(units - 1, T) + kCkStart + all_tiles();
   }
   // the unit that holds place x < cost
-  FP_CK int unit_at(long long x, int T) const {
+  FP_CK int unit_at(int x, int T) const {
     int lo = 0, hi = units;  // before(lo) <= x
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
@@ -88,6 +88,12 @@ struct CkSeq {
   }
 };
 
+// Whether a sequence's places, over all KV heads, stay below 2^31 whatever its lengths.
+inline bool ck_fits(int n_tokens, int max_new, int max_len, int Hkv, int tile_tokens) {
+  const long long units = ((long long)std::min(n_tokens, max_new) + 2 * tile_tokens - 1) / (2 * tile_tokens);
+  return units * Hkv * (kCkStart + (max_len + kCkKeys - 1LL) / kCkKeys) < (1LL << 31);
+}
+
 // A border at place `off` of a unit of nt key tiles, moved off its ends: the place to
 // cut at, 0 (before the unit) or kCkStart + nt (behind it).
 FP_CK int ck_snap(int off, int nt) {
@@ -96,9 +102,14 @@ FP_CK int ck_snap(int off, int nt) {
   return off;
 }
 
-// CTAs that take part of W places.
+// x y / z without a 64-bit division where the numbers are small.
+FP_CK long long ck_muldiv(long long x, int y, int z) {
+  return x < (1 << 22) ? (long long)((uint32_t)x * (uint32_t)y / (uint32_t)z) : x * y / z;
+}
+
+// CTAs that take part of W places (at most 1024).
 FP_CK int ck_ctas(long long W, int grid) {
-  const long long most = W / kCkLeast > 1 ? W / kCkLeast : 1;
+  const long long most = W / kCkLeast > 1 ? W / kCkLeast : 1;  // (kCkLeast: a power of two)
   return most < grid ? (int)most : grid;
 }
 

@@ -10,24 +10,30 @@
 // softmax groups, each with its own maximum, sum and accumulator, added at the end.
 // Tensor memory: the scores of each group (128 columns, P over them as bf16 pairs)
 // and its output accumulator.
-//   warps 0-15  softmax, two groups of 8: a thread has one query row (TMEM lane) and
-//               half of the tile's keys; the two halves of a row meet over their
-//               maximum in shared memory.  P = 2^(s - m) is rounded to bf16 for the
-//               second product (2^-8 of each p, the sums in fp32); the reference m
-//               moves only when a tile passes it by 2^8 (O and the row sum are
-//               rescaled then).  At the end of a unit they write its rows;
-//   warp 16     TMA: the unit's Q tiles (one box per 64 columns: tokens x heads) and,
-//               page by page, the keys; warp 18 the values.  One box a page, in the
-//               order [8 rows][64 columns] the descriptors step through;
-//   warp 17     owns the TMEM and issues the MMAs: O += P(t) V(t), then the group's
-//               next scores over the columns that P(t) has left;
-//   warps 20-23 (int8 cache) K and V tiles from the codes: bf16(q s), the values that
+//   warps 0-7   softmax, two groups of 4: one query row (TMEM lane) a thread.
+//               P = 2^(s - m) is rounded to bf16 for the second product (2^-8 of each
+//               p, the sums in fp32); the reference m moves only when a tile passes it
+//               by 2^8 (O and the row sum are rescaled then).  P goes out in two halves
+//               of 64 keys, so that the first half's products run while the second
+//               half is computed.  At the end of a piece they write its rows;
+//   warp 8      TMA: the unit's Q tiles (one box per 64 columns: tokens x heads) and,
+//               page by page, the keys.  One box a page, in the order [8 rows][64
+//               columns] the descriptors step through;
+//   warps 9, 10 issue the MMAs of a group each: O += P(t) V(t), then the group's next
+//               scores over the columns that P(t) has left.  (One warp for both groups
+//               left the tensor pipe idle for half of each step: a wait costs 100-200
+//               cycles while the operands' reads fill shared memory's bandwidth, and
+//               there were five in a row.)  Warp 9 owns the TMEM;
+//   warp 11     plans the CTA's stretch, describes its pieces of units to the others,
+//               and (bf16 cache) copies the values;
+//   warps 12-19 (int8 cache) K and V tiles from the codes: bf16(q s), the values that
 //               fp_op_kv_read returns (a byte permute gives fp32 2^15 + 128 + q, an exact
 //               subtraction q; 2^-8 of a value, as a bf16 cache's own rounding).
 // Slots behind the sequence's last position may hold anything: their scores are
 // masked, their V rows are zeroed before the product.
 // Every wait on an mbarrier is bounded (error 2 past the limit).
 #include <algorithm>
+#include <type_traits>
 
 #include "attn_tc.cuh"
 #include "chunk.cuh"
@@ -36,15 +42,24 @@
 
 namespace fpk {
 
-constexpr int kCkSoft = 16;                       // softmax warps
-constexpr int kCkWarpQ = 16, kCkWarpMma = 17, kCkWarpV = 18, kCkWarpWiden = 20;
+constexpr int kCkSoft = 8;                        // softmax warps
+constexpr int kCkWarpQ = 8, kCkWarpMma = 9, kCkWarpPlan = 11, kCkWarpWiden = 12, kCkWiden = 8;
 template <bool KV8>
-constexpr int ck_threads() { return KV8 ? 768 : 640; }
-// Registers, moved to the softmax: 640 threads launch with 96, 512 x 104 + 128 x 64 =
-// 640 x 96; 768 (int8 cache) with 80, 512 x 88 + 256 x 64 = 768 x 80
+constexpr int ck_threads() { return KV8 ? (kCkWarpWiden + kCkWiden) * 32 : 384; }
+// Registers a thread, moved to the softmax, which holds a row of scores (int8 cache:
+// half of one): 384 threads launch with 168, 256 x 208 + 128 x 88 = 384 x 168; 640 with
+// 96, 256 x 128 + 384 x 72 <= 640 x 96
+template <bool KV8>
+constexpr int ck_reg_soft() { return KV8 ? 128 : 208; }
+template <bool KV8>
+constexpr int ck_reg_other() { return KV8 ? 72 : 88; }
+// Warps that read each piece's description: softmax, Q, MMA and the widening ones.
+template <bool KV8>
+constexpr int ck_readers() { return kCkSoft + 3 + (KV8 ? kCkWiden : 0); }
+constexpr int kCkPieces = 4;                      // pieces described ahead
 constexpr int kCkRing = 2;                        // K tiles in shared memory, and V tiles
 constexpr uint32_t kCkTmemCols = 512, kCkO = 256; // O of group j at kCkO + 128 j, its scores at 128 j
-constexpr int kCkStage = 32 * 32;                 // a warp's 32 output rows, 16 columns at a time
+constexpr int kCkStage = 32 * 64;                 // a warp's 32 output rows, 32 columns at a time
 constexpr float kCkSlack = 8.f;                   // log2 of the largest P before the reference moves
 constexpr int kCkRows = 256;                      // rows of a unit
 template <int HD>
@@ -57,7 +72,7 @@ constexpr int ck_smem() { return (2 + 2 * kCkRing) * ck_tile_bytes<HD>() + kCkSo
 // slot 1: of the one it left): fp32 O as [HD / 4][256 rows][4], then (m, l) [256 rows].
 struct CkLeft {
   long long end;  // the unit's end on the line; 0: none was left
-  int row0, i0, n, kvh, pair;
+  int row0, n, kvh;
 };
 constexpr size_t kCkHead = 64 * 1024;  // begins and CkLeft of up to 1024 CTAs
 template <int HD>
@@ -79,29 +94,26 @@ FP_DEV void ck_tma_4d(void* dst, const CUtensorMap* map, int x, int y, int z, in
       ::"r"(smem_u32(dst)), "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(smem_u32(bar))
       : "memory");
 }
-FP_DEV float2 ck_fma2(float2 a, float2 b, float2 c) {
-  float2 d;
-  asm("{\n .reg .b64 a, b, c, d;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n mov.b64 c, {%6, %7};\n"
-      " fma.rn.f32x2 d, a, b, c;\n mov.b64 {%0, %1}, d;\n}\n"
-      : "=f"(d.x), "=f"(d.y)
-      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
-  return d;
-}
-FP_DEV float2 ck_add2(float2 a, float2 b) {
-  float2 d;
-  asm("{\n .reg .b64 a, b, d;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n"
-      " add.rn.f32x2 d, a, b;\n mov.b64 {%0, %1}, d;\n}\n"
-      : "=f"(d.x), "=f"(d.y)
-      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-  return d;
-}
-
-FP_DEV float2 ck_mul2(float2 a, float2 b) {
-  float2 d;
-  asm("{\n .reg .b64 a, b, d;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n"
-      " mul.rn.f32x2 d, a, b;\n mov.b64 {%0, %1}, d;\n}\n"
-      : "=f"(d.x), "=f"(d.y)
-      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+#define CK_F32X2(name, op, args, ...)                                                                       \
+  FP_DEV float2 name args {                                                                                 \
+    float2 d;                                                                                               \
+    asm("{\n .reg .b64 a, b, c, d;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n mov.b64 c, {%6, %7};\n " \
+        op "\n mov.b64 {%0, %1}, d;\n}\n"                                                                  \
+        : "=f"(d.x), "=f"(d.y)                                                                              \
+        : __VA_ARGS__);                                                                                     \
+    return d;                                                                                               \
+  }
+// Two fp32 lanes at once: a b + c, a b, a + b.
+CK_F32X2(ck_fma2, "fma.rn.f32x2 d, a, b, c;", (float2 a, float2 b, float2 c), "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y),
+         "f"(c.x), "f"(c.y))
+CK_F32X2(ck_mul2, "mul.rn.f32x2 d, a, b;", (float2 a, float2 b), "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(0.f),
+         "f"(0.f))
+CK_F32X2(ck_add2, "add.rn.f32x2 d, a, b;", (float2 a, float2 b), "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(0.f),
+         "f"(0.f))
+#undef CK_F32X2
+FP_DEV float ck_max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
   return d;
 }
 
@@ -118,27 +130,106 @@ struct CkArgs {
   int32_t* err;
 };
 
-// A place on the line: unit u of KV head kvh of sequence b, `off` places into it.
-struct CkAt {
-  int b, kvh, u, off;
-  long long x;  // its place on the line
+// A piece of a unit, as the planning warp describes it.
+struct __align__(16) CkPiece {
+  int t0, t1, e0;   // key tiles t0 .. t1-1; where the first of two tiles' end
+  int flags;
+  int row0, n, pos; // the unit's first row, its rows (tokens), the first one's position
+  int end;          // cached positions of the sequence that may be read
+  int b, kvh;
+  long long stop;   // the unit's end on the line
+  FP_DEV bool pair() const { return flags & 1; }    // two query tiles
+  FP_DEV bool first() const { return flags & 2; }   // the unit's first part
+  FP_DEV bool last() const { return flags & 4; }
+  FP_DEV bool done() const { return flags & 8; }    // no piece: the stretch is walked
+  FP_DEV bool empty() const { return t1 <= t0; }
+  FP_DEV bool uses(int j) const { return pair() ? (j ? t1 > t0 : e0 > t0) : t1 - t0 > j; }  // accumulator j
 };
 
-// The pieces of units that a stretch of `len` places from `at` takes.
+// The plan of this CTA's stretch, by one whole warp, and its pieces one by one.
 struct CkWalk {
   const CkArgs& a;
   CkSeq s;
-  int b, kvh, u, off;
-  long long x, rem;
-  // the present piece: unit u of (b, kvh), key tiles t0 .. t1-1 of nt (0: no keys)
-  int t0, t1, nt, nt0, i0;
-  bool pair, first, last;  // two tiles; the unit's first / last part
-  FP_DEV CkWalk(const CkArgs& a, const CkAt& at, long long len)
-      : a(a), b(at.b), kvh(at.kvh), u(at.u), off(at.off), x(at.x), rem(at.b < a.B ? len : 0) {
+  int b, kvh, u, off;  // the next place: `off` into unit u of (b, kvh)
+  long long x, rem;    // its place on the line, and places left
+  FP_DEV int places(int bb) {  // of sequence bb; bounds that are broken are reported
+    int first, count;
+    const int lo = __ldg(a.cu + bb), hi = __ldg(a.cu + bb + 1), p = __ldg(a.pos + bb);
+    first = max(lo, 0);
+    count = max(0, min(hi, a.n_tokens) - first);
+    const bool fine = s.set(first, count, p, a.tile_tokens, a.max_new, a.max_len);
+    if ((!fine || lo < 0 || hi < lo || hi > a.n_tokens) && blockIdx.x == 0 && a.err) atomicExch(a.err, 1);
+    return s.cost(2 * a.tile_tokens) * a.Hkv;
+  }
+  FP_DEV CkWalk(const CkArgs& a) : a(a) {
+    const int lane = threadIdx.x & 31, T = 2 * a.tile_tokens;
+    // the line's length (up to 32 sequences: their places stay in the lanes)
+    long long W = 0;
+    int c = 0;
+#pragma unroll 1
+    for (int b0 = 0; b0 < a.B; b0 += 32) {
+      c = b0 + lane < a.B ? places(b0 + lane) : 0;
+      W += c;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) W += __shfl_xor_sync(0xffffffffu, W, o);
+    const int g = ck_ctas(W, gridDim.x), cta = blockIdx.x;
+    const long long x0 = cta < g ? ck_muldiv(W, cta, g) : W, x1 = cta + 1 < g ? ck_muldiv(W, cta + 1, g) : W;
+    b = a.B, kvh = u = off = 0;
+    x = W;
+    long long stop = W, base = 0;
+#pragma unroll 1
+    for (int b0 = 0; b0 < a.B && x0 < W; b0 += 32) {
+      if (a.B > 32) c = b0 + lane < a.B ? places(b0 + lane) : 0;
+      long long incl = c;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const long long f = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += f;
+      }
+      incl += base;
+      base = __shfl_sync(0xffffffffu, incl, 31);
+#pragma unroll 1
+      for (int e = 0; e < 2; ++e) {
+        const long long at = e ? x1 : x0, before = incl - c;
+        if (c == 0 || at < before || at >= incl) continue;
+        // one lane gets here: the unit at this place, and its border off the unit's ends
+        const int per = s.cost(T), d = (int)(at - before), h = (int)((unsigned)d / (unsigned)per), in = d - h * per;
+        const int v = s.unit_at(in, T), start = s.before(v, T), nt = s.tiles(v, T), o = ck_snap(in - start, nt);
+        const long long to = before + (long long)h * per + start + o;
+        if (e) {
+          stop = to;
+        } else {
+          x = to, b = b0 + lane, kvh = h, u = v, off = o;
+          if (o == kCkStart + nt) {  // behind the unit: the next one's beginning
+            off = 0;
+            if (++u == s.units) u = 0, ++kvh;
+          }
+        }
+      }
+      const unsigned m0 = __ballot_sync(0xffffffffu, x < W || b < a.B), m1 = __ballot_sync(0xffffffffu, stop < W);
+      if (m0) {
+        const int l = __ffs(m0) - 1;
+        x = __shfl_sync(0xffffffffu, x, l), b = __shfl_sync(0xffffffffu, b, l), kvh = __shfl_sync(0xffffffffu, kvh, l);
+        u = __shfl_sync(0xffffffffu, u, l), off = __shfl_sync(0xffffffffu, off, l);
+      }
+      if (m1) {
+        stop = __shfl_sync(0xffffffffu, stop, __ffs(m1) - 1);
+        break;
+      }
+    }
+    rem = b < a.B ? stop - x : 0;
+    s.units = 0;
     if (rem > 0) {
       load();
+      if (kvh == a.Hkv) kvh = 0, s.units = 0;
       skip();
     }
+  }
+  FP_DEV void load() {
+    int first, count;
+    chunk_rows(a.cu, b, a.n_tokens, &first, &count);
+    s.set(first, count, __ldg(a.pos + b), a.tile_tokens, a.max_new, a.max_len);
   }
   // on to a sequence that has rows (there is one while places are left)
   FP_DEV void skip() {
@@ -146,26 +237,21 @@ struct CkWalk {
       if (b + 1 < a.B) ++b, load();
       else rem = 0;
   }
-  FP_DEV void load() {
-    int first, count;
-    chunk_rows(a.cu, b, a.n_tokens, &first, &count);
-    s.set(first, count, __ldg(a.pos + b), a.tile_tokens, a.max_new, a.max_len);
-  }
-  FP_DEV bool next() {
-    if (rem <= 0) return false;
-    const int T = 2 * a.tile_tokens;
-    nt = s.tiles(u, T);
-    i0 = u * T;
-    pair = s.n - i0 > a.tile_tokens;
+  FP_DEV void next(CkPiece* p) {
+    if (rem <= 0) {
+      p->flags = 8;
+      return;
+    }
+    const int T = 2 * a.tile_tokens, nt = s.tiles(u, T), i0 = u * T;
+    const bool pair = s.n - i0 > a.tile_tokens;
+    const int left = kCkStart + nt - off, take = (int)(left < rem ? left : rem);
+    p->t0 = max(0, off - kCkStart);
+    p->t1 = min(nt, max(0, off + take - kCkStart));
     // the first tile's own last key tile
-    nt0 = s.bad || !pair ? nt : (s.pos + i0 + a.tile_tokens + kCkKeys - 1) / kCkKeys;
-    const long long left = kCkStart + nt - off;
-    const int take = (int)(left < rem ? left : rem);
-    t0 = max(0, off - kCkStart);
-    t1 = min(nt, max(0, off + take - kCkStart));
-    first = off == 0;
-    last = take == left;
-    ub = b, ukvh = kvh, us = s, ux = x - off;
+    p->e0 = min(p->t1, s.bad || !pair ? nt : (s.pos + i0 + a.tile_tokens + kCkKeys - 1) / kCkKeys);
+    p->flags = (pair ? 1 : 0) | (off == 0 ? 2 : 0) | (take == left ? 4 : 0);
+    p->row0 = s.row0 + i0, p->n = min(T, s.n - i0), p->pos = s.pos + i0, p->end = s.end;
+    p->b = b, p->kvh = kvh, p->stop = x - off + kCkStart + nt;
     rem -= take;
     x += take;
     off = 0;
@@ -177,14 +263,7 @@ struct CkWalk {
         skip();
       }
     }
-    return true;
   }
-  // of the present piece (b, kvh, u, s are the next one's)
-  int ub, ukvh;
-  CkSeq us;
-  long long ux;  // where its unit begins
-  FP_DEV bool uses(int j) const { return pair ? (j ? true : t0 < nt0) && t1 > t0 : t1 - t0 > j; }
-  FP_DEV int end_of(int j) const { return pair && j == 0 ? min(t1, nt0) : t1; }
 };
 
 template <int HD, bool KV8>
@@ -193,393 +272,353 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
                       const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CkArgs a) {
   constexpr int TILE = ck_tile_bytes<HD>(), NH = HD / 64, SBO = NH * 1024, PAGE = 2 * SBO, R = kCkRing;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
-  __shared__ uint64_t qfull, qempty, kfull[R], kempty[R], vfull[R], vempty[R], sfull[2], pfull[2], ofull[2], oempty[2],
-      xch[2][4], met[4], mma_done;
-  __shared__ float s_x[2][2][2][kCkKeys];        // [group][parity][half][row]: what the halves of a row exchange
-  __shared__ float2 s_ml[2][2][2][kCkKeys];      // [parity][group][half][row]: maximum and sum, units of one tile
+  struct Bars {
+    uint64_t kfull[R], vfull[R], kempty[R], vempty[R], qfull, qempty, sfull[2], pfull[2][2], ofull[2], oempty[2], met[4], mma,
+        dfull[kCkPieces], dempty[kCkPieces], done[2];
+  };
+  __shared__ Bars bar;
+  __shared__ CkPiece s_piece[kCkPieces];
+  __shared__ float2 s_ml[2][2][kCkKeys];         // [parity][group][row]: maximum and sum, units of one tile
   __shared__ uint32_t tmem_base;
   __shared__ int abort_word;
-  __shared__ CkAt s_at[2];                       // where this CTA's stretch begins, and the next one's
-  __shared__ long long s_scan[32];
   volatile int* abort_flag = &abort_word;
   uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
   uint8_t* sQ = smem;
   uint8_t* sK = smem + 2 * TILE;
   uint8_t* sV = sK + R * TILE;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  constexpr int NT = ck_threads<KV8>(), NW = NT / 32;
   auto fail = [&]() {
     *abort_flag = 1;
     if (a.err) atomicExch(a.err, 2);
   };
 
   pdl_trigger();
-  if (threadIdx.x == 0) {
-    mbar_init(&qfull, 1);
-    mbar_init(&qempty, 1);
-    for (int i = 0; i < R; ++i) {
-      mbar_init(&kfull[i], KV8 ? 4 : 1);
-      mbar_init(&kempty[i], 1);
-      mbar_init(&vfull[i], KV8 ? 4 : 1);
-      mbar_init(&vempty[i], 1);
+  {
+    // arrivals of each barrier, in their order
+    constexpr int NB = sizeof(Bars) / 8;
+    uint64_t* p = reinterpret_cast<uint64_t*>(&bar);
+    for (int i = threadIdx.x; i < NB; i += ck_threads<KV8>()) {
+      const uint64_t* q = p + i;
+      int n = 1;
+      if (q < bar.kempty) n = KV8 ? kCkWiden : 1;
+      else if (q < &bar.qfull) n = 2;
+      else if (q == &bar.qempty || q == &bar.mma) n = 2;
+      else if (q >= &bar.pfull[0][0] && q < bar.ofull) n = 4;
+      else if (q >= bar.oempty && q < bar.met) n = 8;
+      else if (q >= bar.met && q < &bar.mma) n = 2;
+      else if (q >= bar.dempty && q < bar.done) n = ck_readers<KV8>();
+      mbar_init(p + i, n);
     }
-    for (int j = 0; j < 2; ++j) {
-      mbar_init(&sfull[j], 1);
-      mbar_init(&pfull[j], 8);
-      mbar_init(&ofull[j], 1);
-      mbar_init(&oempty[j], 16);
-      for (int i = 0; i < 4; ++i) mbar_init(&xch[j][i], 2);
-    }
-    for (int i = 0; i < 4; ++i) mbar_init(&met[i], 4);
-    mbar_init(&mma_done, 1);
-    *abort_flag = 0;
+    if (threadIdx.x == 0) *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == kCkWarpMma) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base)),
-                 "r"(kCkTmemCols)
-                 : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-  }
   pdl_wait();
-
-  // ---------------- the line: its length, and where this CTA's stretch begins and ends.
-  // Two passes over the sequences, the first for the sum (a batch of up to NT
-  // sequences has its costs in registers by then).
-  {
-    if (blockIdx.x == 0) chunk_check(a.cu, a.B, a.n_tokens, a.err);
-    const int T = 2 * a.tile_tokens;
-    auto cost = [&](int b, CkSeq& s) -> long long {
-      int first, count;
-      chunk_rows(a.cu, b, a.n_tokens, &first, &count);
-      const bool fine = s.set(first, count, __ldg(a.pos + b), a.tile_tokens, a.max_new, a.max_len);
-      if (!fine && a.err && blockIdx.x == 0) atomicExch(a.err, 1);
-      return s.cost(T) * a.Hkv;
-    };
-    // inclusive sum over the block of one value a thread, and the block's total
-    auto scan = [&](long long v, long long* total) {
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const long long f = __shfl_up_sync(0xffffffffu, v, o);
-        if (lane >= o) v += f;
-      }
-      __syncthreads();  // s_scan of the last call has been read
-      if (lane == 31) s_scan[warp] = v;
-      __syncthreads();
-      long long before = 0, all = 0;
-#pragma unroll
-      for (int i = 0; i < NW; ++i) {
-        const long long w = s_scan[i];
-        before += i < warp ? w : 0;
-        all += w;
-      }
-      *total = all;
-      return v + before;
-    };
-    CkSeq s;
-    long long W = 0, mine = 0, incl = 0;
-    for (int b0 = 0; b0 < a.B; b0 += NT) {
-      const int b = b0 + (int)threadIdx.x;
-      mine = b < a.B ? cost(b, s) : 0;
-      long long all;
-      incl = scan(mine, &all);
-      W += all;
-    }
-    const int g = ck_ctas(W, gridDim.x);
-    const int c = blockIdx.x;
-    if (threadIdx.x < 2) {  // nothing here, or the line's end
-      s_at[threadIdx.x] = {a.B, 0, 0, 0, W};
-    }
-    __syncthreads();
-    long long base = 0;
-    for (int b0 = 0; b0 < a.B; b0 += NT) {
-      const int b = b0 + (int)threadIdx.x;
-      if (a.B > NT) {
-        mine = b < a.B ? cost(b, s) : 0;
-        long long all;
-        incl = base + scan(mine, &all);
-        base += all;
-      }
-      const long long before = incl - mine;
-#pragma unroll 1
-      for (int e = 0; e < 2; ++e) {
-        const int k = c + e;
-        if (k >= g) continue;  // the end
-        const long long x = W * k / g;
-        if (mine == 0 || x < before || x >= incl) continue;
-        const long long per = mine / a.Hkv, in = (x - before) % per;
-        const int kvh = (int)((x - before) / per), u = s.unit_at(in, T), nt = s.tiles(u, T);
-        const long long start = s.before(u, T);
-        const int off = ck_snap((int)(in - start), nt);
-        CkAt at = {b, kvh, u, off, before + kvh * per + start + off};
-        if (off == kCkStart + nt) {  // behind the unit: the next one's beginning
-          at.off = 0;
-          if (++at.u == s.units) {
-            at.u = 0;
-            if (++at.kvh == a.Hkv) at.kvh = 0, ++at.b;
-          }
-        }
-        s_at[e] = at;
-      }
-    }
-  }
-  tc_fence_before();
   __syncthreads();
-  tc_fence_after();
-  const uint32_t tmem = tmem_base;
-  const CkAt at = s_at[0];
-  const long long len = s_at[1].x - at.x;
-  if (threadIdx.x == 0) {
-    reinterpret_cast<long long*>(a.ws)[blockIdx.x] = at.x;
-    reinterpret_cast<CkLeft*>(a.ws + kCkHead / 4)[blockIdx.x].end = 0;
-  }
 
-  if (warp >= kCkSoft) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(64));
-  }
-  if (warp == kCkWarpQ || (warp == kCkWarpV && !KV8)) {
-    // ---------------- TMA: warp 16 the Q tiles (and K), warp 18 V.  Lanes 0-7 copy a
-    // page of a key tile each; the next tile's page ids are read while this one is in
-    // flight.  A page behind the sequence's end, or a bad one, reads zeros.
-    const bool is_v = warp == kCkWarpV;
+  // The next piece, for a whole warp; false: the stretch is done, or (ok false) a wait ran out.
+  int pc = 0;
+  auto next = [&](CkPiece& w, bool& ok) {
+    const int i = pc % kCkPieces;
+    ok = __all_sync(0xffffffffu, mbar_wait(&bar.dfull[i], (pc / kCkPieces) & 1)) && !*abort_flag;
+    if (!__all_sync(0xffffffffu, ok)) return ok = false;
+    w = s_piece[i];
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&bar.dempty[i]);
+    ++pc;
+    return !w.done();
+  };
+
+  if (warp >= kCkSoft) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(ck_reg_other<KV8>()));
+  if (warp == kCkWarpPlan || warp == kCkWarpQ) {
+    // ---------------- warp 11: the plan, the pieces, V.  Warp 8: Q tiles and K.  Lanes
+    // 0-7 copy a page of a key tile each; the next tile's page ids are read while this
+    // one is in flight.  A page behind the sequence's end, or a bad one, reads zeros.
+    const bool is_v = warp == kCkWarpPlan;
     const CUtensorMap* map = is_v ? &map_v : &map_k;
-    uint64_t *full = is_v ? vfull : kfull, *empty = is_v ? vempty : kempty;
+    uint64_t *full = is_v ? bar.vfull : bar.kfull, *empty = is_v ? bar.vempty : bar.kempty;
     uint8_t* dst = is_v ? sV : sK;
-    if (lane == 0) {
-      if (!is_v) asm volatile("prefetch.tensormap [%0];" ::"l"(&map_q) : "memory");
-      if (!KV8) asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
-    }
     int n = 0, kn = 0;
     bool ok = true;
-    CkWalk w(a, at, len);
-    while (ok && w.next()) {
-      if (w.t1 <= w.t0) continue;
-      if (!is_v) {
-        if (n > 0) ok = __all_sync(0xffffffffu, mbar_wait(&qempty, (n - 1) & 1)) && !*abort_flag;
-        if (!__all_sync(0xffffffffu, ok)) {
-          ok = false;
-          break;
-        }
-        if (lane == 0) {
-          const int tiles = w.pair ? 2 : 1;
-          mbar_expect_tx(&qfull, tiles * NH * a.tile_tokens * a.G * 128);
-          for (int j = 0; j < tiles; ++j)
-#pragma unroll
-            for (int h = 0; h < NH; ++h)
-              ck_tma_4d(sQ + j * TILE + h * (TILE / NH), &map_q, 0, h, w.ukvh * a.G,
-                        w.us.row0 + w.i0 + j * a.tile_tokens, &qfull);
-        }
-        ++n;
-        if (KV8) continue;
-      }
-      const int32_t* pt = a.page_table + (long long)w.ub * a.pages_per_seq;
+    auto copy = [&](const CkPiece& w) {
+      const int32_t* pt = a.page_table + (long long)w.b * a.pages_per_seq;
       auto page_row = [&](int t) {  // 8-row group of this lane's page; -2 reads zeros
         const int key0 = t * kCkKeys + lane * 16;
-        if (lane >= 8 || key0 >= w.us.end) return -2;
+        if (KV8 || lane >= 8 || key0 >= w.end) return -2;
         const int id = __ldg(pt + key0 / 16);
-        if (id >= 0 && id < a.n_pages) return (id * a.Hkv + w.ukvh) * 2;
+        if (id >= 0 && id < a.n_pages) return (id * a.Hkv + w.kvh) * 2;
         if (a.err && !is_v) atomicExch(a.err, 1);
         return -2;
       };
       int row = page_row(w.t0);
-      for (int t = w.t0; t < w.t1; ++t, ++kn) {
-        const int s = kn % R;
-        if (kn >= R) ok = mbar_wait(&empty[s], ((kn / R) & 1) ^ 1);
-        ok = __all_sync(0xffffffffu, ok && !*abort_flag);
-        if (!ok) break;
-        if (lane == 0) mbar_expect_tx(&full[s], TILE);
+      if (!is_v) {
+        if (n > 0) ok = mbar_wait(&bar.qempty, (n - 1) & 1) && !*abort_flag;
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) return;
+        if (lane == 0) {
+          const int tiles = w.pair() ? 2 : 1;
+          mbar_expect_tx(&bar.qfull, tiles * NH * a.tile_tokens * a.G * 128);
+#pragma unroll 1
+          for (int j = 0; j < tiles; ++j)
+#pragma unroll
+            for (int h = 0; h < NH; ++h)
+              ck_tma_4d(sQ + j * TILE + h * (TILE / NH), &map_q, 0, h, w.kvh * a.G, w.row0 + j * a.tile_tokens, &bar.qfull);
+        }
+        ++n;
+      }
+      if constexpr (!KV8) {
+        for (int t = w.t0; t < w.t1; ++t, ++kn) {
+          const int s = kn % R;
+          if (kn >= R) ok = mbar_wait(&empty[s], ((kn / R) & 1) ^ 1);
+          ok = __all_sync(0xffffffffu, ok && !*abort_flag);
+          if (!ok) return;
+          if (lane == 0) mbar_expect_tx(&full[s], TILE);
+          __syncwarp();
+          if (lane < 8) ck_tma_4d(dst + s * TILE + lane * PAGE, map, 0, 0, 0, row, &full[s]);
+          if (t + 1 < w.t1) row = page_row(t + 1);
+        }
+      }
+    };
+    if (is_v) {
+      CkWalk walk(a);
+      if (lane == 0) {
+        reinterpret_cast<long long*>(a.ws)[blockIdx.x] = walk.x;
+        reinterpret_cast<CkLeft*>(a.ws + kCkHead / 4)[blockIdx.x].end = 0;
+      }
+      // piece m + 1 is described before the values of piece m are copied
+      CkPiece w, w1;
+      auto tell = [&](int m, CkPiece* p) {
+        walk.next(p);
+        const int i = m % kCkPieces;
+        if (m >= kCkPieces) ok = __all_sync(0xffffffffu, mbar_wait(&bar.dempty[i], ((m / kCkPieces) & 1) ^ 1)) && !*abort_flag;
+        if (!__all_sync(0xffffffffu, ok)) {
+          ok = false;
+          return;
+        }
+        if (lane == 0) {
+          s_piece[i] = *p;
+          mbar_arrive(&bar.dfull[i]);
+        }
         __syncwarp();
-        if (lane < 8) ck_tma_4d(dst + s * TILE + lane * PAGE, map, 0, 0, 0, row, &full[s]);
-        if (t + 1 < w.t1) row = page_row(t + 1);
+      };
+      tell(0, &w);
+      for (int m = 0; ok && !w.done(); ++m) {
+        tell(m + 1, &w1);
+        if (ok && !w.empty() && !KV8) copy(w);
+        w = w1;
+      }
+    } else {
+      CkPiece w;
+      while (next(w, ok)) {
+        if (!w.empty()) copy(w);
+        if (!ok) break;
       }
     }
     if (!ok && lane == 0) fail();
     if (lane == 0) {  // copies still in flight land before the CTA leaves
-      if (!is_v && n > 0) mbar_wait(&qfull, (n - 1) & 1);
+      if (!is_v && n > 0) mbar_wait(&bar.qfull, (n - 1) & 1);
       if (!KV8)
         for (int t = max(0, kn - R); t < kn; ++t) mbar_wait(&full[t % R], (t / R) & 1);
     }
-  } else if (warp == kCkWarpMma) {
-    // ---------------- MMA issuer: every lane runs the loop, one issues.
-    constexpr uint32_t idesc_s = tc_idesc(kCkKeys, kCkKeys), idesc_o = tc_idesc(kCkKeys, HD) | (1u << 16);
-    const uint64_t qd = sdesc(smem_u32(sQ)), kd = ck_sdesc_k(smem_u32(sK), SBO),
-                   vd = ck_sdesc_mn(smem_u32(sV), 1024, SBO);
-    int n = 0, kn = 0, pn[2] = {0, 0}, on[2] = {0, 0};
-    bool ok = true;
-    // descriptor start addresses count 16-byte units
-    auto scores = [&](int j, int q, int s) {  // S_j = Q_q K^T of ring tile s (issuing lane only)
-      const uint64_t qj = qd + q * (TILE >> 4), ks = kd + s * (TILE >> 4);
+  } else if (warp == kCkWarpMma || warp == kCkWarpMma + 1) {
+    // ---------------- MMA issuers, a group each: every lane runs the loop, one issues.
+    // The group and the ring slot are constants of the code that issues, and an
+    // allocation of all 512 columns begins at column 0, so no operand has to be
+    // moved to a uniform register MMA by MMA.
+    if (warp == kCkWarpMma) {
+      asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base)),
+                   "r"(kCkTmemCols)
+                   : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+      tc_fence_before();
+    }
+    auto role = [&](auto cj) {
+      constexpr int j = decltype(cj)::value;
+      constexpr uint32_t idesc_s = tc_idesc(kCkKeys, kCkKeys), idesc_o = tc_idesc(kCkKeys, HD) | (1u << 16);
+      const uint64_t qd = sdesc(smem_u32(sQ)), kd = ck_sdesc_k(smem_u32(sK), SBO),
+                     vd = ck_sdesc_mn(smem_u32(sV), 1024, SBO);
+      int n = 0, kn = 0, pn = 0, on = 0;
+      bool ok = true;
+      // S_j = Q K^T of ring slot s (descriptor start addresses count 16-byte units)
+      auto scores_of = [&](auto cq, auto cs) {
+        constexpr int q = decltype(cq)::value, s = decltype(cs)::value;
 #pragma unroll
-      for (int kk = 0; kk < HD / 16; ++kk)
-        tc_mma(tmem + j * kCkKeys, qj + ((((kk >> 2) * (TILE / NH)) + (kk & 3) * 32) >> 4),
-               ks + (((kk >> 2) * 1024 + (kk & 3) * 32) >> 4), idesc_s, kk > 0 ? 1u : 0u);
-      tc_commit(&sfull[j]);
-    };
-    auto values = [&](int j, int s, bool first) {  // O_j (+)= P_j V of ring tile s (issuing lane only)
-      const uint64_t vs = vd + s * (TILE >> 4);
-#pragma unroll
-      for (int kk = 0; kk < kCkKeys / 16; ++kk)  // a page a step; P in two halves of 64 keys
-        tc_mma_ts(tmem + kCkO + j * 128, tmem + j * kCkKeys + (kk >> 2) * 64 + (kk & 3) * 8, vs + kk * (PAGE >> 4), idesc_o,
-                  (!first || kk > 0) ? 1u : 0u);
-    };
-    CkWalk w(a, at, len);
-    while (ok && w.next()) {
-      const int steps = w.t1 - w.t0;
-      if (steps <= 0) continue;
-      // V rows behind the sequence's last position, zeroed before they are multiplied
-      auto clean = [&](int t, int s) {
-        const int lo = w.us.end - t * kCkKeys;
-        if (KV8 || lo >= kCkKeys || (lo & 15) == 0) return;
-        const int page = lo >> 4;
-        for (int x = (lo & 15) * (HD / 8) + lane; x < 16 * (HD / 8); x += 32) {
-          const int r = x / (HD / 8), c = x % (HD / 8);  // whole rows: the swizzle stays inside them
-          *reinterpret_cast<uint4*>(sV + s * TILE + page * PAGE + (r >> 3) * SBO + (c >> 3) * 1024 + (r & 7) * 128 +
-                                    (c & 7) * 16) = make_uint4(0, 0, 0, 0);
-        }
-        fence_proxy_async();
-        __syncwarp();
+        for (int kk = 0; kk < HD / 16; ++kk)
+          tc_mma(j * kCkKeys, qd + ((q * TILE + (kk >> 2) * (TILE / NH) + (kk & 3) * 32) >> 4),
+                 kd + ((s * TILE + (kk >> 2) * 1024 + (kk & 3) * 32) >> 4), idesc_s, kk > 0 ? 1u : 0u);
+        tc_commit(&bar.sfull[j]);
       };
-      ok = mbar_wait(&qfull, n & 1) && mbar_wait(&kfull[kn % R], (kn / R) & 1) && !*abort_flag;
-      ok = __all_sync(0xffffffffu, ok);
-      if (!ok) break;
-      ++n;
-      tc_fence_after();
-      if (!w.pair) {
-        // one query tile: key tile t0 + i is group i % 2's, scores two tiles ahead
-        if (elect_one()) {
-          scores(0, 0, kn % R);
-          tc_commit(&kempty[kn % R]);
-          if (steps == 1) tc_commit(&qempty);
+      constexpr std::integral_constant<int, 0> c0;
+      constexpr std::integral_constant<int, 1> c1;
+      static_assert(R == 2, "two ring slots");
+      auto scores = [&](bool pair, int s) {
+        if (j && pair) {
+          if (s) scores_of(c1, c1);
+          else scores_of(c1, c0);
+        } else {
+          if (s) scores_of(c0, c1);
+          else scores_of(c0, c0);
         }
-        __syncwarp();
-        if (steps > 1) {
-          ok = __all_sync(0xffffffffu, mbar_wait(&kfull[(kn + 1) % R], ((kn + 1) / R) & 1));
-          if (!ok) break;
-          tc_fence_after();
-          if (elect_one()) {
-            scores(1, 0, (kn + 1) % R);
-            tc_commit(&kempty[(kn + 1) % R]);
-            if (steps == 2) tc_commit(&qempty);
-          }
-          __syncwarp();
-        }
-        for (int i = 0; i < steps && ok; ++i, ++kn) {
-          const int s = kn % R, j = i & 1;
-          const int p = j ? pn[1] : pn[0], o = j ? on[1] : on[0];
-          ok = mbar_wait(&vfull[s], (kn / R) & 1) &&
-               (i + 2 >= steps || mbar_wait(&kfull[s], ((kn + R) / R) & 1)) && mbar_wait(&pfull[j], p & 1) &&
-               (i > 1 || o == 0 || mbar_wait(&oempty[j], (o - 1) & 1)) && !*abort_flag;
-          ok = __all_sync(0xffffffffu, ok);
-          if (!ok) break;
-          clean(w.t0 + i, s);
-          tc_fence_after();
-          if (elect_one()) {
-            values(j, s, i < 2);
-            tc_commit(&vempty[s]);
-            if (i + 2 < steps) {
-              scores(j, 0, s);
-              tc_commit(&kempty[s]);
-            } else {
-              tc_commit(&ofull[j]);
-            }
-            if (i + 3 == steps) tc_commit(&qempty);
-          }
-          __syncwarp();
-          if (j) ++pn[1], on[1] += i + 2 >= steps;
-          else ++pn[0], on[0] += i + 2 >= steps;
-        }
-        continue;
-      }
-      const int e0 = w.end_of(0), e1 = w.t1;  // e0 <= e1: where each tile's keys end
-      if (elect_one()) {
-        if (w.t0 < e0) scores(0, 0, kn % R);
-        scores(1, 1, kn % R);
-        tc_commit(&kempty[kn % R]);
-        if (steps == 1) tc_commit(&qempty);
-      }
-      __syncwarp();
-      for (int t = w.t0; t < e1 && ok; ++t, ++kn) {
-        const int s = kn % R, s1 = (kn + 1) % R;
-        ok = mbar_wait(&vfull[s], (kn / R) & 1);
-        if (t + 1 < e1) ok = ok && mbar_wait(&kfull[s1], ((kn + 1) / R) & 1);
+      };
+      // O_j (+)= P_j V of ring slot s, half h of the keys: a page a step
+      auto values_of = [&](auto cs, auto ch, bool first) {
+        constexpr int s = decltype(cs)::value, h = decltype(ch)::value;
+        auto one = [&](int kk, uint32_t add) {
+          tc_mma_ts(kCkO + j * 128, j * kCkKeys + h * 64 + kk * 8, vd + ((s * TILE + (h * 4 + kk) * PAGE) >> 4), idesc_o, add);
+        };
+        if (h == 0 && first) one(0, 0);
+        else one(0, 1);
+#pragma unroll
+        for (int kk = 1; kk < 4; ++kk) one(kk, 1);
+      };
+      CkPiece w;
+      while (next(w, ok)) {
+        const int steps = w.t1 - w.t0;
+        if (steps <= 0) continue;
+        const bool pair = w.pair();
+        // this group's key tiles: piece tiles i0, i0 + di, .. below i1
+        const int i0 = pair ? 0 : j, di = pair ? 1 : 2, i1 = pair && j == 0 ? w.e0 - w.t0 : steps;
+        // the other group leaves tile i to this one: then both arrivals are this one's
+        auto alone = [&](int i) { return !pair || (j == 1 && i >= w.e0 - w.t0); };
+        auto release = [&](uint64_t* b, bool twice) {
+          tc_commit(b);
+          if (twice) tc_commit(b);
+        };
+        // both issuers have seen every tile of the pieces before (their phases are over)
+        if (lane == 0) mbar_arrive(&bar.mma);
+        ok = mbar_wait(&bar.mma, n & 1) && mbar_wait(&bar.qfull, n & 1) && !*abort_flag;
+        if (i0 < i1) ok = ok && mbar_wait(&bar.kfull[(kn + i0) % R], ((kn + i0) / R) & 1);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
-        clean(t, s);
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const int e = j ? e1 : e0;
-          if (t >= e || !ok) continue;
-          // P_j(t) is written, and (first tile) the last unit's output has been read
-          ok = mbar_wait(&pfull[j], pn[j] & 1) && (t > w.t0 || on[j] == 0 || mbar_wait(&oempty[j], (on[j] - 1) & 1)) &&
-               !*abort_flag;
-          ok = __all_sync(0xffffffffu, ok);
-          if (!ok) continue;
-          ++pn[j];
-          tc_fence_after();
+        ++n;
+        tc_fence_after();
+        const bool q_alone = pair ? j == 1 && w.e0 <= w.t0 : steps == 1;  // the other group has no scores here
+        if (i0 < i1) {
           if (elect_one()) {
-            values(j, s, t == w.t0);
-            if (t + 1 < e) scores(j, j, s1);
-            else tc_commit(&ofull[j]);
+            scores(pair, (kn + i0) % R);
+            release(&bar.kempty[(kn + i0) % R], alone(i0));
+            if (i0 + di >= i1) release(&bar.qempty, q_alone);
           }
           __syncwarp();
-          if (t + 1 >= e) ++on[j];
+        }
+        for (int i = i0; i < i1; i += di) {
+          const int s = (kn + i) % R, s1 = (kn + i + di) % R;
+          const bool more = i + di < i1;
+          // V is there; (first tile) the last unit's output has been read
+          ok = mbar_wait(&bar.vfull[s], ((kn + i) / R) & 1) &&
+               (i > i0 || on == 0 || mbar_wait(&bar.oempty[j], (on - 1) & 1));
+          // V rows behind the sequence's last position, zeroed before they are multiplied
+          // (by both issuers where both read them)
+          const int lo = w.end - (w.t0 + i) * kCkKeys;
+          if (!KV8 && lo < kCkKeys && (lo & 15)) {
+            for (int x = (lo & 15) * (HD / 8) + lane; x < 16 * (HD / 8); x += 32) {
+              const int r = x / (HD / 8), c = x % (HD / 8);  // whole rows: the swizzle stays inside them
+              *reinterpret_cast<uint4*>(sV + s * TILE + (lo >> 4) * PAGE + (r >> 3) * SBO + (c >> 3) * 1024 + (r & 7) * 128 +
+                                        (c & 7) * 16) = make_uint4(0, 0, 0, 0);
+            }
+            fence_proxy_async();
+          }
+          if (more) ok = ok && mbar_wait(&bar.kfull[s1], ((kn + i + di) / R) & 1);
+          ok = __all_sync(0xffffffffu, ok && mbar_wait(&bar.pfull[j][0], pn & 1)) && !*abort_flag;
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          tc_fence_after();
+          if (elect_one()) {
+            if (s) values_of(c1, c0, i == i0);
+            else values_of(c0, c0, i == i0);
+          }
+          __syncwarp();
+          ok = __all_sync(0xffffffffu, mbar_wait(&bar.pfull[j][1], pn & 1));
+          if (!ok) break;
+          ++pn;
+          tc_fence_after();
+          if (elect_one()) {
+            if (s) values_of(c1, c1, false);
+            else values_of(c0, c1, false);
+            release(&bar.vempty[s], alone(i));
+            if (more) {
+              scores(pair, s1);
+              release(&bar.kempty[s1], alone(i + di));
+              if (i + 2 * di >= i1) release(&bar.qempty, q_alone);
+            } else {
+              tc_commit(&bar.ofull[j]);
+            }
+          }
+          __syncwarp();
         }
         if (!ok) break;
-        if (elect_one()) {
-          tc_commit(&vempty[s]);
-          if (t + 1 < e1) tc_commit(&kempty[s1]);
-          if (t + 2 == e1) tc_commit(&qempty);  // the unit's last scores: Q may be overwritten
-        }
-        __syncwarp();
+        on += i0 < i1;
+        kn += steps;
       }
-    }
-    if (!ok && lane == 0) fail();
-    if (elect_one()) tc_commit(&mma_done);
-    __syncwarp();
-    mbar_wait(&mma_done, 0);
+      if (!ok && lane == 0) fail();
+      if (elect_one()) tc_commit(&bar.done[j]);
+      __syncwarp();
+      mbar_wait(&bar.done[j], 0);
+    };
+    if (warp == kCkWarpMma) role(std::integral_constant<int, 0>());
+    else role(std::integral_constant<int, 1>());
   } else if (KV8 && warp >= kCkWarpWiden) {
     // ---------------- int8 cache: bf16(q s) of the key tiles' rows.  Thread: 16 codes
-    // (chunk c) of row rr of every 16 / IN pages; its codes of the next half tile (V
-    // after K, then the next tile's K) are in flight while it writes this one's.
-    constexpr int C = HD / 16;                // chunks a row
-    constexpr int PER = 128 / C, N = kCkKeys / PER;  // rows at a time, turns a tile
+    // (chunk c) of every PER-th row.  Each register of codes is filled again, for the
+    // half tile after (V after K, then the next tile's K), as soon as it has been
+    // written out, so loads are in flight throughout; pages three tiles ahead are on
+    // their way to L2.
+    constexpr int C = HD / 16;                             // chunks a row
+    constexpr int PER = 32 * kCkWiden / C, N = kCkKeys / PER;  // rows at a time, turns a tile
+    constexpr int AHEAD = 3;
     const int wi = threadIdx.x - kCkWarpWiden * 32, c = wi % C, rr = wi / C;
+    const int cb = 2 * (c & 3);
     int kn = 0;
     bool ok = true;
-    CkWalk w(a, at, len);
-    while (ok && w.next()) {
-      const int32_t* pt = a.page_table + (long long)w.ub * a.pages_per_seq;
-      for (int t = w.t0; t < w.t1 && ok; ++t, ++kn) {
-        int rowi[N];  // pool rows (fewer than 2^31); -1 reads zeros
+    CkPiece w;
+    while (next(w, ok)) {
+      const int32_t* pt = a.page_table + (long long)w.b * a.pages_per_seq;
+      // pool row (fewer than 2^31) of this thread's row in turn i of tile t; -1 reads zeros
+      auto pool_row = [&](int t, int i) {
+        const int key = t * kCkKeys + i * PER + rr;
+        if (key >= w.end) return -1;
+        const int id = __ldg(pt + key / 16);
+        if (id >= 0 && id < a.n_pages) return (id * a.Hkv + w.kvh) * 16 + key % 16;
+        if (a.err && c == 0) atomicExch(a.err, 1);
+        return -1;
+      };
+      // pages of tile t: the first warp those of K, the second those of V
+      auto ahead = [&](int t) {
+        const int key = t * kCkKeys + lane * 16;
+        if (warp > kCkWarpWiden + 1 || lane >= 8 || t >= w.t1 || key >= w.end) return;
+        const int id = __ldg(pt + key / 16);
+        if (id < 0 || id >= a.n_pages) return;
+        const int8_t* p = (warp == kCkWarpWiden ? a.k8 : a.v8) + (long long)(id * a.Hkv + w.kvh) * 16 * HD;
+        asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p), "n"(16 * HD) : "memory");
+      };
+      uint4 cw[N];
+      float sc[N];
+      int now[N];
+      auto fetch = [&](int i, int row, bool v) {
+        cw[i] = row >= 0 ? ld_nc16((v ? a.v8 : a.k8) + (long long)row * HD + c * 16) : make_uint4(0, 0, 0, 0);
+        sc[i] = row >= 0 ? __ldg((v ? a.v_scale : a.k_scale) + row) : 0.f;
+      };
+      if (!w.empty()) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-          const int key = t * kCkKeys + i * PER + rr;
-          rowi[i] = -1;
-          if (key < w.us.end) {
-            const int id = __ldg(pt + key / 16);
-            if (id >= 0 && id < a.n_pages) rowi[i] = (id * a.Hkv + w.ukvh) * 16 + key % 16;
-            else if (a.err && c == 0) atomicExch(a.err, 1);
-          }
+          now[i] = pool_row(w.t0, i);
+          fetch(i, now[i], false);
         }
+        for (int t = 1; t < AHEAD; ++t) ahead(w.t0 + t);
+      }
+      for (int t = w.t0; t < w.t1 && ok; ++t, ++kn) {
+        int then[N];
+        ahead(t + AHEAD);
+#pragma unroll
+        for (int i = 0; i < N; ++i) then[i] = t + 1 < w.t1 ? pool_row(t + 1, i) : -1;
 #pragma unroll 1
         for (int which = 0; which < 2; ++which) {
-          const int8_t* pool = which ? a.v8 : a.k8;
-          const float* scale = which ? a.v_scale : a.k_scale;
-          uint4 cw[N];
-          float sc[N];
-#pragma unroll
-          for (int i = 0; i < N; ++i) {
-            cw[i] = rowi[i] >= 0 ? ld_nc16(pool + (long long)rowi[i] * HD + c * 16) : make_uint4(0, 0, 0, 0);
-            sc[i] = rowi[i] >= 0 ? __ldg(scale + rowi[i]) : 0.f;
-          }
           const int s = kn % R;
-          if (kn >= R) ok = mbar_wait(which ? &vempty[s] : &kempty[s], ((kn / R) & 1) ^ 1);
+          if (kn >= R) ok = mbar_wait(which ? &bar.vempty[s] : &bar.kempty[s], ((kn / R) & 1) ^ 1);
           if (!__all_sync(0xffffffffu, ok) || __any_sync(0xffffffffu, *abort_flag != 0)) {
             ok = false;
             break;
           }
           uint8_t* dst = (which ? sV : sK) + s * TILE + (c >> 2) * 1024;
-          const int cb = 2 * (c & 3);
 #pragma unroll
           for (int i = 0; i < N; ++i) {
             const int row = i * PER + rr, sw = row & 7;
@@ -595,6 +634,7 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
               const float2 f = ck_mul2(ck_add2(make_float2(lo, hi), z2), s2);
               o[j] = pa_pack(f.x, f.y);
             }
+            fetch(i, which ? then[i] : now[i], !which);
             const uint4 e = make_uint4(o[0], o[1], o[2], o[3]), f = make_uint4(o[4], o[5], o[6], o[7]);
             uint8_t* rp = dst + (row >> 3) * SBO + sw * 128;
             // the lanes of a row's upper half write their odd chunk first: eight lanes, eight banks of 16 bytes
@@ -608,209 +648,215 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
           }
           fence_proxy_async();  // the MMAs read the tile through the async proxy
           __syncwarp();
-          if (lane == 0) mbar_arrive(which ? &vfull[s] : &kfull[s]);
+          if (lane == 0) mbar_arrive(which ? &bar.vfull[s] : &bar.kfull[s]);
         }
+#pragma unroll
+        for (int i = 0; i < N; ++i) now[i] = then[i];
       }
+      if (!ok) break;
     }
     if (!ok && lane == 0) fail();
   } else if (warp < kCkSoft) {
-    // ---------------- softmax: group j, half `half` of the keys, row 32 quad + lane
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(KV8 ? 88 : 104));
-    const int j = warp >> 3, half = (warp >> 2) & 1, quad = warp & 3, row = quad * 32 + lane;
-    const uint32_t lane_base = tmem + ((uint32_t)(quad * 32) << 16);
-    const uint32_t ts = lane_base + j * kCkKeys + half * 64, to = lane_base + kCkO + j * 128;
+    // ---------------- softmax: group j, row 32 quad + lane (TMEM begins at column 0)
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(ck_reg_soft<KV8>()));
+    const int j = warp >> 2, quad = warp & 3, row = quad * 32 + lane;
+    const uint32_t lane_base = (uint32_t)(quad * 32) << 16;
+    const uint32_t ts = lane_base + j * kCkKeys, to = lane_base + kCkO + j * 128;
     const float scale = kPaLog2e * rsqrtf((float)HD);
     const int tok = row / a.G;  // of a tile's packed rows
     const bool packed = row < a.tile_tokens * a.G;
-    int sn = 0, on[2] = {0, 0}, xn = 0, mn = 0;
+    int sn = 0, on[2] = {0, 0}, mn = 0;
     bool ok = true;
     uint8_t* stage = sV + R * TILE + warp * kCkStage;
-    CkWalk w(a, at, len);
-    while (ok && w.next()) {
-      const int jq = w.pair ? j : 0;  // this group's query tile
-      const int tile_i0 = w.i0 + jq * a.tile_tokens, tile_n = min(a.tile_tokens, w.us.n - tile_i0);
+    CkPiece w;
+    while (next(w, ok)) {
+      const bool pair = w.pair();
+      const int jq = pair ? j : 0;  // this group's query tile
+      const int tile_n = min(a.tile_tokens, w.n - jq * a.tile_tokens), tile_pos = w.pos + jq * a.tile_tokens;
       const bool on_row = packed && tok < tile_n;
       const bool on_warp = __any_sync(0xffffffffu, on_row);
       // keys of this row, and of the tile's first
-      const int lim = on_row ? min(w.us.end, w.us.pos + tile_i0 + tok + 1) : 0;
-      const int lim0 = min(w.us.end, w.us.pos + tile_i0 + 1);
-      const int t_end = w.end_of(j), t_first = w.pair ? w.t0 : w.t0 + j, stride = w.pair ? 1 : 2;
+      const int lim = on_row ? min(w.end, tile_pos + tok + 1) : 0, lim0 = min(w.end, tile_pos + 1);
+      const int t_end = jq == 0 && pair ? w.e0 : w.t1, t_first = pair ? w.t0 : w.t0 + j, stride = pair ? 1 : 2;
       float m = -INFINITY;  // reference maximum (log2 domain)
-      float2 l2[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+      float2 l2[4];         // row sum
+#pragma unroll
+      for (int y = 0; y < 4; ++y) l2[y] = make_float2(0.f, 0.f);
       for (int t = t_first; t < t_end; t += stride, ++sn) {
-        ok = __all_sync(0xffffffffu, mbar_wait(&sfull[j], sn & 1));
+        ok = __all_sync(0xffffffffu, mbar_wait(&bar.sfull[j], sn & 1));
         if (!ok) break;
-        if (on_warp) {
-          tc_fence_after();
-          // the scores stay in registers from their maximum to P, or (int8 cache: fewer
-          // registers a thread) are read again 32 at a time
-          float v[KV8 ? 32 : 64];
-          const int key0 = t * kCkKeys + half * 64;
-          const bool masked = (t + 1) * kCkKeys > lim0;
-          auto load = [&](int x0, float* d) {
-            tc_ld<32>(ts + x0, reinterpret_cast<uint32_t*>(d));
-            if (masked) {
+        if (!on_warp) {
+          if (lane < 2) mbar_arrive(&bar.pfull[j][lane]);
+          continue;
+        }
+        tc_fence_after();
+        // The scores stay in registers from their maximum to P; int8 cache (fewer
+        // registers a thread): half of them, the others are read again.
+        float v[KV8 ? 64 : 128];
+        const bool masked = (t + 1) * kCkKeys > lim0;
+        const int left = lim - t * kCkKeys;  // keys of this tile that the row sees
+        auto load = [&](int h, float* d) {
+          tc_ld<64>(ts + h * 64, reinterpret_cast<uint32_t*>(d));
+          if (masked) {
 #pragma unroll
-              for (int x = 0; x < 32; ++x)
-                if (key0 + x0 + x >= lim) d[x] = -INFINITY;
-            }
-          };
-          float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-          for (int x0 = 0; x0 < 64; x0 += 32) {
-            float* d = KV8 ? v : v + x0;
-            load(x0, d);
-#pragma unroll
-            for (int x = 0; x < 32; x += 8)
-#pragma unroll
-              for (int y = 0; y < 4; ++y) m4[y] = fmaxf(m4[y], fmaxf(d[x + 2 * y], d[x + 2 * y + 1]));
+            for (int x = 0; x < 64; ++x)
+              if (h * 64 + x >= left) d[x] = -INFINITY;
           }
-          float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * scale;
-          // the other half's maximum
-          s_x[j][xn & 1][half][row] = mx;
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&xch[j][quad]);
-          ok = __all_sync(0xffffffffu, mbar_wait(&xch[j][quad], xn & 1));
-          if (!ok) break;
-          mx = fmaxf(mx, s_x[j][xn & 1][half ^ 1][row]);
-          ++xn;
-          // move the reference when the tile would exceed it by more than 2^kCkSlack
-          float corr = 1.f;
-          if (mx > m + kCkSlack) {
-            corr = exp2f(m - mx);  // 0 on the first tile
-            m = mx;
-            l2[0].x *= corr, l2[0].y *= corr, l2[1].x *= corr, l2[1].y *= corr;
-          }
-          if (t > t_first && __any_sync(0xffffffffu, corr != 1.f)) {
-            // O holds P V of the earlier tiles (complete: S(t) was issued after it)
+        };
+        float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int h = 1; h >= 0; --h) {
+          float* d = KV8 ? v : v + h * 64;
+          load(h, d);
+#pragma unroll
+          for (int x = 0; x < 64; x += 8)
+#pragma unroll
+            for (int y = 0; y < 4; ++y) m4[y] = ck_max3(m4[y], d[x + 2 * y], d[x + 2 * y + 1]);
+        }
+        const float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * scale;
+        // move the reference when the tile would exceed it by more than 2^kCkSlack
+        float corr = 1.f;
+        if (mx > m + kCkSlack) {
+          corr = exp2f(m - mx);  // 0 on the first tile
+          m = mx;
+#pragma unroll
+          for (int y = 0; y < 4; ++y) l2[y] = ck_mul2(l2[y], make_float2(corr, corr));
+        }
+        if (t > t_first && __any_sync(0xffffffffu, corr != 1.f)) {
+          // O holds P V of the earlier tiles (complete: S(t) was issued after it)
 #pragma unroll 1
-            for (int x = half * (HD / 2); x < (half + 1) * (HD / 2); x += 16) {
-              uint32_t o[16];
-              tc_ld<16>(to + x, o);
+          for (int x = 0; x < HD; x += 16) {
+            uint32_t o[16];
+            tc_ld<16>(to + x, o);
 #pragma unroll
-              for (int y = 0; y < 16; ++y) o[y] = __float_as_uint(__uint_as_float(o[y]) * corr);
-              tc_st16(to + x, o);
-            }
+            for (int y = 0; y < 16; ++y) o[y] = __float_as_uint(__uint_as_float(o[y]) * corr);
+            tc_st16(to + x, o);
           }
-          const float mref = m == -INFINITY ? 0.f : m;
-          const float2 sc2 = make_float2(scale, scale), nm2 = make_float2(-mref, -mref);
+        }
+        const float mref = m == -INFINITY ? 0.f : m;
+        const float2 sc2 = make_float2(scale, scale), nm2 = make_float2(-mref, -mref);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          float* d = KV8 ? v : v + h * 64;
+          if (KV8 && h) load(1, d);
 #pragma unroll
           for (int x0 = 0; x0 < 64; x0 += 32) {
             uint32_t pw[16];
-            float* d = KV8 ? v : v + x0;
-            if (KV8) load(x0, d);
 #pragma unroll
             for (int x = 0; x < 32; x += 2) {
-              const float2 e = ck_fma2(make_float2(d[x], d[x + 1]), sc2, nm2);
+              const float2 e = ck_fma2(make_float2(d[x0 + x], d[x0 + x + 1]), sc2, nm2);
               const float2 p = make_float2(pa_ex2(e.x), pa_ex2(e.y));
-              l2[(x >> 1) & 1] = ck_add2(l2[(x >> 1) & 1], p);
+              l2[(x >> 1) & 3] = ck_add2(l2[(x >> 1) & 3], p);
               pw[x / 2] = pa_pack(p.x, p.y);
             }
-            tc_st16(ts + x0 / 2, pw);
+            tc_st16(ts + h * 64 + x0 / 2, pw);
           }
           tc_wait_st();
           tc_fence_before();
           __syncwarp();
+          if (lane == 0) mbar_arrive(&bar.pfull[j][h]);
         }
-        if (lane == 0) mbar_arrive(&pfull[j]);
       }
       if (!ok) break;
-      float l = (l2[0].x + l2[0].y) + (l2[1].x + l2[1].y);
+      float l = ((l2[0].x + l2[0].y) + (l2[1].x + l2[1].y)) + ((l2[2].x + l2[2].y) + (l2[3].x + l2[3].y));
       // ---- the piece's output
-      const bool whole = w.first && w.last, empty = w.t1 <= w.t0;
+      const bool whole = w.first() && w.last(), empty = w.empty();
       const bool use0 = w.uses(0), use1 = w.uses(1);
-      float a0 = 1.f, a1 = 0.f;  // factors of O_0 and O_1 (units of one tile), or of O_j
-      if (w.pair) {
+      float a0 = 1.f, a1 = 0.f;  // factors of O_0 and O_1 (units of one tile)
+      if (pair) {
         if (j ? use1 : use0) {
-          if (on_warp) {
-            s_x[j][xn & 1][half][row] = l;
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&xch[j][quad]);
-            ok = __all_sync(0xffffffffu, mbar_wait(&xch[j][quad], xn & 1));
-            if (!ok) break;
-            l += s_x[j][xn & 1][half ^ 1][row];
-            ++xn;
-          }
-          ok = __all_sync(0xffffffffu, mbar_wait(&ofull[j], (j ? on[1] : on[0]) & 1));
+          ok = __all_sync(0xffffffffu, mbar_wait(&bar.ofull[j], (j ? on[1] : on[0]) & 1));
           if (!ok) break;
         }
         on[0] += use0, on[1] += use1;
       } else if (!empty) {
         // every warp meets here, those without rows too: past this point both groups
         // have seen the accumulators of the pieces before
-        s_ml[mn & 1][j][half][row] = make_float2(m, l);
+        s_ml[mn & 1][j][row] = make_float2(m, l);
         __syncwarp();
-        if (lane == 0) mbar_arrive(&met[quad]);
-        ok = __all_sync(0xffffffffu, mbar_wait(&met[quad], mn & 1));
+        if (lane == 0) mbar_arrive(&bar.met[quad]);
+        ok = mbar_wait(&bar.met[quad], mn & 1);
+        ok = __all_sync(0xffffffffu, ok && mbar_wait(&bar.ofull[0], on[0] & 1) && (!use1 || mbar_wait(&bar.ofull[1], on[1] & 1)));
         if (!ok) break;
-        const float2 p0 = s_ml[mn & 1][0][0][row], p1 = s_ml[mn & 1][1][0][row];
-        const float l0 = p0.y + s_ml[mn & 1][0][1][row].y, l1 = p1.y + s_ml[mn & 1][1][1][row].y;
+        ++on[0];
+        on[1] += use1;
+        const float2 p0 = s_ml[mn & 1][0][row], p1 = s_ml[mn & 1][1][row];
         ++mn;
         m = fmaxf(p0.x, p1.x);
         a0 = p0.x == -INFINITY ? 0.f : exp2f(p0.x - m);
         a1 = p1.x == -INFINITY ? 0.f : exp2f(p1.x - m);
-        l = a0 * l0 + a1 * l1;
-        ok = __all_sync(0xffffffffu, mbar_wait(&ofull[0], on[0] & 1) && (!use1 || mbar_wait(&ofull[1], on[1] & 1)));
-        if (!ok) break;
-        ++on[0];
-        on[1] += use1;
+        l = a0 * p0.y + a1 * p1.y;
       }
       tc_fence_after();
-      const bool have = w.pair ? (j ? use1 : use0) : !empty;  // an accumulator to read
+      const bool have = pair ? (j ? use1 : use0) : !empty;  // an accumulator to read
       const float inv = l > 0.f ? 1.f / l : 0.f;
-      const int q4 = w.pair ? half : 2 * j + half;
-      const int cols = w.pair ? HD / 2 : HD / 4, x0 = q4 * cols;
+      // pair: this group's tile, all columns; else half of the sum's columns a group
+      const int x0 = pair ? 0 : j * (HD / 2), x1 = pair ? HD : x0 + HD / 2;
       if (on_warp) {
-        const uint32_t src = w.pair ? to : lane_base + kCkO;
-        auto load = [&](int x, float* r) {  // 16 columns of the sums
+        const uint32_t src = pair ? to : lane_base + kCkO;
+        auto load = [&](int x, float* r) {  // 32 columns of the sums
+          if (!have) {
 #pragma unroll
-          for (int y = 0; y < 16; ++y) r[y] = 0.f;
-          if (!have) return;
-          tc_ld<16>(src + x, reinterpret_cast<uint32_t*>(r));
-          if (w.pair) return;
-          if (use1) {
+            for (int y = 0; y < 32; ++y) r[y] = 0.f;
+            return;
+          }
+          tc_ld<32>(src + x, reinterpret_cast<uint32_t*>(r));
+          if (pair) return;
+#pragma unroll
+          for (int y = 0; y < 32; ++y) r[y] *= a0;
+          if (!use1) return;
+#pragma unroll
+          for (int y0 = 0; y0 < 32; y0 += 16) {
             uint32_t u[16];
-            tc_ld<16>(src + 128 + x, u);
+            tc_ld<16>(src + 128 + x + y0, u);
 #pragma unroll
-            for (int y = 0; y < 16; ++y) r[y] = a0 * r[y] + a1 * __uint_as_float(u[y]);
+            for (int y = 0; y < 16; ++y) r[y0 + y] = fmaf(a1, __uint_as_float(u[y]), r[y0 + y]);
           }
         };
         if (whole) {
-          // through shared memory, two lanes to a row's 32 bytes
-          uint16_t* o = a.out + (long long)(w.us.row0 + tile_i0) * a.H * HD + (long long)w.ukvh * a.G * HD;
-          for (int x = x0; x < x0 + cols; x += 16) {
-            float r[16];
-            load(x, r);
-            uint4 p[2];
-            uint32_t* pw = reinterpret_cast<uint32_t*>(p);
+          // through shared memory, four lanes to a row's 64 bytes; chunk c of row r at c ^ (r / 2 % 4)
+          uint16_t* o = a.out + ((long long)(w.row0 + jq * a.tile_tokens) * a.H + (long long)w.kvh * a.G) * HD;
+          // rows 8 y + lane / 4 of this warp's: where each begins, or -1
+          int at[4];
 #pragma unroll
-            for (int y = 0; y < 8; ++y) pw[y] = pa_pack(r[2 * y] * inv, r[2 * y + 1] * inv);
-            const int sw = (lane >> 2) & 1;
-            *reinterpret_cast<uint4*>(stage + lane * 32 + (sw << 4)) = p[0];
-            *reinterpret_cast<uint4*>(stage + lane * 32 + ((sw ^ 1) << 4)) = p[1];
+          for (int y = 0; y < 4; ++y) {
+            const int r2 = quad * 32 + y * 8 + (lane >> 2), t2 = r2 / a.G;
+            at[y] = r2 < a.tile_tokens * a.G && t2 < tile_n ? (t2 * a.H + r2 - t2 * a.G) * HD : -1;
+          }
+#pragma unroll 1
+          for (int x = x0; x < x1; x += 32) {
+            float r[32];
+            load(x, r);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+              uint32_t p[4];
+#pragma unroll
+              for (int y = 0; y < 4; ++y) p[y] = pa_pack(r[8 * c + 2 * y] * inv, r[8 * c + 2 * y + 1] * inv);
+              *reinterpret_cast<uint4*>(stage + lane * 64 + ((c ^ ((lane >> 1) & 3)) << 4)) = make_uint4(p[0], p[1], p[2], p[3]);
+            }
             __syncwarp();
 #pragma unroll
-            for (int y = 0; y < 2; ++y) {
-              const int lr = y * 16 + (lane >> 1), r2 = quad * 32 + lr, t2 = r2 / a.G;
-              const uint4 v = *reinterpret_cast<const uint4*>(stage + lr * 32 + (((lane & 1) ^ ((lr >> 2) & 1)) << 4));
-              if (r2 < a.tile_tokens * a.G && t2 < tile_n)
-                *reinterpret_cast<uint4*>(o + (long long)t2 * a.H * HD + (r2 - t2 * a.G) * HD + x + (lane & 1) * 8) = v;
+            for (int y = 0; y < 4; ++y) {
+              const int lr = y * 8 + (lane >> 2);
+              const uint4 p = *reinterpret_cast<const uint4*>(stage + lr * 64 + (((lane & 3) ^ ((lr >> 1) & 3)) << 4));
+              if (at[y] >= 0) *reinterpret_cast<uint4*>(o + at[y] + x + (lane & 3) * 8) = p;
             }
             __syncwarp();
           }
         } else {
-          uint8_t* slot = a.ws + kCkHead + ((size_t)blockIdx.x * 2 + (w.first ? 1 : 0)) * ck_slot<HD>();
+          uint8_t* slot = a.ws + kCkHead + ((size_t)blockIdx.x * 2 + (w.first() ? 1 : 0)) * ck_slot<HD>();
           const int r = jq * kCkKeys + row;
           if (have)
-            for (int x = x0; x < x0 + cols; x += 16) {
-              float f[16];
+#pragma unroll 1
+            for (int x = x0; x < x1; x += 32) {
+              float f[32];
               load(x, f);
 #pragma unroll
-              for (int y = 0; y < 4; ++y)
+              for (int y = 0; y < 8; ++y)
                 reinterpret_cast<float4*>(slot)[(size_t)(x / 4 + y) * kCkRows + r] =
                     make_float4(f[4 * y], f[4 * y + 1], f[4 * y + 2], f[4 * y + 3]);
             }
-          if (q4 == 0)
+          if (x0 == 0)
             reinterpret_cast<float2*>(slot + (size_t)kCkRows * HD * 4)[r] =
                 make_float2(have && l > 0.f ? m : -INFINITY, have ? l : 0.f);
         }
@@ -819,17 +865,17 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
         tc_fence_before();
         __syncwarp();
         if (lane == 0) {
-          if (w.pair) {  // the 16 arrivals of an accumulator: two from each of its own group's warps
-            mbar_arrive(&oempty[j]);
-            mbar_arrive(&oempty[j]);
+          if (pair) {  // the 8 arrivals of an accumulator: two from each of its own group's warps
+            mbar_arrive(&bar.oempty[j]);
+            mbar_arrive(&bar.oempty[j]);
           } else {
-            mbar_arrive(&oempty[0]);
-            if (use1) mbar_arrive(&oempty[1]);
+            mbar_arrive(&bar.oempty[0]);
+            if (use1) mbar_arrive(&bar.oempty[1]);
           }
         }
       }
-      if (threadIdx.x == 0 && w.first && !w.last) {
-        const CkLeft left = {w.ux + kCkStart + w.nt, w.us.row0, w.i0, w.us.n, w.ukvh, w.pair};
+      if (threadIdx.x == 0 && w.first() && !w.last()) {
+        const CkLeft left = {w.stop, w.row0, w.n, w.kvh};
         reinterpret_cast<CkLeft*>(a.ws + kCkHead / 4)[blockIdx.x] = left;
       }
     }
@@ -839,72 +885,68 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
   __syncthreads();
   if (warp == kCkWarpMma) {
     tc_fence_after();
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kCkTmemCols) : "memory");
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(kCkTmemCols) : "memory");
   }
 }
 
 // ------------------------------------------------------------------ joining the parts
-// Block (c, s): rows 32 (s / HC) .. + 31 and columns 32 (s % HC) .. + 31 of the unit
-// that CTA c began and left unfinished: o = sum_i 2^(m_i - m) O_i / sum_i 2^(m_i - m) l_i
-// over the CTAs whose stretches begin before the unit's end, in their order.
-constexpr int kCkJoinParts = 4;  // shares of a unit's parts, added in order at the end
+// The unit that CTA c = blockIdx.x began and left unfinished:
+// o = sum_i 2^(m_i - m) O_i / sum_i 2^(m_i - m) l_i over the CTAs whose stretches begin
+// before the unit's end, in their order.  A block takes every gridDim.y-th block of 32
+// rows and 32 columns; its four groups of threads share a unit's parts (up to one a
+// CTA, where there is one sequence and KV head) and add up in order.
+constexpr int kCkJoinParts = 4, kCkJoinBlocks = 16;
 template <int HD>
-__global__ void __launch_bounds__(256 * kCkJoinParts)
+__global__ void __launch_bounds__(256)
     attn_chunk_join_kernel(const uint8_t* __restrict__ ws, int ctas, int H, int G, int tile_tokens,
                            uint16_t* __restrict__ out) {
-  constexpr int HC = HD / 32;
-  __shared__ float4 s_o[kCkJoinParts - 1][256];
-  __shared__ float2 s_ml[kCkJoinParts][32];
+  __shared__ float4 s_o[kCkJoinParts - 1][64];
+  __shared__ float2 s_ml[kCkJoinParts][8];
   pdl_trigger();
   pdl_wait();
   const int c = blockIdx.x;
   const CkLeft u = reinterpret_cast<const CkLeft*>(ws + kCkHead / 4)[c];
   if (u.end == 0) return;
-  const int rows0 = 32 * (blockIdx.y / HC);
-  const int tile = rows0 / kCkKeys, i0 = u.i0 + tile * tile_tokens, n = min(tile_tokens, u.n - i0);
-  if ((tile && !u.pair) || (rows0 % kCkKeys) >= n * G) return;
-  // rows in the lanes' low bits where the parts are read, columns where the result is written
-  const int tid = threadIdx.x & 255, part = threadIdx.x >> 8;
-  const int lr = (tid & 7) + 8 * (tid >> 6), c4 = 8 * (blockIdx.y % HC) + ((tid >> 3) & 7);
+  // 8 rows in the lanes' low bits where the parts are read, 8 column quads above
+  const int tid = threadIdx.x & 63, part = threadIdx.x >> 6;
   const long long* begins = reinterpret_cast<const long long*>(ws);
-  auto slot = [&](int k) { return ws + kCkHead + ((size_t)k * 2 + (k == c ? 1 : 0)) * ck_slot<HD>(); };
-  auto begun = [&](int k) { return k < ctas ? begins[k] : 0x7fffffffffffffffLL; };
-  // the unit's parts: CTA c and the ones after it that begin before its end
   int last = c;
   while (last + 1 < ctas && begins[last + 1] < u.end) ++last;
   const int per = (last - c + kCkJoinParts) / kCkJoinParts, k0 = c + part * per, k1 = min(last + 1, k0 + per);
-  float m = -INFINITY, l = 0.f;
-  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int k = k0; k < k1; ++k) {
-    if (k > c && begun(k + 1) == begins[k]) continue;  // no stretch
-    const uint8_t* p = slot(k);
-    const float2 ml = reinterpret_cast<const float2*>(p + (size_t)kCkRows * HD * 4)[rows0 + lr];
-    if (ml.x == -INFINITY) continue;
-    const float4 f = reinterpret_cast<const float4*>(p)[(size_t)c4 * kCkRows + rows0 + lr];
-    const float m2 = fmaxf(m, ml.x), x = exp2f(m - m2), y = exp2f(ml.x - m2);
-    m = m2;
-    l = l * x + ml.y * y;
-    o = make_float4(o.x * x + f.x * y, o.y * x + f.y * y, o.z * x + f.z * y, o.w * x + f.w * y);
-  }
-  if (part) s_o[part - 1][tid] = o;
-  if (((tid >> 3) & 7) == 0) s_ml[part][lr] = make_float2(m, l);
-  __syncthreads();
-  if (part) return;
+  const int rows = u.n > tile_tokens ? kCkKeys + (u.n - tile_tokens) * G : u.n * G;  // packed rows up to the last
+  for (int item = blockIdx.y; item < (rows + 7) / 8 * (HD / 32); item += gridDim.y) {
+    const int r = item / (HD / 32) * 8 + (tid & 7), c4 = item % (HD / 32) * 8 + (tid >> 3);
+    float m = -INFINITY, l = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    auto add = [&](float2 ml, float4 f) {
+      if (ml.x == -INFINITY) return;
+      const float m2 = fmaxf(m, ml.x), x = exp2f(m - m2), y = exp2f(ml.x - m2);
+      m = m2;
+      l = l * x + ml.y * y;
+      o = make_float4(o.x * x + f.x * y, o.y * x + f.y * y, o.z * x + f.z * y, o.w * x + f.w * y);
+    };
+#pragma unroll 4
+    for (int k = k0; k < k1; ++k) {
+      const uint8_t* p = ws + kCkHead + ((size_t)k * 2 + (k == c ? 1 : 0)) * ck_slot<HD>();
+      // (a CTA whose stretch is empty has no part)
+      const bool none = k > c && k + 1 < ctas && begins[k + 1] == begins[k];
+      const float2 ml = reinterpret_cast<const float2*>(p + (size_t)kCkRows * HD * 4)[r];
+      add(none ? make_float2(-INFINITY, 0.f) : ml, reinterpret_cast<const float4*>(p)[(size_t)c4 * kCkRows + r]);
+    }
+    if (part) s_o[part - 1][tid] = o;
+    if (tid < 8) s_ml[part][tid] = make_float2(m, l);
+    __syncthreads();
+    const int rt = r % kCkKeys, tok = rt / G, row = tok + (r >= kCkKeys ? tile_tokens : 0);
+    if (part == 0) {
 #pragma unroll
-  for (int k = 1; k < kCkJoinParts; ++k) {
-    const float2 ml = s_ml[k][lr];
-    if (ml.x == -INFINITY) continue;
-    const float4 f = s_o[k - 1][tid];
-    const float m2 = fmaxf(m, ml.x), x = exp2f(m - m2), y = exp2f(ml.x - m2);
-    m = m2;
-    l = l * x + ml.y * y;
-    o = make_float4(o.x * x + f.x * y, o.y * x + f.y * y, o.z * x + f.z * y, o.w * x + f.w * y);
+      for (int k = 1; k < kCkJoinParts; ++k) add(s_ml[k][tid & 7], s_o[k - 1][tid]);
+      const float inv = l > 0.f ? 1.f / l : 0.f;
+      if (r < rows && rt < tile_tokens * G && row < u.n)
+        *reinterpret_cast<uint2*>(out + ((long long)(u.row0 + row) * H + (long long)u.kvh * G + rt % G) * HD + c4 * 4) =
+            make_uint2(pa_pack(o.x * inv, o.y * inv), pa_pack(o.z * inv, o.w * inv));
+    }
+    __syncthreads();
   }
-  const float inv = l > 0.f ? 1.f / l : 0.f;
-  const int r = rows0 % kCkKeys + lr, tok = r / G;
-  if (r >= tile_tokens * G || tok >= n) return;
-  *reinterpret_cast<uint2*>(out + ((long long)(u.row0 + i0 + tok) * H + (long long)u.kvh * G + r % G) * HD + c4 * 4) =
-      make_uint2(pa_pack(o.x * inv, o.y * inv), pa_pack(o.z * inv, o.w * inv));
 }
 
 // Row-major [d3][d2][d1][d0] of bf16 (strides in bytes), 128-byte swizzle.
@@ -939,6 +981,10 @@ static int ck_sms() {
   return std::min(sms, 1024);
 }
 
+bool attention_chunk_fits(int n_tokens, int n_heads, int n_kv_heads, int max_new, int max_len) {
+  return ck_fits(n_tokens, max_new, max_len, n_kv_heads, ck_tile_tokens(n_heads / n_kv_heads));
+}
+
 size_t attention_chunk_ws_bytes(int B, int n_heads, int n_kv_heads, int head_dim, int max_new) {
   return kCkHead + (size_t)2 * 152 * (head_dim == 64 ? ck_slot<64>() : ck_slot<128>());
 }
@@ -963,10 +1009,8 @@ static cudaError_t launch_ck(const uint16_t* q, int q_stride, const fp_kv_view& 
   FP_CUDA_TRY(smem_limit_once(attn_chunk_kernel<HD, KV8>, ck_smem<HD>(), &attr));
   const int grid = std::min(ck_sms(), 152);
   FP_CUDA_TRY(launch(attn_chunk_kernel<HD, KV8>, dim3(grid), dim3(ck_threads<KV8>()), (size_t)ck_smem<HD>(), s, mq, mk, mv, a));
-  // the parts of units that several CTAs took: blocks of 32 rows and 32 columns
-  const int rows = std::min(kCkRows, (std::min(a.max_new, 2 * a.tile_tokens) + a.tile_tokens - 1) / a.tile_tokens * kCkKeys);
-  return launch_early(attn_chunk_join_kernel<HD>, dim3(grid, rows / 32 * (HD / 32)), dim3(256 * kCkJoinParts), 0, s,
-                      (const uint8_t*)a.ws, grid, a.H, a.G, a.tile_tokens, a.out);
+  return launch_early(attn_chunk_join_kernel<HD>, dim3(grid, kCkJoinBlocks), dim3(256), 0, s, (const uint8_t*)a.ws, grid, a.H,
+                      a.G, a.tile_tokens, a.out);
 }
 
 cudaError_t launch_attention_chunk(const uint16_t* q, int q_stride, int n_tokens, int B, int n_heads,

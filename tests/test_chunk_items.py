@@ -26,7 +26,7 @@ int main() {
     CkSeq s;
     const bool fine = s.set(0, n, pos, tt, most, top);
     if (fine != (n <= most && (n == 0 || (pos >= 0 && pos + n <= top)))) return bad("bounds", it);
-    long long x = 0;
+    int x = 0;
     for (int u = 0; u < s.units; ++u) {
       const int nt = s.tiles(u, T);
       if (s.before(u, T) != x) return bad("before", it);
@@ -57,7 +57,8 @@ int main() {
     if (g < 1 || g > grid) return bad("ctas", it);
     auto begin = [&](int c) -> long long {
       if (c >= g) return W;
-      const long long x = W * c / g;
+      const long long x = ck_muldiv(W, c, g);
+      if (x != W * c / g) return -1;
       for (auto& u : units)
         if (x >= u.x && x < u.x + kCkStart + u.nt) return u.x + ck_snap((int)(x - u.x), u.nt);
       return W;
