@@ -268,7 +268,11 @@ int fp_op_kv_read(const fp_kv_view* kv, int n_tokens, int B, const int32_t* cu, 
  * pool reads as zero keys and values and sets *err = 1.
  * workspace: 256-byte aligned, at least
  * fp_op_attention_chunk_workspace_bytes(B, n_heads, n_kv_heads, head_dim, max_new)
- * bytes (0: a shape that is refused), of any content; calls that overlap on the GPU need separate ones. */
+ * bytes (0: a shape that is refused).  Its leading 64 KB hold ticket counters that
+ * must be zero before the first call; every call leaves them zero again, so one
+ * workspace serves any sequence of calls of its shape or smaller ones on one
+ * stream (calls that overlap on the GPU need separate workspaces; zero it again
+ * after a call that set *err = 2, a wait that ran out). */
 int fp_op_attention_chunk(const uint16_t* q, int q_stride, int n_tokens, int B, int n_heads, const fp_kv_view* kv,
                           const int32_t* cu, const int32_t* pos, int max_new, int max_len, uint16_t* out,
                           void* workspace, size_t workspace_bytes, int32_t* err, void* stream);

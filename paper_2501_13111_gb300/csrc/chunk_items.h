@@ -107,6 +107,16 @@ FP_CK long long ck_muldiv(long long x, int y, int z) {
   return x < (1 << 22) ? (long long)((uint32_t)x * (uint32_t)y / (uint32_t)z) : x * y / z;
 }
 
+// The first of g CTAs whose stretch begins, before its border is moved, at t or behind:
+// floor(W c / g) >= t.
+FP_CK int ck_first_from(long long t, long long W, int g) { return (int)((t * g + W - 1) / W); }
+
+// The CTAs that share the unit of nt key tiles at place x: *own begins it, *parts in all.
+FP_CK void ck_parts(long long x, int nt, long long W, int g, int* own, int* parts) {
+  *own = ck_first_from(x + kCkStart + kCkSnap, W, g) - 1;
+  *parts = ck_first_from(x + kCkStart + nt - kCkSnap + 1, W, g) - *own;
+}
+
 // CTAs that take part of W places (at most 1024).
 FP_CK int ck_ctas(long long W, int grid) {
   const long long most = W / kCkLeast > 1 ? W / kCkLeast : 1;  // (kCkLeast: a power of two)

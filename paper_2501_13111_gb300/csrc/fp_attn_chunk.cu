@@ -15,7 +15,8 @@
 //               p, the sums in fp32); the reference m moves only when a tile passes it
 //               by 2^8 (O and the row sum are rescaled then).  P goes out in two halves
 //               of 64 keys, so that the first half's products run while the second
-//               half is computed.  At the end of a piece they write its rows;
+//               half is computed.  At the end of a piece they write its rows, or the part
+//               that this CTA has of them: the last CTA to finish a unit adds its parts up;
 //   warp 8      TMA: the unit's Q tiles (one box per 64 columns: tokens x heads) and,
 //               page by page, the keys.  One box a page, in the order [8 rows][64
 //               columns] the descriptors step through;
@@ -26,6 +27,7 @@
 //               there were five in a row.)  Warp 9 owns the TMEM;
 //   warp 11     plans the CTA's stretch, describes its pieces of units to the others,
 //               and (bf16 cache) copies the values;
+//               (int8 cache: warp 8 finds the pages and sends them on to L2);
 //   warps 12-19 (int8 cache) K and V tiles from the codes: bf16(q s), the values that
 //               fp_op_kv_read returns (a byte permute gives fp32 2^15 + 128 + q, an exact
 //               subtraction q; 2^-8 of a value, as a bf16 cache's own rounding).
@@ -53,10 +55,9 @@ template <bool KV8>
 constexpr int ck_reg_soft() { return KV8 ? 128 : 208; }
 template <bool KV8>
 constexpr int ck_reg_other() { return KV8 ? 72 : 88; }
-// Warps that read each piece's description: softmax, Q, MMA and the widening ones.
-template <bool KV8>
-constexpr int ck_readers() { return kCkSoft + 3 + (KV8 ? kCkWiden : 0); }
+constexpr int kCkReaders = kCkSoft + 3;           // warps that read each piece's description: softmax, Q, MMA
 constexpr int kCkPieces = 4;                      // pieces described ahead
+constexpr int kCkAhead = 8;                       // int8 cache: key tiles whose pages are known ahead
 constexpr int kCkRing = 2;                        // K tiles in shared memory, and V tiles
 constexpr uint32_t kCkTmemCols = 512, kCkO = 256; // O of group j at kCkO + 128 j, its scores at 128 j
 constexpr int kCkStage = 32 * 64;                 // a warp's 32 output rows, 32 columns at a time
@@ -67,16 +68,17 @@ constexpr int ck_tile_bytes() { return kCkKeys * HD * 2; }
 template <int HD>
 constexpr int ck_smem() { return (2 + 2 * kCkRing) * ck_tile_bytes<HD>() + kCkSoft * kCkStage + 1024; }
 
-// Workspace: per CTA where its stretch begins, which unit it began and left
-// unfinished, and two partial results (slot 0: of a unit begun by an earlier CTA,
-// slot 1: of the one it left): fp32 O as [HD / 4][256 rows][4], then (m, l) [256 rows].
-struct CkLeft {
-  long long end;  // the unit's end on the line; 0: none was left
-  int row0, n, kvh;
-};
-constexpr size_t kCkHead = 64 * 1024;  // begins and CkLeft of up to 1024 CTAs
+// Workspace: tickets (zero between calls), then for every CTA two partial results (slot
+// 0: of a unit begun by an earlier CTA, slot 1: of the one it began and left): fp32 O as
+// [HD / 4][256 rows][4], (m, l) [256 rows], and (m, l) of a group of parts added up.
+// The parts of a unit are added in groups of kCkGroup CTAs, then the groups' sums:
+// tickets [owner][group], the last for the groups.
+constexpr int kCkGroup = 13, kCkMaxCtas = 152;  // 12 groups at most
+constexpr size_t kCkTickets = 16;
+constexpr size_t kCkHead = 64 * 1024;
+static_assert(kCkMaxCtas * kCkTickets * 4 <= kCkHead, "tickets");
 template <int HD>
-constexpr size_t ck_slot() { return (size_t)kCkRows * (HD * 4 + 8); }
+constexpr size_t ck_slot() { return (size_t)kCkRows * (HD * 4 + 16); }
 
 // [8 rows][64 columns] atoms: 8-row groups `sbo` bytes apart, K-major.
 FP_DEV uint64_t ck_sdesc_k(uint32_t saddr, uint32_t sbo) {
@@ -137,7 +139,7 @@ struct __align__(16) CkPiece {
   int row0, n, pos; // the unit's first row, its rows (tokens), the first one's position
   int end;          // cached positions of the sequence that may be read
   int b, kvh;
-  long long stop;   // the unit's end on the line
+  int own, parts;   // the CTA that begins the unit, and how many take part of it
   FP_DEV bool pair() const { return flags & 1; }    // two query tiles
   FP_DEV bool first() const { return flags & 2; }   // the unit's first part
   FP_DEV bool last() const { return flags & 4; }
@@ -152,6 +154,8 @@ struct CkWalk {
   CkSeq s;
   int b, kvh, u, off;  // the next place: `off` into unit u of (b, kvh)
   long long x, rem;    // its place on the line, and places left
+  long long W;         // the line's length, shared among g CTAs
+  int g;
   FP_DEV int places(int bb) {  // of sequence bb; bounds that are broken are reported
     int first, count;
     const int lo = __ldg(a.cu + bb), hi = __ldg(a.cu + bb + 1), p = __ldg(a.pos + bb);
@@ -164,7 +168,7 @@ struct CkWalk {
   FP_DEV CkWalk(const CkArgs& a) : a(a) {
     const int lane = threadIdx.x & 31, T = 2 * a.tile_tokens;
     // the line's length (up to 32 sequences: their places stay in the lanes)
-    long long W = 0;
+    W = 0;
     int c = 0;
 #pragma unroll 1
     for (int b0 = 0; b0 < a.B; b0 += 32) {
@@ -173,7 +177,8 @@ struct CkWalk {
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) W += __shfl_xor_sync(0xffffffffu, W, o);
-    const int g = ck_ctas(W, gridDim.x), cta = blockIdx.x;
+    g = ck_ctas(W, gridDim.x);
+    const int cta = blockIdx.x;
     const long long x0 = cta < g ? ck_muldiv(W, cta, g) : W, x1 = cta + 1 < g ? ck_muldiv(W, cta + 1, g) : W;
     b = a.B, kvh = u = off = 0;
     x = W;
@@ -251,7 +256,8 @@ struct CkWalk {
     p->e0 = min(p->t1, s.bad || !pair ? nt : (s.pos + i0 + a.tile_tokens + kCkKeys - 1) / kCkKeys);
     p->flags = (pair ? 1 : 0) | (off == 0 ? 2 : 0) | (take == left ? 4 : 0);
     p->row0 = s.row0 + i0, p->n = min(T, s.n - i0), p->pos = s.pos + i0, p->end = s.end;
-    p->b = b, p->kvh = kvh, p->stop = x - off + kCkStart + nt;
+    p->b = b, p->kvh = kvh, p->own = blockIdx.x, p->parts = 1;
+    if (off != 0 || take != left) ck_parts(x - off, nt, W, g, &p->own, &p->parts);
     rem -= take;
     x += take;
     off = 0;
@@ -273,14 +279,15 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
   constexpr int TILE = ck_tile_bytes<HD>(), NH = HD / 64, SBO = NH * 1024, PAGE = 2 * SBO, R = kCkRing;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   struct Bars {
-    uint64_t kfull[R], vfull[R], kempty[R], vempty[R], qfull, qempty, sfull[2], pfull[2][2], ofull[2], oempty[2], met[4], mma,
-        dfull[kCkPieces], dempty[kCkPieces], done[2];
+    uint64_t kfull[R], vfull[R], kempty[R], vempty[R], qfull, qempty, sfull[2], pfull[2][2], ofull[2], oempty[2], join, met[4],
+        mma, dfull[kCkPieces], dempty[kCkPieces], done[2], ifull[kCkAhead], iempty[kCkAhead];
   };
   __shared__ Bars bar;
   __shared__ CkPiece s_piece[kCkPieces];
   __shared__ float2 s_ml[2][2][kCkKeys];         // [parity][group][row]: maximum and sum, units of one tile
   __shared__ uint32_t tmem_base;
-  __shared__ int abort_word;
+  __shared__ int abort_word, s_last;
+  __shared__ int2 s_page[KV8 ? kCkAhead : 1][8];  // int8: pool row of a tile's pages, and how many of their rows count
   volatile int* abort_flag = &abort_word;
   uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
   uint8_t* sQ = smem;
@@ -304,9 +311,10 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
       else if (q < &bar.qfull) n = 2;
       else if (q == &bar.qempty || q == &bar.mma) n = 2;
       else if (q >= &bar.pfull[0][0] && q < bar.ofull) n = 4;
-      else if (q >= bar.oempty && q < bar.met) n = 8;
+      else if (q >= bar.oempty && q < bar.met) n = 8;  // oempty, join
       else if (q >= bar.met && q < &bar.mma) n = 2;
-      else if (q >= bar.dempty && q < bar.done) n = ck_readers<KV8>();
+      else if (q >= bar.dempty && q < bar.done) n = kCkReaders;
+      else if (q >= bar.iempty) n = kCkWiden;
       mbar_init(p + i, n);
     }
     if (threadIdx.x == 0) *abort_flag = 0;
@@ -343,14 +351,15 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
       const int32_t* pt = a.page_table + (long long)w.b * a.pages_per_seq;
       auto page_row = [&](int t) {  // 8-row group of this lane's page; -2 reads zeros
         const int key0 = t * kCkKeys + lane * 16;
-        if (KV8 || lane >= 8 || key0 >= w.end) return -2;
+        if (lane >= 8 || key0 >= w.end) return -2;
         const int id = __ldg(pt + key0 / 16);
         if (id >= 0 && id < a.n_pages) return (id * a.Hkv + w.kvh) * 2;
         if (a.err && !is_v) atomicExch(a.err, 1);
         return -2;
       };
-      int row = page_row(w.t0);
-      if (!is_v) {
+      // The Q tiles, behind the first key tile: that one goes out (and the widening of the
+      // last unit's last tile, which looks a tile ahead, goes on) while Q is still in use.
+      auto queries = [&]() {
         if (n > 0) ok = mbar_wait(&bar.qempty, (n - 1) & 1) && !*abort_flag;
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) return;
@@ -364,8 +373,39 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
               ck_tma_4d(sQ + j * TILE + h * (TILE / NH), &map_q, 0, h, w.kvh * a.G, w.row0 + j * a.tile_tokens, &bar.qfull);
         }
         ++n;
-      }
-      if constexpr (!KV8) {
+      };
+      if constexpr (KV8) {
+        // the tile's pages to the widening warps, its codes and scales to L2
+        auto page = [&](int t) {
+          const int key0 = t * kCkKeys + lane * 16;
+          if (lane >= 8 || t >= w.t1 || key0 >= w.end) return -1;
+          return __ldg(pt + key0 / 16);
+        };
+        int id = page(w.t0);
+        for (int t = w.t0; t < w.t1; ++t, ++kn) {
+          const int s = kn % kCkAhead, id1 = page(t + 1), count = w.end - t * kCkKeys - lane * 16;
+          int at = -1;
+          if (id >= 0 && id < a.n_pages) {
+            at = (id * a.Hkv + w.kvh) * 16;
+            asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(a.k8 + (long long)at * HD), "n"(16 * HD) : "memory");
+            asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(a.v8 + (long long)at * HD), "n"(16 * HD) : "memory");
+            asm volatile("prefetch.global.L2 [%0];" ::"l"(a.k_scale + at) : "memory");
+            asm volatile("prefetch.global.L2 [%0];" ::"l"(a.v_scale + at) : "memory");
+          } else if (lane < 8 && count > 0 && a.err) {
+            atomicExch(a.err, 1);
+          }
+          if (kn >= kCkAhead) ok = mbar_wait(&bar.iempty[s], ((kn / kCkAhead) & 1) ^ 1);
+          ok = __all_sync(0xffffffffu, ok && !*abort_flag);
+          if (!ok) return;
+          if (lane < 8) s_page[s][lane] = make_int2(at, at < 0 ? 0 : min(16, max(0, count)));
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&bar.ifull[s]);
+          id = id1;
+          if (t == w.t0) queries();
+          if (!ok) return;
+        }
+      } else {
+        int row = page_row(w.t0);
         for (int t = w.t0; t < w.t1; ++t, ++kn) {
           const int s = kn % R;
           if (kn >= R) ok = mbar_wait(&empty[s], ((kn / R) & 1) ^ 1);
@@ -375,15 +415,13 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
           __syncwarp();
           if (lane < 8) ck_tma_4d(dst + s * TILE + lane * PAGE, map, 0, 0, 0, row, &full[s]);
           if (t + 1 < w.t1) row = page_row(t + 1);
+          if (!is_v && t == w.t0) queries();
+          if (!ok) return;
         }
       }
     };
     if (is_v) {
       CkWalk walk(a);
-      if (lane == 0) {
-        reinterpret_cast<long long*>(a.ws)[blockIdx.x] = walk.x;
-        reinterpret_cast<CkLeft*>(a.ws + kCkHead / 4)[blockIdx.x].end = 0;
-      }
       // piece m + 1 is described before the values of piece m are copied
       CkPiece w, w1;
       auto tell = [&](int m, CkPiece* p) {
@@ -411,6 +449,14 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
       while (next(w, ok)) {
         if (!w.empty()) copy(w);
         if (!ok) break;
+      }
+      if (KV8 && ok) {  // no more tiles
+        const int s = kn % kCkAhead;
+        if (kn >= kCkAhead) ok = __all_sync(0xffffffffu, mbar_wait(&bar.iempty[s], ((kn / kCkAhead) & 1) ^ 1));
+        if (lane == 0) {
+          s_page[s][0] = make_int2(-2, 0);
+          mbar_arrive(&bar.ifull[s]);
+        }
       }
     }
     if (!ok && lane == 0) fail();
@@ -560,100 +606,86 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
     // ---------------- int8 cache: bf16(q s) of the key tiles' rows.  Thread: 16 codes
     // (chunk c) of every PER-th row.  Each register of codes is filled again, for the
     // half tile after (V after K, then the next tile's K), as soon as it has been
-    // written out, so loads are in flight throughout; pages three tiles ahead are on
-    // their way to L2.
+    // written out, so loads are in flight throughout, across pieces too.
     constexpr int C = HD / 16;                             // chunks a row
     constexpr int PER = 32 * kCkWiden / C, N = kCkKeys / PER;  // rows at a time, turns a tile
-    constexpr int AHEAD = 3;
     const int wi = threadIdx.x - kCkWarpWiden * 32, c = wi % C, rr = wi / C;
     const int cb = 2 * (c & 3);
-    int kn = 0;
+    uint4 cw[N];
+    float sc[N];
+    int now[N], then[N];  // pool rows (fewer than 2^31) of this tile and the next; -1 reads zeros
+    // this thread's rows of tile k; false: there is none (or a wait ran out)
     bool ok = true;
-    CkPiece w;
-    while (next(w, ok)) {
-      const int32_t* pt = a.page_table + (long long)w.b * a.pages_per_seq;
-      // pool row (fewer than 2^31) of this thread's row in turn i of tile t; -1 reads zeros
-      auto pool_row = [&](int t, int i) {
-        const int key = t * kCkKeys + i * PER + rr;
-        if (key >= w.end) return -1;
-        const int id = __ldg(pt + key / 16);
-        if (id >= 0 && id < a.n_pages) return (id * a.Hkv + w.kvh) * 16 + key % 16;
-        if (a.err && c == 0) atomicExch(a.err, 1);
-        return -1;
-      };
-      // pages of tile t: the first warp those of K, the second those of V
-      auto ahead = [&](int t) {
-        const int key = t * kCkKeys + lane * 16;
-        if (warp > kCkWarpWiden + 1 || lane >= 8 || t >= w.t1 || key >= w.end) return;
-        const int id = __ldg(pt + key / 16);
-        if (id < 0 || id >= a.n_pages) return;
-        const int8_t* p = (warp == kCkWarpWiden ? a.k8 : a.v8) + (long long)(id * a.Hkv + w.kvh) * 16 * HD;
-        asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p), "n"(16 * HD) : "memory");
-      };
-      uint4 cw[N];
-      float sc[N];
-      int now[N];
-      auto fetch = [&](int i, int row, bool v) {
-        cw[i] = row >= 0 ? ld_nc16((v ? a.v8 : a.k8) + (long long)row * HD + c * 16) : make_uint4(0, 0, 0, 0);
-        sc[i] = row >= 0 ? __ldg((v ? a.v_scale : a.k_scale) + row) : 0.f;
-      };
-      if (!w.empty()) {
+    auto rows = [&](int k, int* r) {
+      const int s = k % kCkAhead;
+      ok = __all_sync(0xffffffffu, mbar_wait(&bar.ifull[s], (k / kCkAhead) & 1)) && !*abort_flag;
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok || s_page[s][0].x == -2) return false;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int row = i * PER + rr;
+        const int2 p = s_page[s][row >> 4];
+        r[i] = (row & 15) < p.y ? p.x + (row & 15) : -1;
+      }
+      return true;
+    };
+    auto fetch = [&](int i, int row, bool v) {
+      cw[i] = row >= 0 ? ld_nc16((v ? a.v8 : a.k8) + (long long)row * HD + c * 16) : make_uint4(0, 0, 0, 0);
+      sc[i] = row >= 0 ? __ldg((v ? a.v_scale : a.k_scale) + row) : 0.f;
+    };
+    bool more = rows(0, now);
+    if (more)
+#pragma unroll
+      for (int i = 0; i < N; ++i) fetch(i, now[i], false);
+    for (int kn = 0; more && ok; ++kn) {
+      more = rows(kn + 1, then);
+      if (!ok) break;
+#pragma unroll
+      for (int i = 0; i < N; ++i) then[i] = more ? then[i] : -1;
+#pragma unroll 1
+      for (int which = 0; which < 2; ++which) {
+        const int s = kn % R;
+        if (kn >= R) ok = mbar_wait(which ? &bar.vempty[s] : &bar.kempty[s], ((kn / R) & 1) ^ 1);
+        if (!__all_sync(0xffffffffu, ok) || __any_sync(0xffffffffu, *abort_flag != 0)) {
+          ok = false;
+          break;
+        }
+        uint8_t* dst = (which ? sV : sK) + s * TILE + (c >> 2) * 1024;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-          now[i] = pool_row(w.t0, i);
-          fetch(i, now[i], false);
-        }
-        for (int t = 1; t < AHEAD; ++t) ahead(w.t0 + t);
-      }
-      for (int t = w.t0; t < w.t1 && ok; ++t, ++kn) {
-        int then[N];
-        ahead(t + AHEAD);
+          const int row = i * PER + rr, sw = row & 7;
+          const uint32_t ww[4] = {cw[i].x ^ 0x80808080u, cw[i].y ^ 0x80808080u, cw[i].z ^ 0x80808080u,
+                                  cw[i].w ^ 0x80808080u};
+          const float2 s2 = make_float2(sc[i], sc[i]), z2 = make_float2(-32896.f, -32896.f);
+          uint32_t o[8];
 #pragma unroll
-        for (int i = 0; i < N; ++i) then[i] = t + 1 < w.t1 ? pool_row(t + 1, i) : -1;
-#pragma unroll 1
-        for (int which = 0; which < 2; ++which) {
-          const int s = kn % R;
-          if (kn >= R) ok = mbar_wait(which ? &bar.vempty[s] : &bar.kempty[s], ((kn / R) & 1) ^ 1);
-          if (!__all_sync(0xffffffffu, ok) || __any_sync(0xffffffffu, *abort_flag != 0)) {
-            ok = false;
-            break;
+          for (int j = 0; j < 8; ++j) {  // codes 2j, 2j + 1: fp32 2^15 + 128 + q
+            const uint32_t u = ww[j >> 1];
+            const float lo = __uint_as_float(__byte_perm(u, 0x47000000u, (j & 1) ? 0x7424 : 0x7404));
+            const float hi = __uint_as_float(__byte_perm(u, 0x47000000u, (j & 1) ? 0x7434 : 0x7414));
+            const float2 f = ck_mul2(ck_add2(make_float2(lo, hi), z2), s2);
+            o[j] = pa_pack(f.x, f.y);
           }
-          uint8_t* dst = (which ? sV : sK) + s * TILE + (c >> 2) * 1024;
-#pragma unroll
-          for (int i = 0; i < N; ++i) {
-            const int row = i * PER + rr, sw = row & 7;
-            const uint32_t ww[4] = {cw[i].x ^ 0x80808080u, cw[i].y ^ 0x80808080u, cw[i].z ^ 0x80808080u,
-                                    cw[i].w ^ 0x80808080u};
-            const float2 s2 = make_float2(sc[i], sc[i]), z2 = make_float2(-32896.f, -32896.f);
-            uint32_t o[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {  // codes 2j, 2j + 1: fp32 2^15 + 128 + q
-              const uint32_t u = ww[j >> 1];
-              const float lo = __uint_as_float(__byte_perm(u, 0x47000000u, (j & 1) ? 0x7424 : 0x7404));
-              const float hi = __uint_as_float(__byte_perm(u, 0x47000000u, (j & 1) ? 0x7434 : 0x7414));
-              const float2 f = ck_mul2(ck_add2(make_float2(lo, hi), z2), s2);
-              o[j] = pa_pack(f.x, f.y);
-            }
-            fetch(i, which ? then[i] : now[i], !which);
-            const uint4 e = make_uint4(o[0], o[1], o[2], o[3]), f = make_uint4(o[4], o[5], o[6], o[7]);
-            uint8_t* rp = dst + (row >> 3) * SBO + sw * 128;
-            // the lanes of a row's upper half write their odd chunk first: eight lanes, eight banks of 16 bytes
-            if (c < 4) {
-              *reinterpret_cast<uint4*>(rp + ((cb ^ sw) << 4)) = e;
-              *reinterpret_cast<uint4*>(rp + (((cb + 1) ^ sw) << 4)) = f;
-            } else {
-              *reinterpret_cast<uint4*>(rp + (((cb + 1) ^ sw) << 4)) = f;
-              *reinterpret_cast<uint4*>(rp + ((cb ^ sw) << 4)) = e;
-            }
+          fetch(i, which ? then[i] : now[i], !which);
+          const uint4 e = make_uint4(o[0], o[1], o[2], o[3]), f = make_uint4(o[4], o[5], o[6], o[7]);
+          uint8_t* rp = dst + (row >> 3) * SBO + sw * 128;
+          // the lanes of a row's upper half write their odd chunk first: eight lanes, eight banks of 16 bytes
+          if (c < 4) {
+            *reinterpret_cast<uint4*>(rp + ((cb ^ sw) << 4)) = e;
+            *reinterpret_cast<uint4*>(rp + (((cb + 1) ^ sw) << 4)) = f;
+          } else {
+            *reinterpret_cast<uint4*>(rp + (((cb + 1) ^ sw) << 4)) = f;
+            *reinterpret_cast<uint4*>(rp + ((cb ^ sw) << 4)) = e;
           }
-          fence_proxy_async();  // the MMAs read the tile through the async proxy
-          __syncwarp();
-          if (lane == 0) mbar_arrive(which ? &bar.vfull[s] : &bar.kfull[s]);
         }
-#pragma unroll
-        for (int i = 0; i < N; ++i) now[i] = then[i];
+        fence_proxy_async();  // the MMAs read the tile through the async proxy
+        __syncwarp();
+        if (lane == 0) mbar_arrive(which ? &bar.vfull[s] : &bar.kfull[s]);
       }
       if (!ok) break;
+      if (lane == 0) mbar_arrive(&bar.iempty[kn % kCkAhead]);
+#pragma unroll
+      for (int i = 0; i < N; ++i) now[i] = then[i];
     }
     if (!ok && lane == 0) fail();
   } else if (warp < kCkSoft) {
@@ -665,7 +697,7 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
     const float scale = kPaLog2e * rsqrtf((float)HD);
     const int tok = row / a.G;  // of a tile's packed rows
     const bool packed = row < a.tile_tokens * a.G;
-    int sn = 0, on[2] = {0, 0}, mn = 0;
+    int sn = 0, on[2] = {0, 0}, mn = 0, jn = 0;
     bool ok = true;
     uint8_t* stage = sV + R * TILE + warp * kCkStage;
     CkPiece w;
@@ -792,73 +824,80 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
       const float inv = l > 0.f ? 1.f / l : 0.f;
       // pair: this group's tile, all columns; else half of the sum's columns a group
       const int x0 = pair ? 0 : j * (HD / 2), x1 = pair ? HD : x0 + HD / 2;
-      if (on_warp) {
-        const uint32_t src = pair ? to : lane_base + kCkO;
-        auto load = [&](int x, float* r) {  // 32 columns of the sums
-          if (!have) {
+      const uint32_t src = pair ? to : lane_base + kCkO;
+      auto load = [&](int x, float* r) {  // 32 columns of the sums
+        if (!have) {
 #pragma unroll
-            for (int y = 0; y < 32; ++y) r[y] = 0.f;
-            return;
+          for (int y = 0; y < 32; ++y) r[y] = 0.f;
+          return;
+        }
+        tc_ld<32>(src + x, reinterpret_cast<uint32_t*>(r));
+        if (pair) return;
+#pragma unroll
+        for (int y = 0; y < 32; ++y) r[y] *= a0;
+        if (!use1) return;
+#pragma unroll
+        for (int y0 = 0; y0 < 32; y0 += 16) {
+          uint32_t u[16];
+          tc_ld<16>(src + 128 + x + y0, u);
+#pragma unroll
+          for (int y = 0; y < 16; ++y) r[y0 + y] = fmaf(a1, __uint_as_float(u[y]), r[y0 + y]);
+        }
+      };
+      // rows to out, through shared memory: four lanes to a row's 64 bytes; chunk c of row r at c ^ (r / 2 % 4)
+      auto write = [&](auto from, float inv) {
+        uint16_t* o = a.out + ((long long)(w.row0 + jq * a.tile_tokens) * a.H + (long long)w.kvh * a.G) * HD;
+        int at[4];  // rows 8 y + lane / 4 of this warp's: where each begins, or -1
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          const int r2 = quad * 32 + y * 8 + (lane >> 2), t2 = r2 / a.G;
+          at[y] = r2 < a.tile_tokens * a.G && t2 < tile_n ? (t2 * a.H + r2 - t2 * a.G) * HD : -1;
+        }
+#pragma unroll 1
+        for (int x = x0; x < x1; x += 32) {
+          float r[32];
+          from(x, r);
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            uint32_t p[4];
+#pragma unroll
+            for (int y = 0; y < 4; ++y) p[y] = pa_pack(r[8 * c + 2 * y] * inv, r[8 * c + 2 * y + 1] * inv);
+            *reinterpret_cast<uint4*>(stage + lane * 64 + ((c ^ ((lane >> 1) & 3)) << 4)) = make_uint4(p[0], p[1], p[2], p[3]);
           }
-          tc_ld<32>(src + x, reinterpret_cast<uint32_t*>(r));
-          if (pair) return;
-#pragma unroll
-          for (int y = 0; y < 32; ++y) r[y] *= a0;
-          if (!use1) return;
-#pragma unroll
-          for (int y0 = 0; y0 < 32; y0 += 16) {
-            uint32_t u[16];
-            tc_ld<16>(src + 128 + x + y0, u);
-#pragma unroll
-            for (int y = 0; y < 16; ++y) r[y0 + y] = fmaf(a1, __uint_as_float(u[y]), r[y0 + y]);
-          }
-        };
-        if (whole) {
-          // through shared memory, four lanes to a row's 64 bytes; chunk c of row r at c ^ (r / 2 % 4)
-          uint16_t* o = a.out + ((long long)(w.row0 + jq * a.tile_tokens) * a.H + (long long)w.kvh * a.G) * HD;
-          // rows 8 y + lane / 4 of this warp's: where each begins, or -1
-          int at[4];
+          __syncwarp();
 #pragma unroll
           for (int y = 0; y < 4; ++y) {
-            const int r2 = quad * 32 + y * 8 + (lane >> 2), t2 = r2 / a.G;
-            at[y] = r2 < a.tile_tokens * a.G && t2 < tile_n ? (t2 * a.H + r2 - t2 * a.G) * HD : -1;
+            const int lr = y * 8 + (lane >> 2);
+            const uint4 p = *reinterpret_cast<const uint4*>(stage + lr * 64 + (((lane & 3) ^ ((lr >> 1) & 3)) << 4));
+            if (at[y] >= 0) *reinterpret_cast<uint4*>(o + at[y] + x + (lane & 3) * 8) = p;
           }
+          __syncwarp();
+        }
+      };
+      const int r256 = jq * kCkKeys + row;
+      auto slot = [&](int i) {  // part i of this unit
+        return a.ws + kCkHead + ((size_t)(w.own + i) * 2 + (i == 0 ? 1 : 0)) * ck_slot<HD>();
+      };
+      auto keep = [&](uint8_t* p, auto from) {  // O to a slot
 #pragma unroll 1
-          for (int x = x0; x < x1; x += 32) {
-            float r[32];
-            load(x, r);
+        for (int x = x0; x < x1; x += 32) {
+          float f[32];
+          from(x, f);
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-              uint32_t p[4];
-#pragma unroll
-              for (int y = 0; y < 4; ++y) p[y] = pa_pack(r[8 * c + 2 * y] * inv, r[8 * c + 2 * y + 1] * inv);
-              *reinterpret_cast<uint4*>(stage + lane * 64 + ((c ^ ((lane >> 1) & 3)) << 4)) = make_uint4(p[0], p[1], p[2], p[3]);
-            }
-            __syncwarp();
-#pragma unroll
-            for (int y = 0; y < 4; ++y) {
-              const int lr = y * 8 + (lane >> 2);
-              const uint4 p = *reinterpret_cast<const uint4*>(stage + lr * 64 + (((lane & 3) ^ ((lr >> 1) & 3)) << 4));
-              if (at[y] >= 0) *reinterpret_cast<uint4*>(o + at[y] + x + (lane & 3) * 8) = p;
-            }
-            __syncwarp();
-          }
+          for (int y = 0; y < 8; ++y)
+            reinterpret_cast<float4*>(p)[(size_t)(x / 4 + y) * kCkRows + r256] =
+                make_float4(f[4 * y], f[4 * y + 1], f[4 * y + 2], f[4 * y + 3]);
+        }
+      };
+      constexpr size_t ML = (size_t)kCkRows * HD * 4;
+      if (on_warp) {
+        if (whole) {
+          write(load, inv);
         } else {
-          uint8_t* slot = a.ws + kCkHead + ((size_t)blockIdx.x * 2 + (w.first() ? 1 : 0)) * ck_slot<HD>();
-          const int r = jq * kCkKeys + row;
-          if (have)
-#pragma unroll 1
-            for (int x = x0; x < x1; x += 32) {
-              float f[32];
-              load(x, f);
-#pragma unroll
-              for (int y = 0; y < 8; ++y)
-                reinterpret_cast<float4*>(slot)[(size_t)(x / 4 + y) * kCkRows + r] =
-                    make_float4(f[4 * y], f[4 * y + 1], f[4 * y + 2], f[4 * y + 3]);
-            }
+          uint8_t* p = slot(blockIdx.x - w.own);
+          if (have) keep(p, load);
           if (x0 == 0)
-            reinterpret_cast<float2*>(slot + (size_t)kCkRows * HD * 4)[r] =
-                make_float2(have && l > 0.f ? m : -INFINITY, have ? l : 0.f);
+            reinterpret_cast<float2*>(p + ML)[r256] = make_float2(have && l > 0.f ? m : -INFINITY, have ? l : 0.f);
         }
       }
       if (have) {
@@ -874,9 +913,73 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
           }
         }
       }
-      if (threadIdx.x == 0 && w.first() && !w.last()) {
-        const CkLeft left = {w.stop, w.row0, w.n, w.kvh};
-        reinterpret_cast<CkLeft*>(a.ws + kCkHead / 4)[blockIdx.x] = left;
+      if (!whole) {
+        // o = sum 2^(m_i - m) O_i / sum 2^(m_i - m) l_i over the unit's parts, in their
+        // order, by the last CTA to bring its part: first among kCkGroup neighbours, then
+        // (a unit that more CTAs share) the last group among the groups.
+        const int mine = (blockIdx.x - w.own) / kCkGroup, groups = (w.parts + kCkGroup - 1) / kCkGroup;
+        int* tickets = reinterpret_cast<int*>(a.ws) + w.own * kCkTickets;
+        // whether this CTA is the last of n to get here; what the others wrote is then there
+        auto last_of = [&](int* ticket, int n) {
+          __threadfence();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&bar.join);
+          ok = ok && __all_sync(0xffffffffu, mbar_wait(&bar.join, jn++ & 1));
+          if (threadIdx.x == 0) {
+            s_last = atomicAdd(ticket, 1) == n - 1;
+            if (s_last) *ticket = 0;
+          }
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&bar.join);
+          ok = ok && __all_sync(0xffffffffu, mbar_wait(&bar.join, jn++ & 1));
+          __threadfence();
+          return ok && s_last;
+        };
+        float mm = -INFINITY, ll = 0.f;
+        int i0 = mine * kCkGroup, step = 1, n = min(kCkGroup, w.parts - i0);
+        size_t ml_at = ML;
+        auto sums = [&]() {  // the parts' common maximum and sum
+          mm = -INFINITY, ll = 0.f;
+          for (int i = 0; i < n; ++i) mm = fmaxf(mm, __ldcg(reinterpret_cast<const float2*>(slot(i0 + i * step) + ml_at) + r256).x);
+          for (int i = 0; i < n; ++i) {
+            const float2 f = __ldcg(reinterpret_cast<const float2*>(slot(i0 + i * step) + ml_at) + r256);
+            if (f.x != -INFINITY) ll += exp2f(f.x - mm) * f.y;
+          }
+        };
+        auto added = [&](int x, float* r) {  // 32 columns of the parts' sum
+#pragma unroll
+          for (int y = 0; y < 32; ++y) r[y] = 0.f;
+#pragma unroll 1
+          for (int i = 0; i < n; ++i) {
+            const uint8_t* p = slot(i0 + i * step);
+            const float mi = __ldcg(reinterpret_cast<const float2*>(p + ml_at) + r256).x;
+            float4 f[8];
+#pragma unroll
+            for (int y = 0; y < 8; ++y) f[y] = __ldcg(reinterpret_cast<const float4*>(p) + (size_t)(x / 4 + y) * kCkRows + r256);
+            if (mi == -INFINITY) continue;  // (its O was not written)
+            const float c = exp2f(mi - mm);
+#pragma unroll
+            for (int y = 0; y < 8; ++y) {
+              r[4 * y] = fmaf(c, f[y].x, r[4 * y]), r[4 * y + 1] = fmaf(c, f[y].y, r[4 * y + 1]);
+              r[4 * y + 2] = fmaf(c, f[y].z, r[4 * y + 2]), r[4 * y + 3] = fmaf(c, f[y].w, r[4 * y + 3]);
+            }
+          }
+        };
+        bool here = last_of(tickets + mine, n);
+        if (here && groups > 1) {
+          if (on_warp) {
+            sums();
+            keep(slot(i0), added);
+            if (x0 == 0) reinterpret_cast<float2*>(slot(i0) + ML + kCkRows * 8)[r256] = make_float2(mm, ll);
+          }
+          here = last_of(tickets + kCkTickets - 1, groups);
+          i0 = 0, step = kCkGroup, n = groups, ml_at = ML + kCkRows * 8;
+        }
+        if (here && on_warp) {
+          sums();
+          write(added, ll > 0.f ? 1.f / ll : 0.f);
+        }
+        if (!ok) break;
       }
     }
     if (!ok && lane == 0) fail();
@@ -886,66 +989,6 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
   if (warp == kCkWarpMma) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(kCkTmemCols) : "memory");
-  }
-}
-
-// ------------------------------------------------------------------ joining the parts
-// The unit that CTA c = blockIdx.x began and left unfinished:
-// o = sum_i 2^(m_i - m) O_i / sum_i 2^(m_i - m) l_i over the CTAs whose stretches begin
-// before the unit's end, in their order.  A block takes every gridDim.y-th block of 32
-// rows and 32 columns; its four groups of threads share a unit's parts (up to one a
-// CTA, where there is one sequence and KV head) and add up in order.
-constexpr int kCkJoinParts = 4, kCkJoinBlocks = 16;
-template <int HD>
-__global__ void __launch_bounds__(256)
-    attn_chunk_join_kernel(const uint8_t* __restrict__ ws, int ctas, int H, int G, int tile_tokens,
-                           uint16_t* __restrict__ out) {
-  __shared__ float4 s_o[kCkJoinParts - 1][64];
-  __shared__ float2 s_ml[kCkJoinParts][8];
-  pdl_trigger();
-  pdl_wait();
-  const int c = blockIdx.x;
-  const CkLeft u = reinterpret_cast<const CkLeft*>(ws + kCkHead / 4)[c];
-  if (u.end == 0) return;
-  // 8 rows in the lanes' low bits where the parts are read, 8 column quads above
-  const int tid = threadIdx.x & 63, part = threadIdx.x >> 6;
-  const long long* begins = reinterpret_cast<const long long*>(ws);
-  int last = c;
-  while (last + 1 < ctas && begins[last + 1] < u.end) ++last;
-  const int per = (last - c + kCkJoinParts) / kCkJoinParts, k0 = c + part * per, k1 = min(last + 1, k0 + per);
-  const int rows = u.n > tile_tokens ? kCkKeys + (u.n - tile_tokens) * G : u.n * G;  // packed rows up to the last
-  for (int item = blockIdx.y; item < (rows + 7) / 8 * (HD / 32); item += gridDim.y) {
-    const int r = item / (HD / 32) * 8 + (tid & 7), c4 = item % (HD / 32) * 8 + (tid >> 3);
-    float m = -INFINITY, l = 0.f;
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    auto add = [&](float2 ml, float4 f) {
-      if (ml.x == -INFINITY) return;
-      const float m2 = fmaxf(m, ml.x), x = exp2f(m - m2), y = exp2f(ml.x - m2);
-      m = m2;
-      l = l * x + ml.y * y;
-      o = make_float4(o.x * x + f.x * y, o.y * x + f.y * y, o.z * x + f.z * y, o.w * x + f.w * y);
-    };
-#pragma unroll 4
-    for (int k = k0; k < k1; ++k) {
-      const uint8_t* p = ws + kCkHead + ((size_t)k * 2 + (k == c ? 1 : 0)) * ck_slot<HD>();
-      // (a CTA whose stretch is empty has no part)
-      const bool none = k > c && k + 1 < ctas && begins[k + 1] == begins[k];
-      const float2 ml = reinterpret_cast<const float2*>(p + (size_t)kCkRows * HD * 4)[r];
-      add(none ? make_float2(-INFINITY, 0.f) : ml, reinterpret_cast<const float4*>(p)[(size_t)c4 * kCkRows + r]);
-    }
-    if (part) s_o[part - 1][tid] = o;
-    if (tid < 8) s_ml[part][tid] = make_float2(m, l);
-    __syncthreads();
-    const int rt = r % kCkKeys, tok = rt / G, row = tok + (r >= kCkKeys ? tile_tokens : 0);
-    if (part == 0) {
-#pragma unroll
-      for (int k = 1; k < kCkJoinParts; ++k) add(s_ml[k][tid & 7], s_o[k - 1][tid]);
-      const float inv = l > 0.f ? 1.f / l : 0.f;
-      if (r < rows && rt < tile_tokens * G && row < u.n)
-        *reinterpret_cast<uint2*>(out + ((long long)(u.row0 + row) * H + (long long)u.kvh * G + rt % G) * HD + c4 * 4) =
-            make_uint2(pa_pack(o.x * inv, o.y * inv), pa_pack(o.z * inv, o.w * inv));
-    }
-    __syncthreads();
   }
 }
 
@@ -977,8 +1020,8 @@ static int ck_sms() {
   int dev = 0, sms = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
       sms <= 0)
-    sms = 152;
-  return std::min(sms, 1024);
+    sms = kCkMaxCtas;
+  return sms;
 }
 
 bool attention_chunk_fits(int n_tokens, int n_heads, int n_kv_heads, int max_new, int max_len) {
@@ -986,7 +1029,7 @@ bool attention_chunk_fits(int n_tokens, int n_heads, int n_kv_heads, int max_new
 }
 
 size_t attention_chunk_ws_bytes(int B, int n_heads, int n_kv_heads, int head_dim, int max_new) {
-  return kCkHead + (size_t)2 * 152 * (head_dim == 64 ? ck_slot<64>() : ck_slot<128>());
+  return kCkHead + (size_t)2 * kCkMaxCtas * (head_dim == 64 ? ck_slot<64>() : ck_slot<128>());
 }
 
 template <int HD, bool KV8>
@@ -1007,10 +1050,8 @@ static cudaError_t launch_ck(const uint16_t* q, int q_stride, const fp_kv_view& 
   }
   static std::atomic<unsigned long long> attr{0};
   FP_CUDA_TRY(smem_limit_once(attn_chunk_kernel<HD, KV8>, ck_smem<HD>(), &attr));
-  const int grid = std::min(ck_sms(), 152);
-  FP_CUDA_TRY(launch(attn_chunk_kernel<HD, KV8>, dim3(grid), dim3(ck_threads<KV8>()), (size_t)ck_smem<HD>(), s, mq, mk, mv, a));
-  return launch_early(attn_chunk_join_kernel<HD>, dim3(grid, kCkJoinBlocks), dim3(256), 0, s, (const uint8_t*)a.ws, grid, a.H,
-                      a.G, a.tile_tokens, a.out);
+  return launch(attn_chunk_kernel<HD, KV8>, dim3(std::min(ck_sms(), kCkMaxCtas)), dim3(ck_threads<KV8>()),
+                (size_t)ck_smem<HD>(), s, mq, mk, mv, a);
 }
 
 cudaError_t launch_attention_chunk(const uint16_t* q, int q_stride, int n_tokens, int B, int n_heads,

@@ -41,7 +41,7 @@ int main() {
   for (int it = 0; it < 3000; ++it) {  // the stretches
     const int G = 1 + rand() % 16, tt = ck_tile_tokens(G), T = 2 * tt, B = 1 + rand() % 12, Hkv = 1 + rand() % 5;
     const int grid = 1 + rand() % 152;
-    struct Unit { long long x; int nt; std::vector<int> seen; };
+    struct Unit { long long x; int nt; std::vector<int> seen; int own = -1, parts = 0; };
     std::vector<Unit> units;
     long long W = 0;
     for (int b = 0; b < B; ++b) {
@@ -73,7 +73,14 @@ int main() {
         if (p > u.x && t0 < kCkSnap) return bad("a border inside a unit's start", it);
         if (t1 <= t0) return bad("a part without keys", it);
         for (int t = t0; t < t1; ++t) ++u.seen[t];
+        if (u.own < 0) u.own = c;
+        if (c != u.own + u.parts++) return bad("the parts of a unit are not neighbours", it);
       }
+    }
+    for (auto& u : units) {
+      int own, parts;
+      ck_parts(u.x, u.nt, W, g, &own, &parts);
+      if (u.nt > 0 && u.parts > 1 && (own != u.own || parts != u.parts)) return bad("ck_parts", it);
     }
     for (auto& u : units)
       for (int k : u.seen)

@@ -95,7 +95,7 @@ class Batch:
         need = f.fp_op_attention_chunk_workspace_bytes(self.B, self.H, self.Hkv, self.hd, max_new or self.max_new)
         if ws is None:
             ws = empty(need + 256)
-            ws.fill_(255)  # any content will do
+            ws[65536:] = 255  # behind the tickets any content will do
         err = empty(1, np.int32)
         f.fp_op_attention_chunk(ptr(qd), qd.shape[1], self.N, self.B, self.H, view or self.view,
                                 ptr(dev(self.cu if cu is None else cu)), ptr(dev(self.pos if pos is None else pos)),
