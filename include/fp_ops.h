@@ -235,7 +235,7 @@ int fp_op_attention_prefill(const uint16_t* q, int q_stride, int B, int S, int n
  * they were.  cu and pos are read on the device, so one captured launch serves
  * other lengths within the same bounds.  A cu that decreases or leaves
  * [0, n_tokens] sets *err = 1 (err may be NULL) and no row outside the buffers is
- * touched.  All buffers 16-byte aligned and strides multiples of 8 elements, else
+ * touched (fp_op_attention_chunk: nothing is written).  All buffers 16-byte aligned and strides multiples of 8 elements, else
  * FP_ERR_UNSUPPORTED; pools of fewer than 2^31 rows. */
 
 /* RoPE + KV-cache append of a chunk: as fp_op_rope_kv, for a ragged batch and

@@ -88,10 +88,10 @@ struct CkSeq {
   }
 };
 
-// Whether a sequence's places, over all KV heads, stay below 2^31 whatever its lengths.
-inline bool ck_fits(int n_tokens, int max_new, int max_len, int Hkv, int tile_tokens) {
-  const long long units = ((long long)std::min(n_tokens, max_new) + 2 * tile_tokens - 1) / (2 * tile_tokens);
-  return units * Hkv * (kCkStart + (max_len + kCkKeys - 1LL) / kCkKeys) < (1LL << 31);
+// Whether the line of any batch within these bounds is shorter than 2^31 places.
+inline bool ck_fits(int n_tokens, int B, int max_len, int Hkv, int tile_tokens) {
+  const long long units = n_tokens / (2 * tile_tokens) + (long long)B;
+  return units * Hkv < (1LL << 31) && units * Hkv * (kCkStart + (max_len + kCkKeys - 1LL) / kCkKeys) < (1LL << 31);
 }
 
 // A border at place `off` of a unit of nt key tiles, moved off its ends: the place to
@@ -102,25 +102,27 @@ FP_CK int ck_snap(int off, int nt) {
   return off;
 }
 
-// x y / z without a 64-bit division where the numbers are small.
-FP_CK long long ck_muldiv(long long x, int y, int z) {
-  return x < (1 << 22) ? (long long)((uint32_t)x * (uint32_t)y / (uint32_t)z) : x * y / z;
+// Where the stretch of CTA c of g begins, before its border is moved: floor(W c / g).
+FP_CK int ck_begin(int c, int W, int g) {
+  const unsigned q = (unsigned)W / (unsigned)g, r = (unsigned)W - q * g;
+  return (int)(q * c + r * c / (unsigned)g);
 }
 
-// The first of g CTAs whose stretch begins, before its border is moved, at t or behind:
-// floor(W c / g) >= t.
-FP_CK int ck_first_from(long long t, long long W, int g) { return (int)((t * g + W - 1) / W); }
+// The first of g CTAs with ck_begin(c) >= t (1 <= t).
+FP_CK int ck_first_from(int t, int W, int g) {
+  return (int)(((unsigned long long)t * g + (unsigned)W - 1) / (unsigned)W);
+}
 
 // The CTAs that share the unit of nt key tiles at place x: *own begins it, *parts in all.
-FP_CK void ck_parts(long long x, int nt, long long W, int g, int* own, int* parts) {
+FP_CK void ck_parts(int x, int nt, int W, int g, int* own, int* parts) {
   *own = ck_first_from(x + kCkStart + kCkSnap, W, g) - 1;
   *parts = ck_first_from(x + kCkStart + nt - kCkSnap + 1, W, g) - *own;
 }
 
-// CTAs that take part of W places (at most 1024).
-FP_CK int ck_ctas(long long W, int grid) {
-  const long long most = W / kCkLeast > 1 ? W / kCkLeast : 1;  // (kCkLeast: a power of two)
-  return most < grid ? (int)most : grid;
+// CTAs that take part of W places.
+FP_CK int ck_ctas(int W, int grid) {
+  const int most = W / kCkLeast > 1 ? W / kCkLeast : 1;
+  return most < grid ? most : grid;
 }
 
 }  // namespace fpk

@@ -48,13 +48,8 @@ constexpr int kCkSoft = 8;                        // softmax warps
 constexpr int kCkWarpQ = 8, kCkWarpMma = 9, kCkWarpPlan = 11, kCkWarpWiden = 12, kCkWiden = 8;
 template <bool KV8>
 constexpr int ck_threads() { return KV8 ? (kCkWarpWiden + kCkWiden) * 32 : 384; }
-// Registers a thread, moved to the softmax, which holds a row of scores (int8 cache:
-// half of one): 384 threads launch with 168, 256 x 208 + 128 x 88 = 384 x 168; 640 with
-// 96, 256 x 128 + 384 x 72 <= 640 x 96
-template <bool KV8>
-constexpr int ck_reg_soft() { return KV8 ? 128 : 208; }
-template <bool KV8>
-constexpr int ck_reg_other() { return KV8 ? 72 : 88; }
+// Registers a thread: 384 threads may have 168, which none needs; 640 (int8 cache) launch
+// with 96, moved to the softmax: 256 x 120 + 384 x 80 = 640 x 96
 constexpr int kCkReaders = kCkSoft + 3;           // warps that read each piece's description: softmax, Q, MMA
 constexpr int kCkPieces = 4;                      // pieces described ahead
 constexpr int kCkAhead = 8;                       // int8 cache: key tiles whose pages are known ahead
@@ -148,98 +143,100 @@ struct __align__(16) CkPiece {
   FP_DEV bool uses(int j) const { return pair() ? (j ? t1 > t0 : e0 > t0) : t1 - t0 > j; }  // accumulator j
 };
 
-// The plan of this CTA's stretch, by one whole warp, and its pieces one by one.
+// The plan of this CTA's stretch, by one whole warp, and its pieces one by one.  One
+// warp's instructions follow each other at 4-6 cycles and every kernel starts with cold
+// instruction caches, so it is kept short: 32-bit places (ck_fits), both ends of the
+// stretch in two lanes at once.
 struct CkWalk {
   const CkArgs& a;
   CkSeq s;
   int b, kvh, u, off;  // the next place: `off` into unit u of (b, kvh)
-  long long x, rem;    // its place on the line, and places left
-  long long W;         // the line's length, shared among g CTAs
-  int g;
-  FP_DEV int places(int bb) {  // of sequence bb; bounds that are broken are reported
-    int first, count;
+  int x, rem;          // its place on the line, and places left
+  int W, g;            // the line's length, shared among g CTAs
+  FP_DEV int load(int bb, bool* fine) {  // sequence bb, and its places; false: a bound is broken
     const int lo = __ldg(a.cu + bb), hi = __ldg(a.cu + bb + 1), p = __ldg(a.pos + bb);
-    first = max(lo, 0);
-    count = max(0, min(hi, a.n_tokens) - first);
-    const bool fine = s.set(first, count, p, a.tile_tokens, a.max_new, a.max_len);
-    if ((!fine || lo < 0 || hi < lo || hi > a.n_tokens) && blockIdx.x == 0 && a.err) atomicExch(a.err, 1);
-    return s.cost(2 * a.tile_tokens) * a.Hkv;
+    *fine = s.set(lo, hi - lo, p, a.tile_tokens, a.max_new, a.max_len);
+    return lo < 0 || hi < lo || hi > a.n_tokens ? -1 : s.cost(2 * a.tile_tokens) * a.Hkv;
   }
   FP_DEV CkWalk(const CkArgs& a) : a(a) {
     const int lane = threadIdx.x & 31, T = 2 * a.tile_tokens;
     // the line's length (up to 32 sequences: their places stay in the lanes)
-    W = 0;
     int c = 0;
+    bool fine = true, good = true;
+    W = 0;
 #pragma unroll 1
     for (int b0 = 0; b0 < a.B; b0 += 32) {
-      c = b0 + lane < a.B ? places(b0 + lane) : 0;
+      c = 0;
+      bool f = true;
+      if (b0 + lane < a.B) c = load(b0 + lane, &f);
+      fine = fine && f && c >= 0, good = good && c >= 0;
       W += c;
     }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) W += __shfl_xor_sync(0xffffffffu, W, o);
+    if (!__all_sync(0xffffffffu, fine) && blockIdx.x == 0 && lane == 0 && a.err) atomicExch(a.err, 1);
+    // (a cu that decreases or leaves the buffers: nothing is done)
+    W = __all_sync(0xffffffffu, good) ? __reduce_add_sync(0xffffffffu, W) : 0;
+    b = a.B, kvh = u = off = 0, x = W, rem = 0;
+    if (W == 0) return;
     g = ck_ctas(W, gridDim.x);
-    const int cta = blockIdx.x;
-    const long long x0 = cta < g ? ck_muldiv(W, cta, g) : W, x1 = cta + 1 < g ? ck_muldiv(W, cta + 1, g) : W;
-    b = a.B, kvh = u = off = 0;
-    x = W;
-    long long stop = W, base = 0;
+    // lane 0: where the stretch begins, lane 1 where the next one does
+    const int cta = min((int)blockIdx.x + (lane & 1), g), at = cta < g ? ck_begin(cta, W, g) : W;
+    const int at0 = __shfl_sync(0xffffffffu, at, 0), at1 = __shfl_sync(0xffffffffu, at, 1);
+    if (at0 >= W) return;
+    int base = 0;
+    CkSeq mine;
+    int from = 0, per = 1;
+    bool found0 = false, found1 = at1 >= W;
 #pragma unroll 1
-    for (int b0 = 0; b0 < a.B && x0 < W; b0 += 32) {
-      if (a.B > 32) c = b0 + lane < a.B ? places(b0 + lane) : 0;
-      long long incl = c;
+    for (int b0 = 0; b0 < a.B && !(found0 && found1); b0 += 32) {
+      bool f;
+      if (a.B > 32) c = b0 + lane < a.B ? load(b0 + lane, &f) : 0;
+      int incl = c;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
-        const long long f = __shfl_up_sync(0xffffffffu, incl, o);
-        if (lane >= o) incl += f;
+        const int v = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += v;
       }
       incl += base;
       base = __shfl_sync(0xffffffffu, incl, 31);
-#pragma unroll 1
-      for (int e = 0; e < 2; ++e) {
-        const long long at = e ? x1 : x0, before = incl - c;
-        if (c == 0 || at < before || at >= incl) continue;
-        // one lane gets here: the unit at this place, and its border off the unit's ends
-        const int per = s.cost(T), d = (int)(at - before), h = (int)((unsigned)d / (unsigned)per), in = d - h * per;
-        const int v = s.unit_at(in, T), start = s.before(v, T), nt = s.tiles(v, T), o = ck_snap(in - start, nt);
-        const long long to = before + (long long)h * per + start + o;
-        if (e) {
-          stop = to;
-        } else {
-          x = to, b = b0 + lane, kvh = h, u = v, off = o;
-          if (o == kCkStart + nt) {  // behind the unit: the next one's beginning
-            off = 0;
-            if (++u == s.units) u = 0, ++kvh;
-          }
-        }
-      }
-      const unsigned m0 = __ballot_sync(0xffffffffu, x < W || b < a.B), m1 = __ballot_sync(0xffffffffu, stop < W);
-      if (m0) {
-        const int l = __ffs(m0) - 1;
-        x = __shfl_sync(0xffffffffu, x, l), b = __shfl_sync(0xffffffffu, b, l), kvh = __shfl_sync(0xffffffffu, kvh, l);
-        u = __shfl_sync(0xffffffffu, u, l), off = __shfl_sync(0xffffffffu, off, l);
-      }
-      if (m1) {
-        stop = __shfl_sync(0xffffffffu, stop, __ffs(m1) - 1);
-        break;
+      const unsigned m0 = __ballot_sync(0xffffffffu, at0 < incl), m1 = __ballot_sync(0xffffffffu, at1 < incl);
+      const bool new0 = m0 && !found0, new1 = m1 && !found1;
+      found0 |= new0, found1 |= new1;
+      const int l = lane == 1 ? __ffs(m1) - 1 : __ffs(m0) - 1;  // whose sequence this lane looks into
+      const int sb = b0 + l, first = __shfl_sync(0xffffffffu, incl - c, l & 31), cost = __shfl_sync(0xffffffffu, c, l & 31);
+      CkSeq t;
+      t.row0 = __shfl_sync(0xffffffffu, s.row0, l & 31), t.n = __shfl_sync(0xffffffffu, s.n, l & 31);
+      t.pos = __shfl_sync(0xffffffffu, s.pos, l & 31), t.end = __shfl_sync(0xffffffffu, s.end, l & 31);
+      t.units = __shfl_sync(0xffffffffu, s.units, l & 31), t.bad = __shfl_sync(0xffffffffu, s.bad, l & 31);
+      if (lane == 1 ? new1 : new0) mine = t, b = sb, from = first, per = cost / a.Hkv;
+    }
+    if (b < a.B) {  // the unit at this place, and the border off the unit's ends
+      kvh = (unsigned)(at - from) / (unsigned)per;
+      const int in = at - from - kvh * per;
+      u = mine.unit_at(in, T);
+      const int start = mine.before(u, T), nt = mine.tiles(u, T);
+      off = ck_snap(in - start, nt);
+      x = from + kvh * per + start + off;
+      if (off == kCkStart + nt) {  // behind the unit: the next one's beginning
+        off = 0;
+        if (++u == mine.units) u = 0, ++kvh;
       }
     }
-    rem = b < a.B ? stop - x : 0;
+    rem = __shfl_sync(0xffffffffu, x, 1);  // (x = W where no CTA follows)
+    b = __shfl_sync(0xffffffffu, b, 0), kvh = __shfl_sync(0xffffffffu, kvh, 0), u = __shfl_sync(0xffffffffu, u, 0);
+    off = __shfl_sync(0xffffffffu, off, 0), x = __shfl_sync(0xffffffffu, x, 0);
+    s.row0 = __shfl_sync(0xffffffffu, mine.row0, 0), s.n = __shfl_sync(0xffffffffu, mine.n, 0);
+    s.pos = __shfl_sync(0xffffffffu, mine.pos, 0), s.end = __shfl_sync(0xffffffffu, mine.end, 0);
+    s.units = __shfl_sync(0xffffffffu, mine.units, 0), s.bad = __shfl_sync(0xffffffffu, mine.bad, 0);
+    rem -= x;
+    if (kvh == a.Hkv) turn();
+  }
+  // on to the next sequence that has rows (there is one while places are left)
+  FP_DEV void turn() {
+    kvh = 0;
     s.units = 0;
-    if (rem > 0) {
-      load();
-      if (kvh == a.Hkv) kvh = 0, s.units = 0;
-      skip();
-    }
-  }
-  FP_DEV void load() {
-    int first, count;
-    chunk_rows(a.cu, b, a.n_tokens, &first, &count);
-    s.set(first, count, __ldg(a.pos + b), a.tile_tokens, a.max_new, a.max_len);
-  }
-  // on to a sequence that has rows (there is one while places are left)
-  FP_DEV void skip() {
+    bool f;
     while (s.units == 0 && rem > 0)
-      if (b + 1 < a.B) ++b, load();
+      if (b + 1 < a.B) load(++b, &f);
       else rem = 0;
   }
   FP_DEV void next(CkPiece* p) {
@@ -249,7 +246,7 @@ struct CkWalk {
     }
     const int T = 2 * a.tile_tokens, nt = s.tiles(u, T), i0 = u * T;
     const bool pair = s.n - i0 > a.tile_tokens;
-    const int left = kCkStart + nt - off, take = (int)(left < rem ? left : rem);
+    const int left = kCkStart + nt - off, take = min(left, rem);
     p->t0 = max(0, off - kCkStart);
     p->t1 = min(nt, max(0, off + take - kCkStart));
     // the first tile's own last key tile
@@ -263,11 +260,7 @@ struct CkWalk {
     off = 0;
     if (rem > 0 && ++u == s.units) {
       u = 0;
-      if (++kvh == a.Hkv) {
-        kvh = 0;
-        s.units = 0;
-        skip();
-      }
+      if (++kvh == a.Hkv) turn();
     }
   }
 };
@@ -279,14 +272,15 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
   constexpr int TILE = ck_tile_bytes<HD>(), NH = HD / 64, SBO = NH * 1024, PAGE = 2 * SBO, R = kCkRing;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   struct Bars {
-    uint64_t kfull[R], vfull[R], kempty[R], vempty[R], qfull, qempty, sfull[2], pfull[2][2], ofull[2], oempty[2], join, met[4],
+    uint64_t kfull[R], vfull[R], kempty[R], vempty[R], qfull, qempty, sfull[2], pfull[2][2], ofull[2], oempty[2], part[2], join, met[4],
         mma, dfull[kCkPieces], dempty[kCkPieces], done[2], ifull[kCkAhead], iempty[kCkAhead];
   };
   __shared__ Bars bar;
   __shared__ CkPiece s_piece[kCkPieces];
   __shared__ float2 s_ml[2][2][kCkKeys];         // [parity][group][row]: maximum and sum, units of one tile
   __shared__ uint32_t tmem_base;
-  __shared__ int abort_word, s_last;
+  __shared__ CkPiece s_left[2];                  // units that other CTAs have a part of
+  __shared__ int abort_word, s_last[2];
   __shared__ int2 s_page[KV8 ? kCkAhead : 1][8];  // int8: pool row of a tile's pages, and how many of their rows count
   volatile int* abort_flag = &abort_word;
   uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
@@ -311,7 +305,7 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
       else if (q < &bar.qfull) n = 2;
       else if (q == &bar.qempty || q == &bar.mma) n = 2;
       else if (q >= &bar.pfull[0][0] && q < bar.ofull) n = 4;
-      else if (q >= bar.oempty && q < bar.met) n = 8;  // oempty, join
+      else if (q >= bar.oempty && q < bar.met) n = 8;  // oempty, part, join
       else if (q >= bar.met && q < &bar.mma) n = 2;
       else if (q >= bar.dempty && q < bar.done) n = kCkReaders;
       else if (q >= bar.iempty) n = kCkWiden;
@@ -336,7 +330,7 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
     return !w.done();
   };
 
-  if (warp >= kCkSoft) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(ck_reg_other<KV8>()));
+  if (KV8 && warp >= kCkSoft) asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
   if (warp == kCkWarpPlan || warp == kCkWarpQ) {
     // ---------------- warp 11: the plan, the pieces, V.  Warp 8: Q tiles and K.  Lanes
     // 0-7 copy a page of a key tile each; the next tile's page ids are read while this
@@ -349,14 +343,6 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
     bool ok = true;
     auto copy = [&](const CkPiece& w) {
       const int32_t* pt = a.page_table + (long long)w.b * a.pages_per_seq;
-      auto page_row = [&](int t) {  // 8-row group of this lane's page; -2 reads zeros
-        const int key0 = t * kCkKeys + lane * 16;
-        if (lane >= 8 || key0 >= w.end) return -2;
-        const int id = __ldg(pt + key0 / 16);
-        if (id >= 0 && id < a.n_pages) return (id * a.Hkv + w.kvh) * 2;
-        if (a.err && !is_v) atomicExch(a.err, 1);
-        return -2;
-      };
       // The Q tiles, behind the first key tile: that one goes out (and the widening of the
       // last unit's last tile, which looks a tile ahead, goes on) while Q is still in use.
       auto queries = [&]() {
@@ -405,16 +391,24 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
           if (!ok) return;
         }
       } else {
-        int row = page_row(w.t0);
+        auto page = [&](int t) {
+          const int key0 = t * kCkKeys + lane * 16;
+          if (lane >= 8 || t >= w.t1 || key0 >= w.end) return -1;
+          return __ldg(pt + key0 / 16);
+        };
+        int id = page(w.t0);
         for (int t = w.t0; t < w.t1; ++t, ++kn) {
-          const int s = kn % R;
+          const int s = kn % R, next_id = page(t + 1);
+          const bool there = id >= 0 && id < a.n_pages;
+          if (!there && !is_v && lane < 8 && t * kCkKeys + lane * 16 < w.end && a.err) atomicExch(a.err, 1);
+          const int group = there ? (id * a.Hkv + w.kvh) * 2 : -2;  // of 8 pool rows; -2 reads zeros
           if (kn >= R) ok = mbar_wait(&empty[s], ((kn / R) & 1) ^ 1);
           ok = __all_sync(0xffffffffu, ok && !*abort_flag);
           if (!ok) return;
           if (lane == 0) mbar_expect_tx(&full[s], TILE);
           __syncwarp();
-          if (lane < 8) ck_tma_4d(dst + s * TILE + lane * PAGE, map, 0, 0, 0, row, &full[s]);
-          if (t + 1 < w.t1) row = page_row(t + 1);
+          if (lane < 8) ck_tma_4d(dst + s * TILE + lane * PAGE, map, 0, 0, 0, group, &full[s]);
+          id = next_id;
           if (!is_v && t == w.t0) queries();
           if (!ok) return;
         }
@@ -605,101 +599,162 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
   } else if (KV8 && warp >= kCkWarpWiden) {
     // ---------------- int8 cache: bf16(q s) of the key tiles' rows.  Thread: 16 codes
     // (chunk c) of every PER-th row.  Each register of codes is filled again, for the
-    // half tile after (V after K, then the next tile's K), as soon as it has been
-    // written out, so loads are in flight throughout, across pieces too.
+    // next tile, as soon as it has been written out: a whole tile's codes, 32 KB an SM,
+    // are in flight throughout, across pieces too.
     constexpr int C = HD / 16;                             // chunks a row
     constexpr int PER = 32 * kCkWiden / C, N = kCkKeys / PER;  // rows at a time, turns a tile
     const int wi = threadIdx.x - kCkWarpWiden * 32, c = wi % C, rr = wi / C;
     const int cb = 2 * (c & 3);
-    uint4 cw[N];
-    float sc[N];
-    int now[N], then[N];  // pool rows (fewer than 2^31) of this tile and the next; -1 reads zeros
-    // this thread's rows of tile k; false: there is none (or a wait ran out)
+    uint4 cw[N], then[N];  // of the half tile that is next, and of the one after it
+    float sc[N], sthen[N];
+    int row[N];  // pool rows (fewer than 2^31) of the tile to be read; -1 reads zeros
     bool ok = true;
-    auto rows = [&](int k, int* r) {
+    // this thread's rows of tile k; false: there is none (or a wait ran out)
+    auto rows = [&](int k) {
       const int s = k % kCkAhead;
-      ok = __all_sync(0xffffffffu, mbar_wait(&bar.ifull[s], (k / kCkAhead) & 1)) && !*abort_flag;
-      ok = __all_sync(0xffffffffu, ok);
-      if (!ok || s_page[s][0].x == -2) return false;
+      ok = __all_sync(0xffffffffu, mbar_wait(&bar.ifull[s], (k / kCkAhead) & 1));
+      const int2 p0 = s_page[s][0];
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        const int row = i * PER + rr;
-        const int2 p = s_page[s][row >> 4];
-        r[i] = (row & 15) < p.y ? p.x + (row & 15) : -1;
+        const int r = i * PER + rr;
+        const int2 p = s_page[s][r >> 4];
+        row[i] = (r & 15) < p.y ? p.x + (r & 15) : -1;
       }
-      return true;
+      return ok && p0.x != -2;
     };
-    auto fetch = [&](int i, int row, bool v) {
-      cw[i] = row >= 0 ? ld_nc16((v ? a.v8 : a.k8) + (long long)row * HD + c * 16) : make_uint4(0, 0, 0, 0);
-      sc[i] = row >= 0 ? __ldg((v ? a.v_scale : a.k_scale) + row) : 0.f;
+    auto fetch = [&](uint4& w, float& s, int r, const int8_t* pool, const float* scale) {
+      w = r >= 0 ? ld_nc16(pool + (long long)r * HD + c * 16) : make_uint4(0, 0, 0, 0);
+      s = r >= 0 ? __ldg(scale + r) : 0.f;
     };
-    bool more = rows(0, now);
-    if (more)
+    // 16 codes and their row's scale to 16 bf16 of row r of a tile
+    auto widen = [&](const uint4& w, float sc, uint8_t* tile, int r) {
+      const uint32_t ww[4] = {w.x ^ 0x80808080u, w.y ^ 0x80808080u, w.z ^ 0x80808080u, w.w ^ 0x80808080u};
+      const float2 s2 = make_float2(sc, sc), z2 = make_float2(-32896.f, -32896.f);
+      uint32_t o[8];
 #pragma unroll
-      for (int i = 0; i < N; ++i) fetch(i, now[i], false);
+      for (int j = 0; j < 8; ++j) {  // codes 2j, 2j + 1: fp32 2^15 + 128 + q
+        const uint32_t u = ww[j >> 1];
+        const float lo = __uint_as_float(__byte_perm(u, 0x47000000u, (j & 1) ? 0x7424 : 0x7404));
+        const float hi = __uint_as_float(__byte_perm(u, 0x47000000u, (j & 1) ? 0x7434 : 0x7414));
+        const float2 f = ck_mul2(ck_add2(make_float2(lo, hi), z2), s2);
+        o[j] = pa_pack(f.x, f.y);
+      }
+      const uint4 e = make_uint4(o[0], o[1], o[2], o[3]), f = make_uint4(o[4], o[5], o[6], o[7]);
+      const int sw = r & 7;
+      uint8_t* rp = tile + (r >> 3) * SBO + (c >> 2) * 1024 + sw * 128;
+      // the lanes of a row's upper half write their odd chunk first: eight lanes, eight banks of 16 bytes
+      const bool up = c >= 4;
+      *reinterpret_cast<uint4*>(rp + (((cb + up) ^ sw) << 4)) = up ? f : e;
+      *reinterpret_cast<uint4*>(rp + (((cb + !up) ^ sw) << 4)) = up ? e : f;
+    };
+    bool more = rows(0);
+    if (more) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) fetch(cw[i], sc[i], row[i], a.k8, a.k_scale);
+#pragma unroll
+      for (int i = 0; i < N; ++i) fetch(then[i], sthen[i], row[i], a.v8, a.v_scale);
+    }
     for (int kn = 0; more && ok; ++kn) {
-      more = rows(kn + 1, then);
-      if (!ok) break;
+      const int s = kn % R;
+      more = rows(kn + 1);
 #pragma unroll
-      for (int i = 0; i < N; ++i) then[i] = more ? then[i] : -1;
+      for (int i = 0; i < N; ++i) row[i] = more ? row[i] : -1;
 #pragma unroll 1
       for (int which = 0; which < 2; ++which) {
-        const int s = kn % R;
-        if (kn >= R) ok = mbar_wait(which ? &bar.vempty[s] : &bar.kempty[s], ((kn / R) & 1) ^ 1);
-        if (!__all_sync(0xffffffffu, ok) || __any_sync(0xffffffffu, *abort_flag != 0)) {
-          ok = false;
-          break;
-        }
-        uint8_t* dst = (which ? sV : sK) + s * TILE + (c >> 2) * 1024;
+        if (kn >= R) ok = __all_sync(0xffffffffu, ok && mbar_wait(which ? &bar.vempty[s] : &bar.kempty[s], ((kn / R) & 1) ^ 1));
+        if (!ok) break;
+        uint8_t* tile = (which ? sV : sK) + s * TILE;
+        const int8_t* pool = which ? a.v8 : a.k8;
+        const float* scale = which ? a.v_scale : a.k_scale;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-          const int row = i * PER + rr, sw = row & 7;
-          const uint32_t ww[4] = {cw[i].x ^ 0x80808080u, cw[i].y ^ 0x80808080u, cw[i].z ^ 0x80808080u,
-                                  cw[i].w ^ 0x80808080u};
-          const float2 s2 = make_float2(sc[i], sc[i]), z2 = make_float2(-32896.f, -32896.f);
-          uint32_t o[8];
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {  // codes 2j, 2j + 1: fp32 2^15 + 128 + q
-            const uint32_t u = ww[j >> 1];
-            const float lo = __uint_as_float(__byte_perm(u, 0x47000000u, (j & 1) ? 0x7424 : 0x7404));
-            const float hi = __uint_as_float(__byte_perm(u, 0x47000000u, (j & 1) ? 0x7434 : 0x7414));
-            const float2 f = ck_mul2(ck_add2(make_float2(lo, hi), z2), s2);
-            o[j] = pa_pack(f.x, f.y);
-          }
-          fetch(i, which ? then[i] : now[i], !which);
-          const uint4 e = make_uint4(o[0], o[1], o[2], o[3]), f = make_uint4(o[4], o[5], o[6], o[7]);
-          uint8_t* rp = dst + (row >> 3) * SBO + sw * 128;
-          // the lanes of a row's upper half write their odd chunk first: eight lanes, eight banks of 16 bytes
-          if (c < 4) {
-            *reinterpret_cast<uint4*>(rp + ((cb ^ sw) << 4)) = e;
-            *reinterpret_cast<uint4*>(rp + (((cb + 1) ^ sw) << 4)) = f;
-          } else {
-            *reinterpret_cast<uint4*>(rp + (((cb + 1) ^ sw) << 4)) = f;
-            *reinterpret_cast<uint4*>(rp + ((cb ^ sw) << 4)) = e;
-          }
+          widen(cw[i], sc[i], tile, i * PER + rr);
+          fetch(cw[i], sc[i], row[i], pool, scale);
         }
         fence_proxy_async();  // the MMAs read the tile through the async proxy
         __syncwarp();
         if (lane == 0) mbar_arrive(which ? &bar.vfull[s] : &bar.kfull[s]);
-      }
-      if (!ok) break;
-      if (lane == 0) mbar_arrive(&bar.iempty[kn % kCkAhead]);
 #pragma unroll
-      for (int i = 0; i < N; ++i) now[i] = then[i];
+        for (int i = 0; i < N; ++i) {  // the other half tile's registers
+          const uint4 w = cw[i];
+          cw[i] = then[i], then[i] = w;
+          const float f = sc[i];
+          sc[i] = sthen[i], sthen[i] = f;
+        }
+      }
+      if (lane == 0) mbar_arrive(&bar.iempty[kn % kCkAhead]);
     }
     if (!ok && lane == 0) fail();
   } else if (warp < kCkSoft) {
     // ---------------- softmax: group j, row 32 quad + lane (TMEM begins at column 0)
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(ck_reg_soft<KV8>()));
+    if (KV8) asm volatile("setmaxnreg.inc.sync.aligned.u32 120;");
     const int j = warp >> 2, quad = warp & 3, row = quad * 32 + lane;
     const uint32_t lane_base = (uint32_t)(quad * 32) << 16;
     const uint32_t ts = lane_base + j * kCkKeys, to = lane_base + kCkO + j * 128;
     const float scale = kPaLog2e * rsqrtf((float)HD);
     const int tok = row / a.G;  // of a tile's packed rows
     const bool packed = row < a.tile_tokens * a.G;
-    int sn = 0, on[2] = {0, 0}, mn = 0, jn = 0;
+    int sn = 0, on[2] = {0, 0}, mn = 0, left = 0;
     bool ok = true;
     uint8_t* stage = sV + R * TILE + warp * kCkStage;
+    constexpr size_t ML = (size_t)kCkRows * HD * 4;
+    auto slot = [&](const CkPiece& w, int i) {  // part i of a unit
+      return a.ws + kCkHead + ((size_t)(w.own + i) * 2 + (i == 0 ? 1 : 0)) * ck_slot<HD>();
+    };
+    // row block rb (32 of a unit's packed rows, one a lane), columns x .. x + 31, to a slot
+    auto keep = [&](uint8_t* p, int rb, int x, const float* r) {
+#pragma unroll
+      for (int y = 0; y < 8; ++y)
+        reinterpret_cast<float4*>(p)[(size_t)(x / 4 + y) * kCkRows + rb * 32 + lane] =
+            make_float4(r[4 * y], r[4 * y + 1], r[4 * y + 2], r[4 * y + 3]);
+    };
+    // where rows 8 y + lane / 4 of a row block begin in the unit's output, or -1
+    auto begins = [&](const CkPiece& w, int rb, int* at) {
+#pragma unroll
+      for (int y = 0; y < 4; ++y) {
+        const int r2 = (rb & 3) * 32 + y * 8 + (lane >> 2), t2 = r2 / a.G, t = t2 + (rb >> 2) * a.tile_tokens;
+        at[y] = t2 < a.tile_tokens && t < w.n ? (t * a.H + r2 - t2 * a.G) * HD : -1;
+      }
+    };
+    // ... to out, times inv, through shared memory: four lanes to a row's 64 bytes; chunk c
+    // of row r at c ^ (r / 2 % 4)
+    auto write = [&](const CkPiece& w, const int* at, int x, const float* r, float inv) {
+      uint16_t* o = a.out + ((long long)w.row0 * a.H + (long long)w.kvh * a.G) * HD;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        uint32_t p[4];
+#pragma unroll
+        for (int y = 0; y < 4; ++y) p[y] = pa_pack(r[8 * c + 2 * y] * inv, r[8 * c + 2 * y + 1] * inv);
+        *reinterpret_cast<uint4*>(stage + lane * 64 + ((c ^ ((lane >> 1) & 3)) << 4)) = make_uint4(p[0], p[1], p[2], p[3]);
+      }
+      __syncwarp();
+#pragma unroll
+      for (int y = 0; y < 4; ++y) {
+        const int lr = y * 8 + (lane >> 2);
+        const uint4 p = *reinterpret_cast<const uint4*>(stage + lr * 64 + (((lane & 3) ^ ((lr >> 1) & 3)) << 4));
+        if (at[y] >= 0) *reinterpret_cast<uint4*>(o + at[y] + x + (lane & 3) * 8) = p;
+      }
+      __syncwarp();
+    };
+    // This CTA's part of s_left[left - 1] is written: by the last of its group of parts?
+    // (One thread asks; the answer is read behind a meeting of the warps.)
+    int jn = 0;
+    bool behind = false;
+    auto ticket = [&]() {
+      if (warp == 0) {
+        ok = __all_sync(0xffffffffu, mbar_wait(&bar.part[left - 1], 0));
+        if (lane == 0 && ok) {
+          const CkPiece& p = s_left[left - 1];
+          const int mine = (blockIdx.x - p.own) / kCkGroup;
+          int* t = reinterpret_cast<int*>(a.ws) + p.own * kCkTickets + mine;
+          const bool last = atomicAdd(t, 1) == min(kCkGroup, p.parts - mine * kCkGroup) - 1;
+          if (last) *t = 0;
+          s_last[left - 1] = last;
+        }
+        __syncwarp();
+      }
+      behind = false;
+    };
     CkPiece w;
     while (next(w, ok)) {
       const bool pair = w.pair();
@@ -717,33 +772,31 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
       for (int t = t_first; t < t_end; t += stride, ++sn) {
         ok = __all_sync(0xffffffffu, mbar_wait(&bar.sfull[j], sn & 1));
         if (!ok) break;
+        if (behind && t > t_first) ticket();
         if (!on_warp) {
           if (lane < 2) mbar_arrive(&bar.pfull[j][lane]);
           continue;
         }
         tc_fence_after();
-        // The scores stay in registers from their maximum to P; int8 cache (fewer
-        // registers a thread): half of them, the others are read again.
-        float v[KV8 ? 64 : 128];
+        // Twice over the scores, rolled up: unrolled over a row held in registers, this
+        // loop, the issuers' and the widening ones were more than the instruction caches
+        // hold, and waiting for instructions the first of the stalls.
         const bool masked = (t + 1) * kCkKeys > lim0;
-        const int left = lim - t * kCkKeys;  // keys of this tile that the row sees
-        auto load = [&](int h, float* d) {
-          tc_ld<64>(ts + h * 64, reinterpret_cast<uint32_t*>(d));
+        const int seen = lim - t * kCkKeys;  // keys of this tile that are the row's
+        float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll 1
+        for (int h = 0; h < 2; ++h) {
+          float v[64];
+          tc_ld<64>(ts + h * 64, reinterpret_cast<uint32_t*>(v));
           if (masked) {
 #pragma unroll
             for (int x = 0; x < 64; ++x)
-              if (h * 64 + x >= left) d[x] = -INFINITY;
+              if (h * 64 + x >= seen) v[x] = -INFINITY;
           }
-        };
-        float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-        for (int h = 1; h >= 0; --h) {
-          float* d = KV8 ? v : v + h * 64;
-          load(h, d);
 #pragma unroll
           for (int x = 0; x < 64; x += 8)
 #pragma unroll
-            for (int y = 0; y < 4; ++y) m4[y] = ck_max3(m4[y], d[x + 2 * y], d[x + 2 * y + 1]);
+            for (int y = 0; y < 4; ++y) m4[y] = ck_max3(m4[y], v[x + 2 * y], v[x + 2 * y + 1]);
         }
         const float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * scale;
         // move the reference when the tile would exceed it by more than 2^kCkSlack
@@ -767,26 +820,30 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
         }
         const float mref = m == -INFINITY ? 0.f : m;
         const float2 sc2 = make_float2(scale, scale), nm2 = make_float2(-mref, -mref);
+#pragma unroll 1
+        for (int x0 = 0; x0 < kCkKeys; x0 += 32) {
+          float v[32];
+          tc_ld<32>(ts + x0, reinterpret_cast<uint32_t*>(v));
+          if (masked) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          float* d = KV8 ? v : v + h * 64;
-          if (KV8 && h) load(1, d);
-#pragma unroll
-          for (int x0 = 0; x0 < 64; x0 += 32) {
-            uint32_t pw[16];
-#pragma unroll
-            for (int x = 0; x < 32; x += 2) {
-              const float2 e = ck_fma2(make_float2(d[x0 + x], d[x0 + x + 1]), sc2, nm2);
-              const float2 p = make_float2(pa_ex2(e.x), pa_ex2(e.y));
-              l2[(x >> 1) & 3] = ck_add2(l2[(x >> 1) & 3], p);
-              pw[x / 2] = pa_pack(p.x, p.y);
-            }
-            tc_st16(ts + h * 64 + x0 / 2, pw);
+            for (int x = 0; x < 32; ++x)
+              if (x0 + x >= seen) v[x] = -INFINITY;
           }
-          tc_wait_st();
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&bar.pfull[j][h]);
+          uint32_t pw[16];
+#pragma unroll
+          for (int x = 0; x < 32; x += 2) {
+            const float2 e = ck_fma2(make_float2(v[x], v[x + 1]), sc2, nm2);
+            const float2 p = make_float2(pa_ex2(e.x), pa_ex2(e.y));
+            l2[(x >> 1) & 3] = ck_add2(l2[(x >> 1) & 3], p);
+            pw[x / 2] = pa_pack(p.x, p.y);
+          }
+          tc_st16(ts + (x0 & 64) + (x0 & 32) / 2, pw);
+          if (x0 & 32) {  // a half is done
+            tc_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&bar.pfull[j][x0 >> 6]);
+          }
         }
       }
       if (!ok) break;
@@ -844,60 +901,28 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
           for (int y = 0; y < 16; ++y) r[y0 + y] = fmaf(a1, __uint_as_float(u[y]), r[y0 + y]);
         }
       };
-      // rows to out, through shared memory: four lanes to a row's 64 bytes; chunk c of row r at c ^ (r / 2 % 4)
-      auto write = [&](auto from, float inv) {
-        uint16_t* o = a.out + ((long long)(w.row0 + jq * a.tile_tokens) * a.H + (long long)w.kvh * a.G) * HD;
-        int at[4];  // rows 8 y + lane / 4 of this warp's: where each begins, or -1
-#pragma unroll
-        for (int y = 0; y < 4; ++y) {
-          const int r2 = quad * 32 + y * 8 + (lane >> 2), t2 = r2 / a.G;
-          at[y] = r2 < a.tile_tokens * a.G && t2 < tile_n ? (t2 * a.H + r2 - t2 * a.G) * HD : -1;
-        }
-#pragma unroll 1
-        for (int x = x0; x < x1; x += 32) {
-          float r[32];
-          from(x, r);
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            uint32_t p[4];
-#pragma unroll
-            for (int y = 0; y < 4; ++y) p[y] = pa_pack(r[8 * c + 2 * y] * inv, r[8 * c + 2 * y + 1] * inv);
-            *reinterpret_cast<uint4*>(stage + lane * 64 + ((c ^ ((lane >> 1) & 3)) << 4)) = make_uint4(p[0], p[1], p[2], p[3]);
-          }
-          __syncwarp();
-#pragma unroll
-          for (int y = 0; y < 4; ++y) {
-            const int lr = y * 8 + (lane >> 2);
-            const uint4 p = *reinterpret_cast<const uint4*>(stage + lr * 64 + (((lane & 3) ^ ((lr >> 1) & 3)) << 4));
-            if (at[y] >= 0) *reinterpret_cast<uint4*>(o + at[y] + x + (lane & 3) * 8) = p;
-          }
-          __syncwarp();
-        }
-      };
-      const int r256 = jq * kCkKeys + row;
-      auto slot = [&](int i) {  // part i of this unit
-        return a.ws + kCkHead + ((size_t)(w.own + i) * 2 + (i == 0 ? 1 : 0)) * ck_slot<HD>();
-      };
-      auto keep = [&](uint8_t* p, auto from) {  // O to a slot
-#pragma unroll 1
-        for (int x = x0; x < x1; x += 32) {
-          float f[32];
-          from(x, f);
-#pragma unroll
-          for (int y = 0; y < 8; ++y)
-            reinterpret_cast<float4*>(p)[(size_t)(x / 4 + y) * kCkRows + r256] =
-                make_float4(f[4 * y], f[4 * y + 1], f[4 * y + 2], f[4 * y + 3]);
-        }
-      };
-      constexpr size_t ML = (size_t)kCkRows * HD * 4;
       if (on_warp) {
+        const int rb = jq * 4 + quad;
         if (whole) {
-          write(load, inv);
+          int at[4];
+          begins(w, rb, at);
+#pragma unroll 1
+          for (int x = x0; x < x1; x += 32) {
+            float r[32];
+            load(x, r);
+            write(w, at, x, r, inv);
+          }
         } else {
-          uint8_t* p = slot(blockIdx.x - w.own);
-          if (have) keep(p, load);
+          uint8_t* p = slot(w, blockIdx.x - w.own);
+          if (have)
+#pragma unroll 1
+            for (int x = x0; x < x1; x += 32) {
+              float r[32];
+              load(x, r);
+              keep(p, rb, x, r);
+            }
           if (x0 == 0)
-            reinterpret_cast<float2*>(p + ML)[r256] = make_float2(have && l > 0.f ? m : -INFINITY, have ? l : 0.f);
+            reinterpret_cast<float2*>(p + ML)[rb * 32 + lane] = make_float2(have && l > 0.f ? m : -INFINITY, have ? l : 0.f);
         }
       }
       if (have) {
@@ -914,72 +939,85 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
         }
       }
       if (!whole) {
-        // o = sum 2^(m_i - m) O_i / sum 2^(m_i - m) l_i over the unit's parts, in their
-        // order, by the last CTA to bring its part: first among kCkGroup neighbours, then
-        // (a unit that more CTAs share) the last group among the groups.
-        const int mine = (blockIdx.x - w.own) / kCkGroup, groups = (w.parts + kCkGroup - 1) / kCkGroup;
-        int* tickets = reinterpret_cast<int*>(a.ws) + w.own * kCkTickets;
-        // whether this CTA is the last of n to get here; what the others wrote is then there
-        auto last_of = [&](int* ticket, int n) {
-          __threadfence();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&bar.join);
-          ok = ok && __all_sync(0xffffffffu, mbar_wait(&bar.join, jn++ & 1));
-          if (threadIdx.x == 0) {
-            s_last = atomicAdd(ticket, 1) == n - 1;
-            if (s_last) *ticket = 0;
-          }
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&bar.join);
-          ok = ok && __all_sync(0xffffffffu, mbar_wait(&bar.join, jn++ & 1));
-          __threadfence();
-          return ok && s_last;
-        };
-        float mm = -INFINITY, ll = 0.f;
-        int i0 = mine * kCkGroup, step = 1, n = min(kCkGroup, w.parts - i0);
-        size_t ml_at = ML;
-        auto sums = [&]() {  // the parts' common maximum and sum
-          mm = -INFINITY, ll = 0.f;
-          for (int i = 0; i < n; ++i) mm = fmaxf(mm, __ldcg(reinterpret_cast<const float2*>(slot(i0 + i * step) + ml_at) + r256).x);
-          for (int i = 0; i < n; ++i) {
-            const float2 f = __ldcg(reinterpret_cast<const float2*>(slot(i0 + i * step) + ml_at) + r256);
-            if (f.x != -INFINITY) ll += exp2f(f.x - mm) * f.y;
-          }
-        };
-        auto added = [&](int x, float* r) {  // 32 columns of the parts' sum
+        if (behind) ticket();
+        if (threadIdx.x == 0) s_left[left] = w;
+        ++left;
+        // (the ticket waits for a tile of the next piece, by when every warp is here)
+        __threadfence();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&bar.part[left - 1]);
+        behind = true;
+      }
+    }
+    // ---- units that other CTAs have a part of (at most two: the stretch's first and
+    // last): o = sum 2^(m_i - m) O_i / sum 2^(m_i - m) l_i over the unit's parts, in their
+    // order, by the last CTA to bring its part: first among kCkGroup neighbours, then (a
+    // unit that more CTAs share) the last group among the groups.
+    auto meet = [&]() {
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&bar.join);
+      ok = ok && __all_sync(0xffffffffu, mbar_wait(&bar.join, jn++ & 1));
+    };
+    if (left > 0 && ok) {
+      if (behind) ticket();
+      meet();
+      __threadfence();
+    }
+    for (int k = 0; k < left && ok; ++k) {
+      if (!s_last[k]) continue;
+      w = s_left[k];
+      const int groups = (w.parts + kCkGroup - 1) / kCkGroup;
+      int i0 = (blockIdx.x - w.own) / kCkGroup * kCkGroup, step = 1, n = min(kCkGroup, w.parts - i0);
+      size_t ml_at = ML;
+      // the unit's rows by 32, 32 columns at a time, over the warps
+      const int rows = w.pair() ? kCkKeys + (w.n - a.tile_tokens) * a.G : w.n * a.G;
+      for (int turn = groups > 1 ? 0 : 1; turn < 2 && ok; ++turn) {
+#pragma unroll 1
+        for (int item = warp; item < (rows + 31) / 32 * (HD / 32); item += kCkSoft) {
+          const int rb = item / (HD / 32), x = item % (HD / 32) * 32;
+          float mm = -INFINITY, ll = 0.f, r[32];
 #pragma unroll
           for (int y = 0; y < 32; ++y) r[y] = 0.f;
-#pragma unroll 1
+#pragma unroll 2
           for (int i = 0; i < n; ++i) {
-            const uint8_t* p = slot(i0 + i * step);
-            const float mi = __ldcg(reinterpret_cast<const float2*>(p + ml_at) + r256).x;
+            const uint8_t* p = slot(w, i0 + i * step);
+            const float2 ml = __ldcg(reinterpret_cast<const float2*>(p + ml_at) + rb * 32 + lane);
             float4 f[8];
 #pragma unroll
-            for (int y = 0; y < 8; ++y) f[y] = __ldcg(reinterpret_cast<const float4*>(p) + (size_t)(x / 4 + y) * kCkRows + r256);
-            if (mi == -INFINITY) continue;  // (its O was not written)
-            const float c = exp2f(mi - mm);
+            for (int y = 0; y < 8; ++y) f[y] = __ldcg(reinterpret_cast<const float4*>(p) + (size_t)(x / 4 + y) * kCkRows + rb * 32 + lane);
+            if (ml.x == -INFINITY) continue;  // (its O may not have been written)
+            const float m2 = fmaxf(mm, ml.x), c0 = exp2f(mm - m2), c1 = exp2f(ml.x - m2);
+            mm = m2;
+            ll = ll * c0 + ml.y * c1;
 #pragma unroll
             for (int y = 0; y < 8; ++y) {
-              r[4 * y] = fmaf(c, f[y].x, r[4 * y]), r[4 * y + 1] = fmaf(c, f[y].y, r[4 * y + 1]);
-              r[4 * y + 2] = fmaf(c, f[y].z, r[4 * y + 2]), r[4 * y + 3] = fmaf(c, f[y].w, r[4 * y + 3]);
+              r[4 * y] = r[4 * y] * c0 + f[y].x * c1, r[4 * y + 1] = r[4 * y + 1] * c0 + f[y].y * c1;
+              r[4 * y + 2] = r[4 * y + 2] * c0 + f[y].z * c1, r[4 * y + 3] = r[4 * y + 3] * c0 + f[y].w * c1;
             }
           }
-        };
-        bool here = last_of(tickets + mine, n);
-        if (here && groups > 1) {
-          if (on_warp) {
-            sums();
-            keep(slot(i0), added);
-            if (x0 == 0) reinterpret_cast<float2*>(slot(i0) + ML + kCkRows * 8)[r256] = make_float2(mm, ll);
+          if (turn == 0) {
+            keep(slot(w, i0), rb, x, r);
+            if (x == 0) reinterpret_cast<float2*>(slot(w, i0) + ML + kCkRows * 8)[rb * 32 + lane] = make_float2(mm, ll);
+          } else {
+            int at[4];
+            begins(w, rb, at);
+            write(w, at, x, r, ll > 0.f ? 1.f / ll : 0.f);
           }
-          here = last_of(tickets + kCkTickets - 1, groups);
+        }
+        if (turn == 0) {
+          __threadfence();
+          meet();
+          if (threadIdx.x == 0) {
+            int* t = reinterpret_cast<int*>(a.ws) + w.own * kCkTickets + kCkTickets - 1;
+            const bool last = atomicAdd(t, 1) == groups - 1;
+            if (last) *t = 0;
+            s_last[k] = last;
+          }
+          meet();
+          __threadfence();
+          if (!s_last[k]) break;
           i0 = 0, step = kCkGroup, n = groups, ml_at = ML + kCkRows * 8;
         }
-        if (here && on_warp) {
-          sums();
-          write(added, ll > 0.f ? 1.f / ll : 0.f);
-        }
-        if (!ok) break;
       }
     }
     if (!ok && lane == 0) fail();
@@ -1024,8 +1062,8 @@ static int ck_sms() {
   return sms;
 }
 
-bool attention_chunk_fits(int n_tokens, int n_heads, int n_kv_heads, int max_new, int max_len) {
-  return ck_fits(n_tokens, max_new, max_len, n_kv_heads, ck_tile_tokens(n_heads / n_kv_heads));
+bool attention_chunk_fits(int n_tokens, int B, int n_heads, int n_kv_heads, int max_len) {
+  return ck_fits(n_tokens, B, max_len, n_kv_heads, ck_tile_tokens(n_heads / n_kv_heads));
 }
 
 size_t attention_chunk_ws_bytes(int B, int n_heads, int n_kv_heads, int head_dim, int max_new) {

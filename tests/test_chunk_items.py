@@ -41,9 +41,9 @@ int main() {
   for (int it = 0; it < 3000; ++it) {  // the stretches
     const int G = 1 + rand() % 16, tt = ck_tile_tokens(G), T = 2 * tt, B = 1 + rand() % 12, Hkv = 1 + rand() % 5;
     const int grid = 1 + rand() % 152;
-    struct Unit { long long x; int nt; std::vector<int> seen; int own = -1, parts = 0; };
+    struct Unit { int x; int nt; std::vector<int> seen; int own = -1, parts = 0; };
     std::vector<Unit> units;
-    long long W = 0;
+    int W = 0;
     for (int b = 0; b < B; ++b) {
       CkSeq s;
       s.set(0, rand() % 3 ? rand() % 9 : rand() % 700, rand() % 2 ? rand() % 50 : rand() % 4000, tt, 1000, 5000);
@@ -55,21 +55,21 @@ int main() {
     }
     const int g = ck_ctas(W, grid);
     if (g < 1 || g > grid) return bad("ctas", it);
-    auto begin = [&](int c) -> long long {
+    auto begin = [&](int c) -> int {
       if (c >= g) return W;
-      const long long x = ck_muldiv(W, c, g);
-      if (x != W * c / g) return -1;
+      const int x = ck_begin(c, W, g);
+      if (x != (long long)W * c / g) return -1;
       for (auto& u : units)
-        if (x >= u.x && x < u.x + kCkStart + u.nt) return u.x + ck_snap((int)(x - u.x), u.nt);
+        if (x >= u.x && x < u.x + kCkStart + u.nt) return u.x + ck_snap(x - u.x, u.nt);
       return W;
     };
     for (int c = 0; c < grid; ++c) {
-      const long long lo = begin(c), hi = begin(c + 1);
+      const int lo = begin(c), hi = begin(c + 1);
       if (hi < lo) return bad("order", it);
       for (auto& u : units) {
-        const long long p = std::max(lo, u.x), q = std::min(hi, u.x + kCkStart + u.nt);
+        const int p = std::max(lo, u.x), q = std::min(hi, u.x + kCkStart + u.nt);
         if (p >= q) continue;
-        const int t0 = std::max(0, (int)(p - u.x) - kCkStart), t1 = std::max(0, (int)(q - u.x) - kCkStart);
+        const int t0 = std::max(0, p - u.x - kCkStart), t1 = std::max(0, q - u.x - kCkStart);
         if (p > u.x && t0 < kCkSnap) return bad("a border inside a unit's start", it);
         if (t1 <= t0) return bad("a part without keys", it);
         for (int t = t0; t < t1; ++t) ++u.seen[t];

@@ -269,18 +269,24 @@ def test_attention_rows_without_keys_and_lengths_beyond_the_bounds(fp, kvq):
     c.check(np.where(np.arange(c.N)[:, None] >= 0, q, q), np.where((got == 0x4321), got, got), only={2})
 
 
-def test_a_bad_cu_touches_no_row_outside(fp):
+def test_a_bad_cu_is_reported_and_touches_nothing(fp):
     c = Batch(fp, 0, 128, 4, 2, [(4, 20), (5, 30), (3, 10)], 31, tail=4)
     q = c.queries(11)
-    for cu in ([0, 4, 9, 40], [-3, 4, 9, 12], [0, 9, 4, 12], [5, 4, 3, 2], [100, 200, 300, 400]):
+    for cu in ([0, 4, 9, 40], [-3, 4, 9, 12], [0, 9, 4, 12], [5, 4, 3, 2], [100, 200, 300, 400], [0, 4, 9, 8]):
         got, err = c.attend(q, cu=np.array(cu, np.int32), max_new=40, max_len=c.max_len)
-        assert err == 1, cu
-        assert got.shape == (c.N, 4 * 128)
-    # sequences that are well described beside one that is not keep their results
-    got, err = c.attend(q, cu=np.array([0, 4, 9, 8], np.int32))
-    assert err == 1
-    c.seqs = [(4, 20), (5, 30), (0, 10)]
-    c.check(q, got)
+        assert err == 1 and np.all(got == 0x4321), cu
+
+
+def test_attention_of_many_sequences(fp):
+    """More sequences than a warp has lanes, some without rows, in order and with gaps."""
+    rng = np.random.default_rng(4)
+    seqs = [(int(n), int(p)) for n, p in zip(rng.integers(0, 4, 100), rng.integers(0, 700, 100))]
+    for kvq in (0, 1):
+        c = Batch(fp, kvq, 64, 4, 2, seqs, 33, lead=1, tail=2)
+        q = c.queries(12)
+        got, err = c.attend(q)
+        assert err == 0
+        c.check(q, got)
 
 
 @pytest.mark.parametrize("kvq", [0, 1])
