@@ -461,9 +461,9 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
     }
   } else if (warp == kCkWarpMma || warp == kCkWarpMma + 1) {
     // ---------------- MMA issuers, a group each: every lane runs the loop, one issues.
-    // The group and the ring slot are constants of the code that issues, and an
-    // allocation of all 512 columns begins at column 0, so no operand has to be
-    // moved to a uniform register MMA by MMA.
+    // The group is a constant of the code that issues, the ring slot comes from a vote, and
+    // an allocation of all 512 columns begins at column 0, so no operand has to be moved
+    // to a uniform register MMA by MMA.
     if (warp == kCkWarpMma) {
       asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base)),
                    "r"(kCkTmemCols)
@@ -478,37 +478,24 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
                      vd = ck_sdesc_mn(smem_u32(sV), 1024, SBO);
       int n = 0, kn = 0, pn = 0, on = 0;
       bool ok = true;
+      // A vote's result is in a uniform register, and so is all that follows from it.
+      auto uniform = [](bool b) { return __any_sync(0xffffffffu, b) ? 1 : 0; };
       // S_j = Q K^T of ring slot s (descriptor start addresses count 16-byte units)
-      auto scores_of = [&](auto cq, auto cs) {
-        constexpr int q = decltype(cq)::value, s = decltype(cs)::value;
+      auto scores = [&](int q, int s) {
+        const uint64_t qs = qd + q * (TILE >> 4), ks = kd + s * (TILE >> 4);
+#pragma unroll 1
+        for (int h = 0; h < NH; ++h)
 #pragma unroll
-        for (int kk = 0; kk < HD / 16; ++kk)
-          tc_mma(j * kCkKeys, qd + ((q * TILE + (kk >> 2) * (TILE / NH) + (kk & 3) * 32) >> 4),
-                 kd + ((s * TILE + (kk >> 2) * 1024 + (kk & 3) * 32) >> 4), idesc_s, kk > 0 ? 1u : 0u);
+          for (int kk = 0; kk < 4; ++kk)
+            tc_mma(j * kCkKeys, qs + h * (TILE / NH >> 4) + kk * 2, ks + h * (1024 >> 4) + kk * 2, idesc_s, h + kk > 0 ? 1u : 0u);
         tc_commit(&bar.sfull[j]);
       };
-      constexpr std::integral_constant<int, 0> c0;
-      constexpr std::integral_constant<int, 1> c1;
-      static_assert(R == 2, "two ring slots");
-      auto scores = [&](bool pair, int s) {
-        if (j && pair) {
-          if (s) scores_of(c1, c1);
-          else scores_of(c1, c0);
-        } else {
-          if (s) scores_of(c0, c1);
-          else scores_of(c0, c0);
-        }
-      };
       // O_j (+)= P_j V of ring slot s, half h of the keys: a page a step
-      auto values_of = [&](auto cs, auto ch, bool first) {
-        constexpr int s = decltype(cs)::value, h = decltype(ch)::value;
-        auto one = [&](int kk, uint32_t add) {
-          tc_mma_ts(kCkO + j * 128, j * kCkKeys + h * 64 + kk * 8, vd + ((s * TILE + (h * 4 + kk) * PAGE) >> 4), idesc_o, add);
-        };
-        if (h == 0 && first) one(0, 0);
-        else one(0, 1);
+      auto values = [&](int s, int h, bool first) {
+        const uint64_t vs = vd + s * (TILE >> 4) + h * (4 * PAGE >> 4);
 #pragma unroll
-        for (int kk = 1; kk < 4; ++kk) one(kk, 1);
+        for (int kk = 0; kk < 4; ++kk)
+          tc_mma_ts(kCkO + j * 128, j * kCkKeys + h * 64 + kk * 8, vs + kk * (PAGE >> 4), idesc_o, kk > 0 || !first ? 1u : 0u);
       };
       CkPiece w;
       while (next(w, ok)) {
@@ -532,9 +519,11 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
         ++n;
         tc_fence_after();
         const bool q_alone = pair ? j == 1 && w.e0 <= w.t0 : steps == 1;  // the other group has no scores here
+        const int q = uniform(j && pair);
         if (i0 < i1) {
+          const int u = uniform((kn + i0) & 1);
           if (elect_one()) {
-            scores(pair, (kn + i0) % R);
+            scores(q, u);
             release(&bar.kempty[(kn + i0) % R], alone(i0));
             if (i0 + di >= i1) release(&bar.qempty, q_alone);
           }
@@ -562,21 +551,19 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
           ok = __all_sync(0xffffffffu, ok);
           if (!ok) break;
           tc_fence_after();
-          if (elect_one()) {
-            if (s) values_of(c1, c0, i == i0);
-            else values_of(c0, c0, i == i0);
-          }
+          const int u = uniform(s), first = uniform(i == i0);
+          if (elect_one()) values(u, 0, first);
           __syncwarp();
           ok = __all_sync(0xffffffffu, mbar_wait(&bar.pfull[j][1], pn & 1));
           if (!ok) break;
           ++pn;
           tc_fence_after();
+          const int u1 = uniform(s1);
           if (elect_one()) {
-            if (s) values_of(c1, c1, false);
-            else values_of(c0, c1, false);
+            values(u, 1, false);
             release(&bar.vempty[s], alone(i));
             if (more) {
-              scores(pair, s1);
+              scores(q, u1);
               release(&bar.kempty[s1], alone(i + di));
               if (i + 2 * di >= i1) release(&bar.qempty, q_alone);
             } else {
