@@ -301,7 +301,7 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
     for (int i = threadIdx.x; i < NB; i += ck_threads<KV8>()) {
       const uint64_t* q = p + i;
       int n = 1;
-      if (q < bar.kempty) n = KV8 ? kCkWiden : 1;
+      if (q < bar.kempty) n = KV8 ? kCkWiden / 2 : 1;
       else if (q < &bar.qfull) n = 2;
       else if (q == &bar.qempty || q == &bar.mma) n = 2;
       else if (q >= &bar.pfull[0][0] && q < bar.ofull) n = 4;
@@ -584,92 +584,74 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
     if (warp == kCkWarpMma) role(std::integral_constant<int, 0>());
     else role(std::integral_constant<int, 1>());
   } else if (KV8 && warp >= kCkWarpWiden) {
-    // ---------------- int8 cache: bf16(q s) of the key tiles' rows.  Thread: 16 codes
-    // (chunk c) of every PER-th row.  Each register of codes is filled again, for the
-    // next tile, as soon as it has been written out: a whole tile's codes, 32 KB an SM,
-    // are in flight throughout, across pieces too.
-    constexpr int C = HD / 16;                             // chunks a row
-    constexpr int PER = 32 * kCkWiden / C, N = kCkKeys / PER;  // rows at a time, turns a tile
-    const int wi = threadIdx.x - kCkWarpWiden * 32, c = wi % C, rr = wi / C;
-    const int cb = 2 * (c & 3);
-    uint4 cw[N], then[N];  // of the half tile that is next, and of the one after it
-    float sc[N], sthen[N];
+    // ---------------- int8 cache: bf16(q s) of the key tiles' rows, four warps for K and
+    // four for V.  Thread: 16 codes (chunk c) of every PER-th row.  Each register of codes
+    // is filled again, for the next tile, as soon as it has been written out: a whole
+    // tile's codes, 32 KB an SM, are in flight throughout, across pieces too.
+    constexpr int C = HD / 16;                                      // chunks a row
+    constexpr int PER = 16 * kCkWiden / C, N = kCkKeys / PER;       // rows at a time, turns a tile
+    const bool is_v = warp >= kCkWarpWiden + kCkWiden / 2;
+    // four chunks of two rows go out at a time, whose swizzles differ: eight banks of 16 bytes
+    const int wi = threadIdx.x % (16 * kCkWiden), c = C == 4 ? wi & 3 : (wi & 3) | (wi >> 1 & 4);
+    const int rr = C == 4 ? wi >> 2 : (wi >> 4) * 2 + (wi >> 2 & 1);
+    const int8_t* pool = (is_v ? a.v8 : a.k8) + c * 16;
+    const float* scale = is_v ? a.v_scale : a.k_scale;
+    uint64_t *full = is_v ? bar.vfull : bar.kfull, *empty = is_v ? bar.vempty : bar.kempty;
+    uint8_t* tiles = (is_v ? sV : sK) + (rr >> 3) * SBO + (c >> 2) * 1024 + (rr & 7) * 128;
+    const int o0 = ((2 * (c & 3)) ^ (rr & 7)) << 4, o1 = ((2 * (c & 3) + 1) ^ (rr & 7)) << 4;
+    uint4 cw[N];
+    float sc[N];
     int row[N];  // pool rows (fewer than 2^31) of the tile to be read; -1 reads zeros
     bool ok = true;
     // this thread's rows of tile k; false: there is none (or a wait ran out)
     auto rows = [&](int k) {
       const int s = k % kCkAhead;
       ok = __all_sync(0xffffffffu, mbar_wait(&bar.ifull[s], (k / kCkAhead) & 1));
-      const int2 p0 = s_page[s][0];
+      const bool there = ok && s_page[s][0].x != -2;
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         const int r = i * PER + rr;
         const int2 p = s_page[s][r >> 4];
-        row[i] = (r & 15) < p.y ? p.x + (r & 15) : -1;
+        row[i] = there && (r & 15) < p.y ? p.x + (r & 15) : -1;
       }
-      return ok && p0.x != -2;
+      return there;
     };
-    auto fetch = [&](uint4& w, float& s, int r, const int8_t* pool, const float* scale) {
-      w = r >= 0 ? ld_nc16(pool + (long long)r * HD + c * 16) : make_uint4(0, 0, 0, 0);
-      s = r >= 0 ? __ldg(scale + r) : 0.f;
-    };
-    // 16 codes and their row's scale to 16 bf16 of row r of a tile
-    auto widen = [&](const uint4& w, float sc, uint8_t* tile, int r) {
-      const uint32_t ww[4] = {w.x ^ 0x80808080u, w.y ^ 0x80808080u, w.z ^ 0x80808080u, w.w ^ 0x80808080u};
-      const float2 s2 = make_float2(sc, sc), z2 = make_float2(-32896.f, -32896.f);
-      uint32_t o[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {  // codes 2j, 2j + 1: fp32 2^15 + 128 + q
-        const uint32_t u = ww[j >> 1];
-        const float lo = __uint_as_float(__byte_perm(u, 0x47000000u, (j & 1) ? 0x7424 : 0x7404));
-        const float hi = __uint_as_float(__byte_perm(u, 0x47000000u, (j & 1) ? 0x7434 : 0x7414));
-        const float2 f = ck_mul2(ck_add2(make_float2(lo, hi), z2), s2);
-        o[j] = pa_pack(f.x, f.y);
-      }
-      const uint4 e = make_uint4(o[0], o[1], o[2], o[3]), f = make_uint4(o[4], o[5], o[6], o[7]);
-      const int sw = r & 7;
-      uint8_t* rp = tile + (r >> 3) * SBO + (c >> 2) * 1024 + sw * 128;
-      // the lanes of a row's upper half write their odd chunk first: eight lanes, eight banks of 16 bytes
-      const bool up = c >= 4;
-      *reinterpret_cast<uint4*>(rp + (((cb + up) ^ sw) << 4)) = up ? f : e;
-      *reinterpret_cast<uint4*>(rp + (((cb + !up) ^ sw) << 4)) = up ? e : f;
+    auto fetch = [&](int i) {
+      cw[i] = row[i] >= 0 ? ld_nc16(pool + (long long)row[i] * HD) : make_uint4(0, 0, 0, 0);
+      sc[i] = row[i] >= 0 ? __ldg(scale + row[i]) : 0.f;
     };
     bool more = rows(0);
-    if (more) {
 #pragma unroll
-      for (int i = 0; i < N; ++i) fetch(cw[i], sc[i], row[i], a.k8, a.k_scale);
-#pragma unroll
-      for (int i = 0; i < N; ++i) fetch(then[i], sthen[i], row[i], a.v8, a.v_scale);
-    }
-    for (int kn = 0; more && ok; ++kn) {
+    for (int i = 0; i < N; ++i) fetch(i);
+    for (int kn = 0; more; ++kn) {
       const int s = kn % R;
       more = rows(kn + 1);
+      if (kn >= R) ok = __all_sync(0xffffffffu, ok && mbar_wait(&empty[s], ((kn / R) & 1) ^ 1));
+      if (!ok) break;
 #pragma unroll
-      for (int i = 0; i < N; ++i) row[i] = more ? row[i] : -1;
-#pragma unroll 1
-      for (int which = 0; which < 2; ++which) {
-        if (kn >= R) ok = __all_sync(0xffffffffu, ok && mbar_wait(which ? &bar.vempty[s] : &bar.kempty[s], ((kn / R) & 1) ^ 1));
-        if (!ok) break;
-        uint8_t* tile = (which ? sV : sK) + s * TILE;
-        const int8_t* pool = which ? a.v8 : a.k8;
-        const float* scale = which ? a.v_scale : a.k_scale;
+      for (int i = 0; i < N; ++i) {
+        const uint32_t ww[4] = {cw[i].x ^ 0x80808080u, cw[i].y ^ 0x80808080u, cw[i].z ^ 0x80808080u, cw[i].w ^ 0x80808080u};
+        const float2 s2 = make_float2(sc[i], sc[i]), z2 = make_float2(-32896.f, -32896.f);
+        uint32_t o[8];
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-          widen(cw[i], sc[i], tile, i * PER + rr);
-          fetch(cw[i], sc[i], row[i], pool, scale);
+        for (int j = 0; j < 8; ++j) {  // codes 2j, 2j + 1: fp32 2^15 + 128 + q
+          const uint32_t u = ww[j >> 1];
+          const float lo = __uint_as_float(__byte_perm(u, 0x47000000u, (j & 1) ? 0x7424 : 0x7404));
+          const float hi = __uint_as_float(__byte_perm(u, 0x47000000u, (j & 1) ? 0x7434 : 0x7414));
+          const float2 f = ck_mul2(ck_add2(make_float2(lo, hi), z2), s2);
+          o[j] = pa_pack(f.x, f.y);
         }
-        fence_proxy_async();  // the MMAs read the tile through the async proxy
-        __syncwarp();
-        if (lane == 0) mbar_arrive(which ? &bar.vfull[s] : &bar.kfull[s]);
-#pragma unroll
-        for (int i = 0; i < N; ++i) {  // the other half tile's registers
-          const uint4 w = cw[i];
-          cw[i] = then[i], then[i] = w;
-          const float f = sc[i];
-          sc[i] = sthen[i], sthen[i] = f;
-        }
+        uint8_t* rp = tiles + s * TILE + i * (PER / 8 * SBO);
+        *reinterpret_cast<uint4*>(rp + o0) = make_uint4(o[0], o[1], o[2], o[3]);
+        *reinterpret_cast<uint4*>(rp + o1) = make_uint4(o[4], o[5], o[6], o[7]);
+        fetch(i);
       }
-      if (lane == 0) mbar_arrive(&bar.iempty[kn % kCkAhead]);
+      fence_proxy_async();  // the MMAs read the tile through the async proxy
+      __syncwarp();
+      if (lane == 0) {
+        mbar_arrive(&full[s]);
+        mbar_arrive(&bar.iempty[kn % kCkAhead]);
+      }
     }
     if (!ok && lane == 0) fail();
   } else if (warp < kCkSoft) {
