@@ -753,19 +753,25 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
         const bool masked = (t + 1) * kCkKeys > lim0;
         const int seen = lim - t * kCkKeys;  // keys of this tile that are the row's
         float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll 1
-        for (int h = 0; h < 2; ++h) {
-          float v[64];
-          tc_ld<64>(ts + h * 64, reinterpret_cast<uint32_t*>(v));
-          if (masked) {
+        auto maximum = [&](auto cut, int x0) {
+          float v[32];
+          tc_ld<32>(ts + x0, reinterpret_cast<uint32_t*>(v));
+          if constexpr (decltype(cut)::value) {
 #pragma unroll
-            for (int x = 0; x < 64; ++x)
-              if (h * 64 + x >= seen) v[x] = -INFINITY;
+            for (int x = 0; x < 32; ++x)
+              if (x0 + x >= seen) v[x] = -INFINITY;
           }
 #pragma unroll
-          for (int x = 0; x < 64; x += 8)
+          for (int x = 0; x < 32; x += 8)
 #pragma unroll
             for (int y = 0; y < 4; ++y) m4[y] = ck_max3(m4[y], v[x + 2 * y], v[x + 2 * y + 1]);
+        };
+        if (masked) {
+#pragma unroll 1
+          for (int x0 = 0; x0 < kCkKeys; x0 += 32) maximum(std::true_type(), x0);
+        } else {
+#pragma unroll 1
+          for (int x0 = 0; x0 < kCkKeys; x0 += 32) maximum(std::false_type(), x0);
         }
         const float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * scale;
         // move the reference when the tile would exceed it by more than 2^kCkSlack
@@ -789,30 +795,39 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
         }
         const float mref = m == -INFINITY ? 0.f : m;
         const float2 sc2 = make_float2(scale, scale), nm2 = make_float2(-mref, -mref);
-#pragma unroll 1
-        for (int x0 = 0; x0 < kCkKeys; x0 += 32) {
+        auto weights = [&](auto cut, int x0) {  // P of 32 keys
           float v[32];
           tc_ld<32>(ts + x0, reinterpret_cast<uint32_t*>(v));
-          if (masked) {
+          if constexpr (decltype(cut)::value) {
 #pragma unroll
             for (int x = 0; x < 32; ++x)
               if (x0 + x >= seen) v[x] = -INFINITY;
           }
-          uint32_t pw[16];
 #pragma unroll
-          for (int x = 0; x < 32; x += 2) {
-            const float2 e = ck_fma2(make_float2(v[x], v[x + 1]), sc2, nm2);
-            const float2 p = make_float2(pa_ex2(e.x), pa_ex2(e.y));
-            l2[(x >> 1) & 3] = ck_add2(l2[(x >> 1) & 3], p);
-            pw[x / 2] = pa_pack(p.x, p.y);
+          for (int y = 0; y < 32; y += 32) {
+            uint32_t pw[16];
+#pragma unroll
+            for (int x = 0; x < 32; x += 2) {
+              const float2 e = ck_fma2(make_float2(v[y + x], v[y + x + 1]), sc2, nm2);
+              const float2 p = make_float2(pa_ex2(e.x), pa_ex2(e.y));
+              l2[(x >> 1) & 3] = ck_add2(l2[(x >> 1) & 3], p);
+              pw[x / 2] = pa_pack(p.x, p.y);
+            }
+            tc_st16(ts + (x0 & 64) + ((x0 + y) & 32) / 2, pw);
           }
-          tc_st16(ts + (x0 & 64) + (x0 & 32) / 2, pw);
-          if (x0 & 32) {  // a half is done
+          if ((x0 + 32) % 64 == 0) {  // a half is done
             tc_wait_st();
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(&bar.pfull[j][x0 >> 6]);
           }
+        };
+        if (masked) {
+#pragma unroll 1
+          for (int x0 = 0; x0 < kCkKeys; x0 += 32) weights(std::true_type(), x0);
+        } else {
+#pragma unroll 1
+          for (int x0 = 0; x0 < kCkKeys; x0 += 32) weights(std::false_type(), x0);
         }
       }
       if (!ok) break;
