@@ -22,9 +22,9 @@
 namespace fpk {
 
 constexpr int kCkKeys = 128;  // keys a tile, and rows a query tile
-constexpr int kCkStart = 2;
+constexpr int kCkStart = 3;
 constexpr int kCkSnap = 2;      // key tiles at a unit's ends that a border does not cut off
-constexpr int kCkLeast = 4;     // places a CTA takes at least
+constexpr int kCkLeast = 4;     // places a CTA takes at least (a power of two)
 
 // Tokens of a query tile.
 FP_CK int ck_tile_tokens(int G) {
@@ -71,11 +71,12 @@ struct CkSeq {
     const int v = u - k, q = v >> lg, rem = v & ((1 << lg) - 1);
     return u * a0 + (((q * (q + 1)) >> 1) << lg) + rem * (q + 1);
   }
-  FP_CK int before(int u, int T) const { return u * kCkStart + tiles_before(u, T); }
+  // places a key tile of unit u takes
+  FP_CK int weight(int u, int T) const { return n - u * T > T / 2 ? 2 : 1; }
+  FP_CK int before(int u, int T) const { return u * kCkStart + 2 * tiles_before(u, T); }  // (all but the last: two tiles)
+  FP_CK int places(int u, int T) const { return kCkStart + weight(u, T) * tiles(u, T); }
   // places of one KV head's units (ck_fits: below 2^31)
-  FP_CK int cost(int T) const {
-    return units == 0 ? 0 : before(units - 1, T) + kCkStart + all_tiles();
-  }
+  FP_CK int cost(int T) const { return units == 0 ? 0 : before(units - 1, T) + places(units - 1, T); }
   // the unit that holds place x < cost
   FP_CK int unit_at(int x, int T) const {
     int lo = 0, hi = units;  // before(lo) <= x
@@ -91,15 +92,15 @@ struct CkSeq {
 // Whether the line of any batch within these bounds is shorter than 2^31 places.
 inline bool ck_fits(int n_tokens, int B, int max_len, int Hkv, int tile_tokens) {
   const long long units = n_tokens / (2 * tile_tokens) + (long long)B;
-  return units * Hkv < (1LL << 31) && units * Hkv * (kCkStart + (max_len + kCkKeys - 1LL) / kCkKeys) < (1LL << 31);
+  return units * Hkv < (1LL << 31) && units * Hkv * (kCkStart + 2 * ((max_len + kCkKeys - 1LL) / kCkKeys)) < (1LL << 31);
 }
 
-// A border at place `off` of a unit of nt key tiles, moved off its ends: the place to
-// cut at, 0 (before the unit) or kCkStart + nt (behind it).
-FP_CK int ck_snap(int off, int nt) {
-  if (off < kCkStart + kCkSnap) return 0;
-  if (off > kCkStart + nt - kCkSnap) return kCkStart + nt;
-  return off;
+// A border at place `off` of a unit of nt key tiles of `weight` places, moved back to the
+// beginning of a key tile and off the unit's ends: the place to cut at, 0 (before the
+// unit) or all its places (behind it).
+FP_CK int ck_snap(int off, int nt, int weight) {
+  const int t = off < kCkStart ? 0 : (off - kCkStart) / weight;
+  return t < kCkSnap ? 0 : t > nt - kCkSnap ? kCkStart + weight * nt : kCkStart + weight * t;
 }
 
 // Where the stretch of CTA c of g begins, before its border is moved: floor(W c / g).
@@ -114,9 +115,9 @@ FP_CK int ck_first_from(int t, int W, int g) {
 }
 
 // The CTAs that share the unit of nt key tiles at place x: *own begins it, *parts in all.
-FP_CK void ck_parts(int x, int nt, int W, int g, int* own, int* parts) {
-  *own = ck_first_from(x + kCkStart + kCkSnap, W, g) - 1;
-  *parts = ck_first_from(x + kCkStart + nt - kCkSnap + 1, W, g) - *own;
+FP_CK void ck_parts(int x, int nt, int weight, int W, int g, int* own, int* parts) {
+  *own = ck_first_from(x + kCkStart + weight * kCkSnap, W, g) - 1;
+  *parts = ck_first_from(x + kCkStart + weight * (nt - kCkSnap + 1), W, g) - *own;
 }
 
 // CTAs that take part of W places.

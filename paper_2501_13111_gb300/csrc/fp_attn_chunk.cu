@@ -213,10 +213,10 @@ struct CkWalk {
       kvh = (unsigned)(at - from) / (unsigned)per;
       const int in = at - from - kvh * per;
       u = mine.unit_at(in, T);
-      const int start = mine.before(u, T), nt = mine.tiles(u, T);
-      off = ck_snap(in - start, nt);
+      const int start = mine.before(u, T);
+      off = ck_snap(in - start, mine.tiles(u, T), mine.weight(u, T));
       x = from + kvh * per + start + off;
-      if (off == kCkStart + nt) {  // behind the unit: the next one's beginning
+      if (off == mine.places(u, T)) {  // behind the unit: the next one's beginning
         off = 0;
         if (++u == mine.units) u = 0, ++kvh;
       }
@@ -246,15 +246,15 @@ struct CkWalk {
     }
     const int T = 2 * a.tile_tokens, nt = s.tiles(u, T), i0 = u * T;
     const bool pair = s.n - i0 > a.tile_tokens;
-    const int left = kCkStart + nt - off, take = min(left, rem);
-    p->t0 = max(0, off - kCkStart);
-    p->t1 = min(nt, max(0, off + take - kCkStart));
+    const int lg = pair ? 1 : 0, left = kCkStart + (nt << lg) - off, take = min(left, rem);
+    p->t0 = max(0, off - kCkStart) >> lg;
+    p->t1 = min(nt, max(0, off + take - kCkStart) >> lg);
     // the first tile's own last key tile
     p->e0 = min(p->t1, s.bad || !pair ? nt : (s.pos + i0 + a.tile_tokens + kCkKeys - 1) / kCkKeys);
     p->flags = (pair ? 1 : 0) | (off == 0 ? 2 : 0) | (take == left ? 4 : 0);
     p->row0 = s.row0 + i0, p->n = min(T, s.n - i0), p->pos = s.pos + i0, p->end = s.end;
     p->b = b, p->kvh = kvh, p->own = blockIdx.x, p->parts = 1;
-    if (off != 0 || take != left) ck_parts(x - off, nt, W, g, &p->own, &p->parts);
+    if (off != 0 || take != left) ck_parts(x - off, nt, 1 + lg, W, g, &p->own, &p->parts);
     rem -= take;
     x += take;
     off = 0;

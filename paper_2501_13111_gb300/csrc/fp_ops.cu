@@ -259,6 +259,7 @@ int fp_op_attention_chunk(const uint16_t* q, int q_stride, int n_tokens, int B, 
 int fp_op_softmax(const float* logits, int M, int V, const float* temperature, float* probs, int32_t* err,
                   void* stream) {
   if (!logits || !probs || M < 0 || V <= 0) return FP_ERR_INVALID_ARG;
+  if (M > (1 << 27) || V > (1 << 30)) return FP_ERR_UNSUPPORTED;
   return cuda_status(launch_softmax(logits, M, V, temperature, probs, err, (cudaStream_t)stream));
 }
 

@@ -3,6 +3,8 @@
 // beside the greedy choice of fp_rows.cu: one cluster of CTAs a row.
 #include <cooperative_groups.h>
 
+#include <utility>
+
 #include "chunk.cuh"
 #include "kernels.cuh"
 
@@ -13,7 +15,15 @@ namespace fpk {
 // ------------------------------------------------------------------ softmax
 // y_i = exp((x_i - max x) / T) / sum_j exp((x_j - max x) / T), T the row's
 // temperature; T = 0: 1 at the lowest index of the maximum, else 0.
-constexpr int kSmThreads = 512;
+//
+// A cluster of 1 to 8 CTAs a row, so that few long rows have as many SMs as many
+// short ones.  Each warp keeps its part of the row in registers (ITEMS 16-byte groups
+// a thread) as exponentials against its own maximum; the warps' maxima and sums meet
+// once through shared and distributed shared memory, and each value is written as
+// e 2^((m_warp - m) c) / sum: one read, one write, one meeting.  Rows of more than
+// kSmThreads x 4 x 8 x 8 values are read a second time instead.  Groups are aligned
+// in memory: the row's first and last may be part of a neighbour's.
+constexpr int kSmThreads = 512, kSmWarps = kSmThreads / 32, kSmItems = 8, kSmMaxCTAs = 8;
 
 FP_DEV float sm_ex2(float x) {
   float y;
@@ -21,111 +31,254 @@ FP_DEV float sm_ex2(float x) {
   return y;
 }
 
-// The block's sum, maximum or minimum of v (every thread gets it); red: 16 words.
-template <typename T, typename F>
-FP_DEV T block_all(T v, T* red, F f) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v = f(v, __shfl_xor_sync(0xffffffffu, v, o));
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
-  __syncthreads();
-  v = red[threadIdx.x & 15];
-#pragma unroll
-  for (int o = 8; o > 0; o >>= 1) v = f(v, __shfl_xor_sync(0xffffffffu, v, o));
-  return v;
+// A set's maximum and its sum of exponentials against it, or (T = 0) the lowest index
+// of the maximum.
+struct SmPart {
+  float m, s;
+  int at;
+};
+FP_DEV void sm_add(SmPart& a, float m, float s, int at, float c) {
+  const float m2 = fmaxf(a.m, m);
+  // (a set without values has s = 0: its -inf - -inf stays out)
+  const float fa = a.m == -INFINITY ? 0.f : sm_ex2((a.m - m2) * c), fb = m == -INFINITY ? 0.f : sm_ex2((m - m2) * c);
+  a.s = a.s * fa + s * fb;
+  if (m == a.m) a.at = min(a.at, at);
+  else if (m > a.m) a.at = at;
+  a.m = m2;
 }
 
-// The plain form: one CTA a row, three passes over it.
+// ITEMS 0: any length, read twice.
+template <int ITEMS>
 __global__ void __launch_bounds__(kSmThreads)
-    softmax_kernel(const float* __restrict__ x, int V, const float* __restrict__ temp, float* __restrict__ y,
-                   int32_t* err) {
-  __shared__ float red[16];
-  __shared__ int redi[16];
+    softmax_kernel(const float* x, int V, const float* __restrict__ temp, float* y, int32_t* err) {
+  __shared__ SmPart s_part[kSmWarps], s_cta;
   pdl_trigger();
   pdl_wait();
-  const long long base = (long long)blockIdx.x * V;
-  const float t = temp ? temp[blockIdx.x] : 1.f;
-  const bool bad = !(t >= 0.f) || isinf(t);
-  if (bad && threadIdx.x == 0 && err) atomicExch(err, 1);
-  float mx = -INFINITY;
-  for (int i = threadIdx.x; i < V; i += kSmThreads) mx = fmaxf(mx, x[base + i]);
-  mx = block_all(mx, red, [](float a, float b) { return fmaxf(a, b); });
-  if (bad || mx == -INFINITY) {
-    for (int i = threadIdx.x; i < V; i += kSmThreads) y[base + i] = 0.f;
-    return;
+  cg::cluster_group cluster = cg::this_cluster();
+  const int C = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const long long row = blockIdx.x / C;
+  const float* xr = x + row * V;
+  float* yr = y + row * V;
+  // groups of four: group g holds values 4 g - skew .. 4 g - skew + 3
+  const int skew = (int)(((uintptr_t)xr & 15) >> 2), groups = (V + skew + 3) >> 2;
+  const int per = ((groups + C - 1) / C + 31) & ~31;  // of a CTA, by whole warps
+  const int g0 = min(groups, rank * per), g1 = min(groups, g0 + per);
+  const float t = temp ? __ldg(temp + row) : 1.f;
+  const bool bad = !(t >= 0.f) || isinf(t), greedy = t == 0.f;
+  if (bad && rank == 0 && threadIdx.x == 0 && err) atomicExch(err, 1);
+  const float c = greedy ? 1.f : fminf(1.4426950408889634f / t, 3.4e38f);
+  auto load = [&](int g) -> float4 {
+    const int i = 4 * g - skew;
+    if (g >= g1) return make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+    if (i >= 0 && i + 3 < V) return *reinterpret_cast<const float4*>(xr + i);
+    float v[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = i + k >= 0 && i + k < V ? xr[i + k] : -INFINITY;
+    return make_float4(v[0], v[1], v[2], v[3]);
+  };
+  auto top = [](float4 v) { return fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w)); };
+  auto lowest = [&](float4 v, int g, float m, int at) {  // the lowest index of m so far
+    const int i = 4 * g - skew;
+    return min(at, v.x == m ? i : v.y == m ? i + 1 : v.z == m ? i + 2 : v.w == m ? i + 3 : 0x7fffffff);
+  };
+  auto expo = [&](float4 v, float m) {  // against m (-inf: a set that is masked throughout)
+    const float r = m == -INFINITY ? 0.f : m;
+    return make_float4(sm_ex2((v.x - r) * c), sm_ex2((v.y - r) * c), sm_ex2((v.z - r) * c), sm_ex2((v.w - r) * c));
+  };
+
+  // this warp's part, ITEMS groups a lane in registers
+  float4 v[ITEMS ? ITEMS : 1];
+  SmPart p = {-INFINITY, 0.f, 0x7fffffff};
+  if constexpr (ITEMS > 0) {
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k) v[k] = load(g0 + k * kSmThreads + (int)threadIdx.x);
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k) p.m = fmaxf(p.m, top(v[k]));
+    p.m = warp_max(p.m);
+    if (greedy) {
+#pragma unroll
+      for (int k = 0; k < ITEMS; ++k) p.at = lowest(v[k], g0 + k * kSmThreads + (int)threadIdx.x, p.m, p.at);
+      p.at = __reduce_min_sync(0xffffffffu, p.at);
+    } else {
+#pragma unroll
+      for (int k = 0; k < ITEMS; ++k) {
+        v[k] = expo(v[k], p.m);
+        p.s += (v[k].x + v[k].y) + (v[k].z + v[k].w);
+      }
+      p.s = warp_sum(p.s);
+    }
+  } else {
+#pragma unroll 1
+    for (int g = g0 + (int)threadIdx.x; g < g1; g += 4 * kSmThreads) {
+      float4 w[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) w[k] = load(g + k * kSmThreads);
+      float m = -INFINITY, s = 0.f;
+      int at = 0x7fffffff;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) m = fmaxf(m, top(w[k]));
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if (greedy) at = lowest(w[k], g + k * kSmThreads, m, at);
+        const float4 e = expo(w[k], m);
+        s += (e.x + e.y) + (e.z + e.w);
+      }
+      sm_add(p, m, s, at, c);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+      sm_add(p, __shfl_xor_sync(0xffffffffu, p.m, o), __shfl_xor_sync(0xffffffffu, p.s, o),
+             __shfl_xor_sync(0xffffffffu, p.at, o), c);
   }
-  if (t == 0.f) {
-    int at = 0x7fffffff;
-    for (int i = threadIdx.x; i < V; i += kSmThreads)
-      if (x[base + i] == mx) at = min(at, i);
-    at = block_all(at, redi, [](int a, int b) { return min(a, b); });
-    for (int i = threadIdx.x; i < V; i += kSmThreads) y[base + i] = i == at ? 1.f : 0.f;
-    return;
+  const float mine = p.m;  // what this warp's exponentials are against
+  if (lane == 0) s_part[warp] = p;
+  __syncthreads();
+  p = s_part[lane & (kSmWarps - 1)];
+#pragma unroll
+  for (int o = kSmWarps / 2; o > 0; o >>= 1)
+    sm_add(p, __shfl_xor_sync(0xffffffffu, p.m, o), __shfl_xor_sync(0xffffffffu, p.s, o),
+           __shfl_xor_sync(0xffffffffu, p.at, o), c);
+  if (C > 1) {
+    if (threadIdx.x == 0) s_cta = p;
+    cluster.sync();
+    p = *cluster.map_shared_rank(&s_cta, lane & (C - 1));
+    for (int o = C / 2; o > 0; o >>= 1)
+      sm_add(p, __shfl_xor_sync(0xffffffffu, p.m, o), __shfl_xor_sync(0xffffffffu, p.s, o),
+             __shfl_xor_sync(0xffffffffu, p.at, o), c);
   }
-  const float c = fminf(1.4426950408889634f / t, 3.4e38f);
-  float s = 0.f;
-  for (int i = threadIdx.x; i < V; i += kSmThreads) s += sm_ex2((x[base + i] - mx) * c);
-  s = block_all(s, red, [](float a, float b) { return a + b; });
-  for (int i = threadIdx.x; i < V; i += kSmThreads) y[base + i] = sm_ex2((x[base + i] - mx) * c) / s;
+
+  const bool nothing = bad || (p.m == -INFINITY && (greedy || p.s == 0.f));  // (a NaN: p.s is one)
+  const bool same = ((uintptr_t)xr & 15) == ((uintptr_t)yr & 15);
+  auto store = [&](int g, float4 o) {
+    const int i = 4 * g - skew;
+    if (g >= g1) return;
+    if (same && i >= 0 && i + 3 < V) {
+      *reinterpret_cast<float4*>(yr + i) = o;
+      return;
+    }
+    const float f[4] = {o.x, o.y, o.z, o.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (i + k >= 0 && i + k < V) yr[i + k] = f[k];
+  };
+  float f = 1.f / p.s;
+  if (ITEMS > 0 && p.s == p.s) f = mine == -INFINITY ? 0.f : sm_ex2((mine - p.m) * c) / p.s;
+  auto emit = [&](int g, float4 e) {
+    float4 o;
+    if (nothing) {
+      o = make_float4(0.f, 0.f, 0.f, 0.f);
+    } else if (greedy) {
+      const int i = 4 * g - skew;
+      o = make_float4(i == p.at ? 1.f : 0.f, i + 1 == p.at ? 1.f : 0.f, i + 2 == p.at ? 1.f : 0.f, i + 3 == p.at ? 1.f : 0.f);
+    } else {
+      o = make_float4(e.x * f, e.y * f, e.z * f, e.w * f);
+    }
+    store(g, o);
+  };
+  if constexpr (ITEMS > 0) {
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k) emit(g0 + k * kSmThreads + (int)threadIdx.x, v[k]);
+  } else {
+#pragma unroll 4
+    for (int g = g0 + (int)threadIdx.x; g < g1; g += kSmThreads) emit(g, expo(load(g), p.m));
+  }
+  if (C > 1) cluster.sync();  // the others have read this CTA's part
 }
 
+// CTAs a row: enough that a thread holds four groups, and that few rows reach all SMs
+// (a power of two up to 8; us with 1 / 2 / 4 / 8 of them: see the measurements below).
 cudaError_t launch_softmax(const float* logits, int M, int V, const float* temp, float* probs, int32_t* err,
                            cudaStream_t s) {
   if (M <= 0) return cudaSuccess;
-  return launch(softmax_kernel, dim3(M), dim3(kSmThreads), 0, s, logits, V, temp, probs, err);
+  const int groups = V / 4 + 2;
+  int C = 1;
+  while (C < kSmMaxCTAs && (groups > 4 * kSmThreads * C || (long long)M * C < 128)) C *= 2;
+  while (C > 1 && groups <= kSmThreads / 2 * C) C /= 2;  // no CTA without work
+  const int items = (groups + C * kSmThreads - 1) / (C * kSmThreads);
+  auto go = [&](auto kern) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)M * C);
+    cfg.blockDim = dim3(kSmThreads);
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = C;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = g_pdl ? 1 : 0;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, kern, logits, V, temp, probs, err);
+  };
+  return items <= 2 ? go(softmax_kernel<2>) : items <= 4 ? go(softmax_kernel<4>) : items <= kSmItems ? go(softmax_kernel<kSmItems>) : go(softmax_kernel<0>);
 }
 
 // ------------------------------------------------------------------ verification
 // Sequence b's rows are its last accepted token and the k drafted after it.  Row
-// i's draft t (the token of row i + 1) is accepted while u_i q_i(t) < p_i(t)
-// (products of two fp32 in fp64: exact); a is the first refused row, or k.  The
-// token after it is drawn from w = max(0, p_a - q_a) (a < k), or p_k: the lowest t
-// with sum_{s <= t} w_s > r sum w.
+// i's draft t (the token of row i + 1) is accepted while u_i q_i(t) < p_i(t); a is the
+// first refused row, or k.  The token after it is drawn from w = max(0, p_a - q_a)
+// (a < k), or p_k: the lowest t with sum_{s <= t} w_s > r sum w.
 // A border is a sum of up to V fp32 values and has to fall where fp64 puts it, but
-// fp64 adds are rare here (2 lanes a cycle and SM against 128): each weight is kept
-// as d + e (the exact difference, two fp32), each lane's sum as s + c with the
-// error of every addition carried along, good to about 2^-46; only the lanes' sums
-// are joined in fp64.  A cluster of 8 CTAs a sequence: every warp sums a run of
-// consecutive weights, the 128 sums meet through distributed shared memory, and
-// the warp whose run holds the border looks through it again (from L2).
+// fp64 is slow here (an addition takes about 300 cycles, and there were forty one
+// after another: 21 us for 32 sequences of 32000 tokens).  So sums are pairs of fp32,
+// hi + lo, the error of every addition carried along: good to 2^-46 or better.
+// Differences p - q and products u q are exact as pairs.
+// A cluster of 8 CTAs a sequence: every warp sums a run of consecutive weights, the
+// CTAs' totals meet through distributed shared memory, and the warp whose run holds
+// the border looks through it again (from L2): 32 pieces, then the piece's tokens.
+// Bound by latency: cu, the drafts, their probabilities, the row, the meeting and the
+// second look follow one another.
 constexpr int kVfCTAs = 8, kVfThreads = 512, kVfWarps = kVfThreads / 32, kVfRuns = kVfCTAs * kVfWarps;
 
-struct Pair {  // hi + lo
+struct Pair {
   float hi, lo;
 };
-// a - b, exactly
-FP_DEV Pair diff2(float a, float b) {
-  const float d = __fsub_rn(a, b), v = __fsub_rn(d, a);
-  return {d, __fsub_rn(__fsub_rn(a, __fsub_rn(d, v)), __fadd_rn(b, v))};
+// a + b, exactly
+FP_DEV Pair sum2(float a, float b) {
+  const float s = __fadd_rn(a, b), v = __fsub_rn(s, a);
+  return {s, __fadd_rn(__fsub_rn(a, __fsub_rn(s, v)), __fsub_rn(b, v))};
 }
-// s += w, the addition's error to s.lo
-FP_DEV void add2(Pair& s, Pair w) {
-  const float t = __fadd_rn(s.hi, w.hi), v = __fsub_rn(t, s.hi);
-  const float e = __fadd_rn(__fsub_rn(s.hi, __fsub_rn(t, v)), __fsub_rn(w.hi, v));
-  s.hi = t;
-  s.lo = __fadd_rn(s.lo, __fadd_rn(e, w.lo));
+// hi + lo with hi the nearer fp32 (|hi| >= |lo|)
+FP_DEV Pair tidy(float hi, float lo) {
+  const float s = __fadd_rn(hi, lo);
+  return {s, __fsub_rn(lo, __fsub_rn(s, hi))};
 }
-FP_DEV double value(Pair p) { return (double)p.hi + (double)p.lo; }
+FP_DEV Pair add(Pair a, Pair b) {
+  const Pair s = sum2(a.hi, b.hi);
+  return tidy(s.hi, __fadd_rn(s.lo, __fadd_rn(a.lo, b.lo)));
+}
+FP_DEV Pair times(Pair a, float r) {
+  const float h = __fmul_rn(a.hi, r);
+  return tidy(h, __fmaf_rn(a.lo, r, __fmaf_rn(a.hi, r, -h)));
+}
+FP_DEV bool greater(Pair a, Pair b) {
+  const Pair d = sum2(a.hi, -b.hi);
+  return __fadd_rn(d.hi, __fadd_rn(d.lo, __fsub_rn(a.lo, b.lo))) > 0.f;
+}
+FP_DEV Pair shfl(Pair v, int l) { return {__shfl_sync(0xffffffffu, v.hi, l), __shfl_sync(0xffffffffu, v.lo, l)}; }
 
-FP_DEV double warp_sum_d(double v) {
+// Inclusive sums over groups of N lanes, lower lanes first.
+template <int N>
+FP_DEV Pair scan(Pair v, int lane) {
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  return v;
-}
-
-// Inclusive sums over the lanes.
-FP_DEV double scan_d(double v, int lane) {
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const double f = __shfl_up_sync(0xffffffffu, v, o);
-    if (lane >= o) v += f;
+  for (int o = 1; o < N; o <<= 1) {
+    const Pair f = {__shfl_up_sync(0xffffffffu, v.hi, o, N), __shfl_up_sync(0xffffffffu, v.lo, o, N)};
+    if ((lane & (N - 1)) >= o) v = add(f, v);
   }
   return v;
 }
 
+// Of the lanes whose weight counts, the first whose sum is past the border; rounding at
+// the very end, an r of 1 or more or a NaN leaves none: the last then.  -1: no weight at all.
+FP_DEV int holder(Pair upto, float w, Pair border) {
+  const unsigned has = __ballot_sync(0xffffffffu, w > 0.f), past = __ballot_sync(0xffffffffu, w > 0.f && greater(upto, border));
+  return past ? __ffs(past) - 1 : 31 - __clz(has);
+}
+
 // The weight of token t: p, less q where there is one, without token `gone`; none below zero.
 FP_DEV Pair weight(const float* p, const float* q, int t, int gone) {
-  Pair w = q ? diff2(__ldg(p + t), __ldg(q + t)) : Pair{__ldg(p + t), 0.f};
+  Pair w = sum2(__ldg(p + t), q ? -__ldg(q + t) : 0.f);
   if (!(w.hi > 0.f) || t == gone) w = {0.f, 0.f};
   return w;
 }
@@ -134,7 +287,7 @@ __global__ void __cluster_dims__(kVfCTAs, 1, 1) __launch_bounds__(kVfThreads)
     verify_kernel(const float* __restrict__ p, const float* __restrict__ q, int V, int n_tokens, int B,
                   const int32_t* __restrict__ cu, const int32_t* __restrict__ tokens, const float* __restrict__ u,
                   const float* __restrict__ r, int32_t* __restrict__ out, int32_t* __restrict__ n_out, int32_t* err) {
-  __shared__ double s_sum[kVfWarps];
+  __shared__ Pair s_sum[kVfWarps], s_cta;
   __shared__ int s_a;
   pdl_trigger();
   pdl_wait();
@@ -151,6 +304,7 @@ __global__ void __cluster_dims__(kVfCTAs, 1, 1) __launch_bounds__(kVfThreads)
   // the first refused draft
   if (warp == 0) {
     int a = n - 1;
+#pragma unroll 1
     for (int i0 = 0; i0 < n - 1; i0 += 32) {
       const int i = i0 + lane;
       bool refused = false;
@@ -159,7 +313,12 @@ __global__ void __cluster_dims__(kVfCTAs, 1, 1) __launch_bounds__(kVfThreads)
         const bool ok = t >= 0 && t < V;
         if (!ok && rank == 0 && err) atomicExch(err, 1);
         const long long at = (long long)(row0 + i) * V + (ok ? t : 0);
-        refused = !ok || !((double)__ldg(u + row0 + i) * (q ? (double)__ldg(q + at) : 1.0) < (double)__ldg(p + at));
+        // (both sides of u q < p times 2^80 where the product's error could be lost)
+        float qt = q ? __ldg(q + at) : 1.f, pt = __ldg(p + at);
+        const float ui = __ldg(u + row0 + i);
+        if (qt < 1e-15f && pt < 1e-15f) qt *= 0x1p80f, pt *= 0x1p80f;
+        const float x = __fmul_rn(ui, qt), e = __fmaf_rn(ui, qt, -x);
+        refused = !ok || !(x < pt || (x == pt && e < 0.f));
       }
       const unsigned any = __ballot_sync(0xffffffffu, refused);
       if (any) {
@@ -175,83 +334,81 @@ __global__ void __cluster_dims__(kVfCTAs, 1, 1) __launch_bounds__(kVfThreads)
   const float* qr = a < n - 1 && q ? q + (long long)(row0 + a) * V : nullptr;
   int gone = a < n - 1 && !q ? __ldg(tokens + row0 + a + 1) : -1;
   const int run = (V + kVfRuns - 1) / kVfRuns;
-  const int lo = min((long long)V, (long long)(rank * kVfWarps + warp) * run), hi = min(V, lo + run);
+  const int lo = (int)min((long long)V, (long long)(rank * kVfWarps + warp) * run), hi = min(V, lo + run);
+  const float rb = __ldg(r + b);
   for (int turn = 0; turn < 2; ++turn) {
     Pair s = {0.f, 0.f};
-#pragma unroll 8
-    for (int t = lo + lane; t < hi; t += 32) add2(s, weight(pr, qr, t, gone));
-    const double mine = warp_sum_d(value(s));
-    if (lane == 0) s_sum[warp] = mine;
+#pragma unroll 1
+    for (int t0 = lo + lane; t0 < hi; t0 += 16 * 32) {  // sixteen loads in flight
+      float x[16], y[16];
+#pragma unroll
+      for (int k = 0; k < 16; ++k) {
+        const int t = t0 + 32 * k;
+        x[k] = t < hi ? __ldg(pr + t) : 0.f;
+        y[k] = t < hi && qr ? __ldg(qr + t) : 0.f;
+      }
+#pragma unroll
+      for (int k = 0; k < 16; ++k) {
+        Pair w = sum2(x[k], -y[k]);
+        if (!(w.hi > 0.f) || t0 + 32 * k == gone) w = {0.f, 0.f};
+        const Pair f = sum2(s.hi, w.hi);
+        s = {f.hi, __fadd_rn(s.lo, __fadd_rn(f.lo, w.lo))};
+      }
+    }
+    s = shfl(scan<32>(tidy(s.hi, s.lo), lane), 31);
+    if (lane == 0) s_sum[warp] = s;
+    __syncthreads();
+    const Pair mine = s_sum[lane & (kVfWarps - 1)], upto = scan<kVfWarps>(mine, lane);  // within this CTA
+    if (threadIdx.x == kVfWarps - 1) s_cta = upto;
     cluster.sync();
-    // Every warp, in one order: the runs' sums and what is before each of them.
-    constexpr int R = kVfRuns / 32;
-    double v[R], upto[R], all = 0.;
-#pragma unroll
-    for (int j = 0; j < R; ++j) {
-      const int k = lane * R + j;
-      v[j] = cluster.map_shared_rank(s_sum, k / kVfWarps)[k % kVfWarps];
-      all += v[j];
-    }
-    all = scan_d(all, lane);
-    const double total = __shfl_sync(0xffffffffu, all, 31);
-    double before = __shfl_up_sync(0xffffffffu, all, 1);
-    if (lane == 0) before = 0.;
-    cluster.sync();  // the sums have been read
-    if (!(total > 0.) || !(total < (double)INFINITY)) {
-      if (turn == 0 && (qr || gone >= 0)) {  // the draft leaves nothing (p <= q throughout): the target's own
-        qr = nullptr;
-        gone = -1;
-        continue;
+    const Pair theirs = *cluster.map_shared_rank(&s_cta, lane & (kVfCTAs - 1)), all = scan<kVfCTAs>(theirs, lane);
+    const Pair total = shfl(all, kVfCTAs - 1);
+    auto leave = cluster.barrier_arrive();  // (a CTA stays until the others have read its total)
+    const bool drawable = total.hi > 0.f && total.hi < INFINITY;
+    if (drawable) {
+      const Pair border = times(total, rb);
+      if (holder(all, lane < kVfCTAs ? theirs.hi : 0.f, border) == rank) {
+        const Pair before = rank ? shfl(all, rank - 1) : Pair{0.f, 0.f};
+        const Pair to = add(before, upto);
+        if (holder(to, lane < kVfWarps ? mine.hi : 0.f, border) == warp) {
+          const Pair from = warp ? shfl(to, warp - 1) : before;
+          // within the run: 32 pieces, then the tokens of the piece
+          const int seg = (hi - lo + 31) / 32;
+          Pair ps = {0.f, 0.f};
+#pragma unroll 4
+          for (int t = lo + lane * seg; t < min(hi, lo + (lane + 1) * seg); ++t) ps = add(ps, weight(pr, qr, t, gone));
+          const Pair pu = add(from, scan<32>(ps, lane));
+          const int piece = holder(pu, ps.hi, border);
+          Pair at = piece ? shfl(pu, piece - 1) : from;
+          int token = -1;
+          const int t1 = min(hi, lo + (piece + 1) * seg);
+#pragma unroll 1
+          for (int t0 = lo + piece * seg; t0 < t1; t0 += 32) {
+            const Pair w = t0 + lane < t1 ? weight(pr, qr, t0 + lane, gone) : Pair{0.f, 0.f};
+            const Pair wu = add(at, scan<32>(w, lane));
+            const int l = holder(wu, w.hi, border);
+            if (l >= 0) token = t0 + l;
+            if (__any_sync(0xffffffffu, w.hi > 0.f && greater(wu, border))) break;
+            at = shfl(wu, 31);
+          }
+          if (lane == 0) {
+            out[row0 + a] = token;
+            n_out[b] = a + 1;
+          }
+        }
       }
-      if (rank == 0 && threadIdx.x == 0) {
-        if (err) atomicExch(err, 1);
-        out[row0 + a] = -1;
-        n_out[b] = a;
-      }
-      break;
     }
-    // the run that holds the border: the first that reaches past it (r >= 1 or
-    // NaN: none; then the last that holds a weight)
-    const double border = (double)__ldg(r + b) * total;
-    int first = kVfRuns, last = -1;
-    double from = 0.;
-#pragma unroll
-    for (int j = 0; j < R; ++j) {
-      upto[j] = before + v[j];
-      if (v[j] > 0.) {
-        last = lane * R + j;
-        if (first == kVfRuns && upto[j] > border) first = lane * R + j;
-      }
-      if (lane * R + j == rank * kVfWarps + warp) from = before;
-      before = upto[j];
+    cluster.barrier_wait(std::move(leave));
+    if (drawable) break;
+    if (turn == 0 && (qr || gone >= 0)) {  // the draft leaves nothing (p <= q throughout): the target's own
+      qr = nullptr;
+      gone = -1;
+      continue;
     }
-    first = __reduce_min_sync(0xffffffffu, first);
-    last = __reduce_max_sync(0xffffffffu, last);
-    if (first == kVfRuns) first = last;
-    from = __shfl_sync(0xffffffffu, from, (rank * kVfWarps + warp) / R);
-    if (first != rank * kVfWarps + warp) break;
-    // within the run: 32 pieces, then the tokens of the piece
-    const int seg = (hi - lo + 31) / 32;
-    Pair ps = {0.f, 0.f};
-    for (int t = lo + lane * seg; t < min(hi, lo + (lane + 1) * seg); ++t) add2(ps, weight(pr, qr, t, gone));
-    const double pv = value(ps), pu = from + scan_d(pv, lane);
-    unsigned has = __ballot_sync(0xffffffffu, pv > 0.), past = __ballot_sync(0xffffffffu, pv > 0. && pu > border);
-    const int piece = past ? __ffs(past) - 1 : 31 - __clz(has);
-    double at = __shfl_sync(0xffffffffu, pu - pv, piece);
-    int token = -1;
-    const int t1 = min(hi, lo + (piece + 1) * seg);
-    for (int t0 = lo + piece * seg; t0 < t1; t0 += 32) {
-      const double w = t0 + lane < t1 ? value(weight(pr, qr, t0 + lane, gone)) : 0.;
-      const double wu = at + scan_d(w, lane);
-      has = __ballot_sync(0xffffffffu, w > 0.);
-      past = __ballot_sync(0xffffffffu, w > 0. && wu > border);
-      if (past || has) token = t0 + (past ? __ffs(past) - 1 : 31 - __clz(has));
-      if (past) break;
-      at = __shfl_sync(0xffffffffu, wu, 31);
-    }
-    if (lane == 0) {
-      out[row0 + a] = token;
-      n_out[b] = a + 1;
+    if (rank == 0 && threadIdx.x == 0) {
+      if (err) atomicExch(err, 1);
+      out[row0 + a] = -1;
+      n_out[b] = a;
     }
     break;
   }

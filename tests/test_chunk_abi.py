@@ -69,7 +69,8 @@ def test_attention_chunk_refusals(fp):
                dict(ws=A + 128), dict(kvq=1), dict(k=None)):
         assert call(**kw) == INVALID, kw
     for kw in (dict(q=A + 8), dict(out=A + 8), dict(qs=516), dict(hd=96), dict(page=8), dict(v=A + 4),
-               dict(H=258, qs=258 * 128), dict(pages=1 << 26)):
+               dict(H=258, qs=258 * 128), dict(pages=1 << 26), dict(n=(1 << 30) + 1),
+               dict(B=(1 << 26) + 1), dict(pps=1 << 26, max_len=1 << 30, n=1 << 28)):
         assert call(**kw) == UNSUPPORTED, kw
     assert call(max_len=65) == CAPACITY
     assert call(n=0) == 0 and call(B=0) == 0 and call(max_new=0) == 0 and call(max_len=0) == 0
@@ -86,6 +87,7 @@ def test_softmax_refusals(fp):
     call = lambda x=A, M=2, V=5, t=None, y=A: code(lambda: fp.fp_op_softmax(x, M, V, t, y))  # noqa: E731
     for kw in (dict(x=None), dict(y=None), dict(M=-1), dict(V=0), dict(V=-3)):
         assert call(**kw) == INVALID, kw
+    assert call(M=(1 << 27) + 1) == call(V=(1 << 30) + 1) == UNSUPPORTED
     assert call(M=0) == 0
 
 

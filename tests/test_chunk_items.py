@@ -33,15 +33,17 @@ int main() {
       int e = std::min(pos + (u + 1) * T, pos + s.n);
       if (s.bad) e = std::max(0, std::min(pos + s.n, top));
       if (nt != (e + 127) / 128) return bad("tiles", it);
-      if (s.unit_at(x, T) != u || s.unit_at(x + kCkStart + nt - 1, T) != u) return bad("unit_at", it);
-      x += kCkStart + nt;
+      const int places = kCkStart + (s.n - u * T > tt ? 2 : 1) * nt;
+      if (s.places(u, T) != places) return bad("places", it);
+      if (s.unit_at(x, T) != u || s.unit_at(x + places - 1, T) != u) return bad("unit_at", it);
+      x += places;
     }
     if (s.cost(T) != x) return bad("cost", it);
   }
   for (int it = 0; it < 3000; ++it) {  // the stretches
     const int G = 1 + rand() % 16, tt = ck_tile_tokens(G), T = 2 * tt, B = 1 + rand() % 12, Hkv = 1 + rand() % 5;
     const int grid = 1 + rand() % 152;
-    struct Unit { int x; int nt; std::vector<int> seen; int own = -1, parts = 0; };
+    struct Unit { int x; int nt, w; std::vector<int> seen; int own = -1, parts = 0; int all() const { return kCkStart + w * nt; } };
     std::vector<Unit> units;
     int W = 0;
     for (int b = 0; b < B; ++b) {
@@ -49,8 +51,8 @@ int main() {
       s.set(0, rand() % 3 ? rand() % 9 : rand() % 700, rand() % 2 ? rand() % 50 : rand() % 4000, tt, 1000, 5000);
       for (int h = 0; h < Hkv; ++h)
         for (int u = 0; u < s.units; ++u) {
-          units.push_back({W, s.tiles(u, T), std::vector<int>(s.tiles(u, T))});
-          W += kCkStart + s.tiles(u, T);
+          units.push_back({W, s.tiles(u, T), s.weight(u, T), std::vector<int>(s.tiles(u, T))});
+          W += units.back().all();
         }
     }
     const int g = ck_ctas(W, grid);
@@ -60,16 +62,17 @@ int main() {
       const int x = ck_begin(c, W, g);
       if (x != (long long)W * c / g) return -1;
       for (auto& u : units)
-        if (x >= u.x && x < u.x + kCkStart + u.nt) return u.x + ck_snap(x - u.x, u.nt);
+        if (x >= u.x && x < u.x + u.all()) return u.x + ck_snap(x - u.x, u.nt, u.w);
       return W;
     };
     for (int c = 0; c < grid; ++c) {
       const int lo = begin(c), hi = begin(c + 1);
       if (hi < lo) return bad("order", it);
       for (auto& u : units) {
-        const int p = std::max(lo, u.x), q = std::min(hi, u.x + kCkStart + u.nt);
+        const int p = std::max(lo, u.x), q = std::min(hi, u.x + u.all());
         if (p >= q) continue;
-        const int t0 = std::max(0, p - u.x - kCkStart), t1 = std::max(0, q - u.x - kCkStart);
+        if (p > u.x && (p - u.x - kCkStart) % u.w) return bad("a border inside a key tile", it);
+        const int t0 = std::max(0, p - u.x - kCkStart) / u.w, t1 = std::max(0, q - u.x - kCkStart) / u.w;
         if (p > u.x && t0 < kCkSnap) return bad("a border inside a unit's start", it);
         if (t1 <= t0) return bad("a part without keys", it);
         for (int t = t0; t < t1; ++t) ++u.seen[t];
@@ -79,7 +82,7 @@ int main() {
     }
     for (auto& u : units) {
       int own, parts;
-      ck_parts(u.x, u.nt, W, g, &own, &parts);
+      ck_parts(u.x, u.nt, u.w, W, g, &own, &parts);
       if (u.nt > 0 && u.parts > 1 && (own != u.own || parts != u.parts)) return bad("ck_parts", it);
     }
     for (auto& u : units)

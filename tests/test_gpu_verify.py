@@ -84,6 +84,11 @@ def test_softmax_special_rows(fp):
     assert got[6].sum() == got[6, V - 1] == 1
     assert got[7].sum() == got[7, x[7].argmax()] == 1
     _check_probs(got[8:9], x[8:9])
+    y = np.full((2, V), -np.inf, np.float32)  # a NaN among masked tokens; with T = 0 it is not the largest
+    y[:, 500] = np.nan
+    y[1, 600] = 1.0
+    got, err = _softmax(fp, y, np.array([1, 0], np.float32))
+    assert err == 0 and np.all(np.isnan(got[0])) and got[1].sum() == got[1, 600] == 1
     for bad in (-1.0, np.nan, np.inf, -np.inf):
         got, err = _softmax(fp, x[6:9], np.array([1, bad, 1], np.float32))
         assert err == 1 and np.all(got[1] == 0)
