@@ -49,13 +49,17 @@ FP_DEV uint2 codes8(const float* x, float s) {
 // cache rows out.
 template <int HD, bool KV8>
 __global__ void __launch_bounds__(256)
-    rope_kv_chunk_kernel(const uint16_t* __restrict__ qkv, int row_stride, int n_tokens, int B, int H, fp_kv_view kv,
+    rope_kv_chunk_kernel(const uint16_t* qkv, int row_stride, int n_tokens, int B, int H, fp_kv_view kv,
                          const int32_t* __restrict__ cu, const int32_t* __restrict__ pos, const float* __restrict__ cs,
                          uint16_t* q_out, int q_out_stride, int32_t* err) {
   pdl_trigger();
   pdl_wait();
   constexpr int L = HD / 16;  // lanes a head
-  const int m = blockIdx.x;
+  const int m = blockIdx.x, c = threadIdx.x % L, Hkv = kv.n_kv_heads, slots = H + 2 * Hkv;
+  // the first heads are on their way while the sequence is looked for
+  const uint16_t* src = qkv + (long long)m * row_stride + 8 * c;
+  const uint16_t* first = src + min((int)threadIdx.x / L, slots - 1) * HD;
+  uint4 lo = *reinterpret_cast<const uint4*>(first), hi = *reinterpret_cast<const uint4*>(first + HD / 2);
   if (m == 0) chunk_check(cu, B, n_tokens, err);
   const int b = chunk_owner(cu, B, m);
   if (b < 0) return;
@@ -66,7 +70,6 @@ __global__ void __launch_bounds__(256)
   }
   const long long row = cache_row(kv, b, p);
   if (row < 0 && threadIdx.x == 0 && err) atomicExch(err, 1);
-  const int c = threadIdx.x % L, Hkv = kv.n_kv_heads, slots = H + 2 * Hkv;
   float co[8], si[8];
   const float4* t = reinterpret_cast<const float4*>(cs + p * HD + 16 * c);
 #pragma unroll
@@ -74,15 +77,15 @@ __global__ void __launch_bounds__(256)
     const float4 f = __ldg(t + i);
     co[2 * i] = f.x, si[2 * i] = f.y, co[2 * i + 1] = f.z, si[2 * i + 1] = f.w;
   }
-  const uint16_t* src = qkv + (long long)m * row_stride + 8 * c;
   // every lane of a warp takes every turn: the shuffles need them all
   for (int s0 = 0; s0 < slots; s0 += 256 / L) {
     const int slot = s0 + threadIdx.x / L;
     const bool on = slot < slots;
     float x[16];
-    const uint16_t* sp = src + (on ? slot : 0) * HD;
-    unpack8(*reinterpret_cast<const uint4*>(sp), x);
-    unpack8(*reinterpret_cast<const uint4*>(sp + HD / 2), x + 8);
+    unpack8(lo, x);
+    unpack8(hi, x + 8);
+    const uint16_t* sp = src + min(slot + 256 / L, slots - 1) * HD;  // the next turn's
+    if (s0 + 256 / L < slots) lo = *reinterpret_cast<const uint4*>(sp), hi = *reinterpret_cast<const uint4*>(sp + HD / 2);
     if (slot < H + Hkv) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
