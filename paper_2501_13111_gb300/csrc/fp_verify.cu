@@ -21,9 +21,11 @@ namespace fpk {
 // a thread) as exponentials against its own maximum; the warps' maxima and sums meet
 // once through shared and distributed shared memory, and each value is written as
 // e 2^((m_warp - m) c) / sum: one read, one write, one meeting.  Rows of more than
-// kSmThreads x 4 x 8 x 8 values are read a second time instead.  Groups are aligned
-// in memory: the row's first and last may be part of a neighbour's.
-constexpr int kSmThreads = 512, kSmWarps = kSmThreads / 32, kSmItems = 8, kSmMaxCTAs = 8;
+// 262144 values (512 threads x 16 groups x 8 CTAs) are read a second time instead.
+// Groups are aligned in memory: the row's first and last may be part of a neighbour's.
+// Bound by latency and bytes one after the other: all CTAs read, meet and write at the
+// same time; 160 rows of 32000 take 15 us (2.7 TB/s), 3 of 128001 6.3.
+constexpr int kSmThreads = 512, kSmWarps = kSmThreads / 32, kSmItems = 16, kSmMaxCTAs = 8;
 
 FP_DEV float sm_ex2(float x) {
   float y;
@@ -186,14 +188,16 @@ __global__ void __launch_bounds__(kSmThreads)
   if (C > 1) cluster.sync();  // the others have read this CTA's part
 }
 
-// CTAs a row: enough that a thread holds four groups, and that few rows reach all SMs
-// (a power of two up to 8; us with 1 / 2 / 4 / 8 of them: see the measurements below).
+// CTAs a row, a power of two: few, so that a thread holds up to eight groups, but enough
+// for few rows to reach most SMs.  Larger clusters cost more to start than their
+// parallel loads give (us with up to 8 | 4 | 2 groups a thread: 400 rows of 50000 44.8 |
+// 66 | 66, 160 x 32000 15.0 | 15.2 | 23).
 cudaError_t launch_softmax(const float* logits, int M, int V, const float* temp, float* probs, int32_t* err,
                            cudaStream_t s) {
   if (M <= 0) return cudaSuccess;
   const int groups = V / 4 + 2;
   int C = 1;
-  while (C < kSmMaxCTAs && (groups > 4 * kSmThreads * C || (long long)M * C < 128)) C *= 2;
+  while (C < kSmMaxCTAs && (groups > 8 * kSmThreads * C || (long long)M * C < 128)) C *= 2;
   while (C > 1 && groups <= kSmThreads / 2 * C) C /= 2;  // no CTA without work
   const int items = (groups + C * kSmThreads - 1) / (C * kSmThreads);
   auto go = [&](auto kern) {
@@ -211,7 +215,7 @@ cudaError_t launch_softmax(const float* logits, int M, int V, const float* temp,
     cfg.numAttrs = 2;
     return cudaLaunchKernelEx(&cfg, kern, logits, V, temp, probs, err);
   };
-  return items <= 2 ? go(softmax_kernel<2>) : items <= 4 ? go(softmax_kernel<4>) : items <= kSmItems ? go(softmax_kernel<kSmItems>) : go(softmax_kernel<0>);
+  return items <= 2 ? go(softmax_kernel<2>) : items <= 4 ? go(softmax_kernel<4>) : items <= 8 ? go(softmax_kernel<8>) : items <= kSmItems ? go(softmax_kernel<kSmItems>) : go(softmax_kernel<0>);
 }
 
 // ------------------------------------------------------------------ verification
