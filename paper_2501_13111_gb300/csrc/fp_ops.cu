@@ -211,6 +211,7 @@ int fp_op_rope_kv_chunk(const uint16_t* qkv, int row_stride, int n_tokens, int B
   if (!qkv || !rope_cs || !q_out || n_heads <= 0 || n_heads % kv->n_kv_heads != 0) return FP_ERR_INVALID_ARG;
   if (row_stride < (n_heads + 2LL * kv->n_kv_heads) * kv->head_dim || q_out_stride < (long long)n_heads * kv->head_dim)
     return FP_ERR_INVALID_ARG;
+  if (q_out == qkv && q_out_stride != row_stride) return FP_ERR_INVALID_ARG;  // rows would overlap others'
   if (row_stride % 8 || q_out_stride % 8 || !aligned16(qkv) || !aligned16(q_out) || !aligned16(rope_cs))
     return FP_ERR_UNSUPPORTED;
   return cuda_status(launch_rope_kv_chunk(qkv, row_stride, n_tokens, B, n_heads, *kv, cu, pos, rope_cs, q_out,

@@ -31,13 +31,14 @@ def code(call):
 
 
 def test_rope_kv_chunk_refusals(fp):
-    def call(kv=None, qkv=A, row=1024, n=4, B=2, H=4, cu=A, pos=A, cs=A, q=A, qs=512, **kw):
+    def call(kv=None, qkv=A, row=1024, n=4, B=2, H=4, cu=A, pos=A, cs=A, q=2 * A, qs=512, **kw):
         return code(lambda: fp.fp_op_rope_kv_chunk(qkv, row, n, B, H, kv or view(fp, **kw), cu, pos, cs, q, qs))
 
     for kw in (dict(qkv=None), dict(cu=None), dict(pos=None), dict(cs=None), dict(q=None), dict(n=-1), dict(B=-1),
                dict(H=3), dict(H=0), dict(row=1016), dict(qs=504), dict(kvq=2), dict(kvq=1), dict(k=None),
-               dict(table=None), dict(Hkv=0)):
+               dict(table=None), dict(Hkv=0), dict(q=A)):
         assert call(**kw) == INVALID, kw
+    assert call(q=A, qs=1024, n=0) == 0
     for kw in (dict(qkv=A + 8), dict(q=A + 2), dict(cs=A + 4), dict(row=1028), dict(qs=516), dict(hd=96), dict(page=32),
                dict(k=A + 8), dict(v=A + 8), dict(pages=1 << 26)):
         assert call(**kw) == UNSUPPORTED, kw

@@ -163,6 +163,34 @@ def test_attention_long_chunks(fp, kvq, hd, H, Hkv, seqs):
     c.check(q, got)
 
 
+@pytest.mark.parametrize("kvq,hd,H,Hkv,seqs", [
+    (0, 128, 8, 1, [(4, 30000)]),            # 59 CTAs share a unit of one tile
+    (1, 128, 8, 1, [(1, 20000), (2, 7)]),
+    (0, 128, 8, 1, [(64, 12000)]),           # two units of two tiles, 60 CTAs each
+    (1, 64, 3, 1, [(100, 9000)]),
+    (0, 64, 16, 2, [(3, 16000), (1, 15999)]),
+])
+def test_attention_units_that_many_ctas_share(fp, kvq, hd, H, Hkv, seqs):
+    """More parts of a unit than are added at once: groups of them, then the groups; the tickets are left at zero."""
+    c = Batch(fp, kvq, hd, H, Hkv, seqs, 61)
+    q = c.queries(14)
+    ws = empty(fp.fp_op_attention_chunk_workspace_bytes(c.B, H, Hkv, hd, c.max_new) + 256)
+    for _ in range(2):
+        got, err = c.attend(q, ws=ws)
+        assert err == 0
+        c.check(q, got)
+    off = -ptr(ws) % 256
+    assert not host(ws, np.uint8)[off:off + 65536].any()
+
+
+@pytest.mark.parametrize("kvq", [0, 1])
+def test_attention_of_no_rows(fp, kvq):
+    """Sequences without rows only, in a buffer that has some: nothing is written, nothing reported."""
+    c = Batch(fp, kvq, 128, 4, 2, [(0, 5), (0, 0), (0, 70)], 63, tail=6)
+    got, err = c.attend(c.queries(15), max_new=3)
+    assert err == 0 and np.all(got == 0x4321)
+
+
 @pytest.mark.parametrize("kvq", [0, 1])
 def test_attention_queries_inside_the_fused_rows(fp, kvq):
     """q read in place from QKV rows (a stride larger than the heads)."""
