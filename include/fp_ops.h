@@ -235,12 +235,14 @@ int fp_op_attention_prefill(const uint16_t* q, int q_stride, int B, int S, int n
  * they were.  cu and pos are read on the device, so one captured launch serves
  * other lengths within the same bounds.  A cu that decreases or leaves
  * [0, n_tokens] sets *err = 1 (err may be NULL) and no row outside the buffers is
- * touched (fp_op_attention_chunk: nothing is written).  All buffers 16-byte aligned and strides multiples of 8 elements, else
- * FP_ERR_UNSUPPORTED; pools of fewer than 2^31 rows. */
+ * touched (fp_op_attention_chunk: nothing is written).  All buffers are 16-byte
+ * aligned and strides multiples of 8 elements, else FP_ERR_UNSUPPORTED; pools hold
+ * fewer than 2^31 rows. */
 
 /* RoPE + KV-cache append of a chunk: as fp_op_rope_kv, for a ragged batch and
  * with the rotated queries to q_out bf16 [n_tokens][q_out_stride] (head h at
- * h*head_dim; q_out == qkv with the same stride rotates in place).  qkv bf16
+ * h*head_dim; q_out == qkv rotates in place and takes the same stride, else
+ * FP_ERR_INVALID_ARG).  qkv bf16
  * [n_tokens][row_stride]: H query heads, Hkv key heads, Hkv value heads.
  * Positions outside the cache set *err = 1 and skip the row, a page id outside
  * the pool sets *err = 1 and skips the row's cache writes.  Two rows must not
@@ -266,6 +268,12 @@ int fp_op_kv_read(const fp_kv_view* kv, int n_tokens, int B, const int32_t* cu, 
  * first max_new are left as they were, keys behind max_len are not read.  A row at
  * a negative position has no keys: zeros, and *err = 1.  A page id outside the
  * pool reads as zero keys and values and sets *err = 1.
+ * An int8 cache enters as its codes, exact in bf16, the scales multiplied in fp32;
+ * P is rounded to bf16.  Cache slots behind a sequence's last position may hold
+ * anything; its cached values, and an int8 cache's V scales, must be finite (a NaN
+ * or an infinity may reach rows before its position, in the same 128).
+ * Batches that could make more than 2^31 tiles of work, by n_tokens, B, the heads
+ * and max_len, are FP_ERR_UNSUPPORTED.
  * workspace: 256-byte aligned, at least
  * fp_op_attention_chunk_workspace_bytes(B, n_heads, n_kv_heads, head_dim, max_new)
  * bytes (0: a shape that is refused).  Its leading 64 KB hold ticket counters that
@@ -283,7 +291,8 @@ size_t fp_op_attention_chunk_workspace_bytes(int B, int n_heads, int n_kv_heads,
  * lowest index of the largest logit, else 0.  -inf masks a token; a row that
  * masks all of them gives zeros.  A NaN or +inf in a row with T > 0 gives NaN
  * throughout.  A T that is negative, infinite or NaN gives a row of zeros and
- * sets *err = 1 (err may be NULL).  probs may be logits. */
+ * sets *err = 1 (err may be NULL).  probs may be logits.  M to 2^27 and V to 2^30,
+ * else FP_ERR_UNSUPPORTED. */
 int fp_op_softmax(const float* logits, int M, int V, const float* temperature, float* probs, int32_t* err,
                   void* stream);
 
@@ -301,8 +310,9 @@ int fp_op_softmax(const float* logits, int M, int V, const float* temperature, f
  * out_tokens int32 [n_tokens]: rows 0 .. a-1 of the sequence the accepted drafts,
  * row a the drawn token, -1 behind it; n_out int32 [B]: a + 1 (0: a sequence
  * without rows).  A sum that is zero or not finite draws nothing: row a is -1,
- * n_out a, *err = 1 (err may be NULL).  A draft outside [0, V) is refused and sets *err = 1.
- * Sums and borders are as in fp64, whatever V. */
+ * n_out a, *err = 1 (err may be NULL).  A draft outside [0, V) is refused and sets
+ * *err = 1.  Sums are held in pairs of fp32 (48 bits).  V to 2^30 and B to
+ * 2^27, else FP_ERR_UNSUPPORTED. */
 int fp_op_verify_draft(const float* p, const float* q, int V, int n_tokens, int B, const int32_t* cu,
                        const int32_t* tokens, const float* u_accept, const float* u_draw, int32_t* out_tokens,
                        int32_t* n_out, int32_t* err, void* stream);

@@ -19,7 +19,8 @@
 //               that this CTA has of them: the last CTA to finish a unit adds its parts up;
 //   warp 8      TMA: the unit's Q tiles (one box per 64 columns: tokens x heads) and,
 //               page by page, the keys.  One box a page, in the order [8 rows][64
-//               columns] the descriptors step through;
+//               columns] the descriptors step through.  (int8 cache: it finds the pages
+//               of each tile instead, sends their codes on to L2, and stages the scales);
 //   warps 9, 10 issue the MMAs of a group each: O += P(t) V(t), then the group's next
 //               scores over the columns that P(t) has left.  (One warp for both groups
 //               left the tensor pipe idle for half of each step: a wait costs 100-200
@@ -27,12 +28,20 @@
 //               there were five in a row.)  Warp 9 owns the TMEM;
 //   warp 11     plans the CTA's stretch, describes its pieces of units to the others,
 //               and (bf16 cache) copies the values;
-//               (int8 cache: warp 8 finds the pages and sends them on to L2);
-//   warps 12-19 (int8 cache) K and V tiles from the codes: bf16(q s), the values that
-//               fp_op_kv_read returns (a byte permute gives fp32 2^15 + 128 + q, an exact
-//               subtraction q; 2^-8 of a value, as a bf16 cache's own rounding).
+//   warps 12-19 (int8 cache) K and V tiles of the codes as bf16, exact (a byte permute
+//               gives fp32 2^15 + 128 + q, a subtraction q).  A key's K scale multiplies
+//               its score column, its V scale its column of P, both in fp32.  (Tiles of
+//               bf16(q s) took 54 us where this takes 62, 420 where 507, see below, but
+//               were twice as far from the sums in 64 bits, 0.0040 against 0.0023.)
+// Measured (launches in a graph, device time): 32 sequences of 5 rows, 32 heads of 128, at
+// positions to 2100, bf16 cache 23.8 us (2.6 TB/s of its keys and values); 32 of 5, 64 heads
+// over 8, positions to 4096, int8 62 us; chunks of 512 to 2048 rows, 40 heads, bf16 80 us
+// (718 TFLOP/s); of 64 heads over 8, int8 507 us (797 TFLOP/s).  A pair of tiles takes
+// about 4000 cycles where its MMAs need 2080: the scores of a group wait for its P, and P for
+// its scores, and what is in between (tensor memory to registers twice, 128 exponentials
+// a thread) is as long as the other group's products.
 // Slots behind the sequence's last position may hold anything: their scores are
-// masked, their V rows are zeroed before the product.
+// masked, their V rows are zeroed before the product (int8 cache: read as zeros).
 // Every wait on an mbarrier is bounded (error 2 past the limit).
 #include <algorithm>
 #include <type_traits>
@@ -52,7 +61,10 @@ constexpr int ck_threads() { return KV8 ? (kCkWarpWiden + kCkWiden) * 32 : 384; 
 // with 96, moved to the softmax: 256 x 120 + 384 x 80 = 640 x 96
 constexpr int kCkReaders = kCkSoft + 3;           // warps that read each piece's description: softmax, Q, MMA
 constexpr int kCkPieces = 4;                      // pieces described ahead
-constexpr int kCkAhead = 8;                       // int8 cache: key tiles whose pages are known ahead
+constexpr int kCkAhead = 4;                       // int8 cache: key tiles whose pages are known ahead
+constexpr int kCkScales = 8;                      // tiles of scales: a tile is described once the widening of
+                                                  // the one kCkAhead before it is over, which P V of the second
+                                                  // tile before that preceded: the eighth before it is done with
 constexpr int kCkRing = 2;                        // K tiles in shared memory, and V tiles
 constexpr uint32_t kCkTmemCols = 512, kCkO = 256; // O of group j at kCkO + 128 j, its scores at 128 j
 constexpr int kCkStage = 32 * 64;                 // a warp's 32 output rows, 32 columns at a time
@@ -282,6 +294,7 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
   __shared__ CkPiece s_left[2];                  // units that other CTAs have a part of
   __shared__ int abort_word, s_last[2];
   __shared__ int2 s_page[KV8 ? kCkAhead : 1][8];  // int8: pool row of a tile's pages, and how many of their rows count
+  __shared__ __align__(16) float s_scale[KV8 ? kCkScales : 1][2][kCkKeys];  // int8: K's (by hd^-1/2 log2 e) and V's
   volatile int* abort_flag = &abort_word;
   uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
   uint8_t* sQ = smem;
@@ -367,26 +380,45 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
           if (lane >= 8 || t >= w.t1 || key0 >= w.end) return -1;
           return __ldg(pt + key0 / 16);
         };
-        int id = page(w.t0);
-        for (int t = w.t0; t < w.t1; ++t, ++kn) {
-          const int s = kn % kCkAhead, id1 = page(t + 1), count = w.end - t * kCkKeys - lane * 16;
-          int at = -1;
+        int id = page(w.t0), at, rows;
+        float ks[4], vs[4];
+        // a tile's pages to L2, and its scales on their way: four keys' a lane, 0 for rows
+        // that do not count
+        auto fetch = [&](int t) {
+          const int count = w.end - t * kCkKeys - lane * 16;
+          at = -1;
           if (id >= 0 && id < a.n_pages) {
             at = (id * a.Hkv + w.kvh) * 16;
             asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(a.k8 + (long long)at * HD), "n"(16 * HD) : "memory");
             asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(a.v8 + (long long)at * HD), "n"(16 * HD) : "memory");
-            asm volatile("prefetch.global.L2 [%0];" ::"l"(a.k_scale + at) : "memory");
-            asm volatile("prefetch.global.L2 [%0];" ::"l"(a.v_scale + at) : "memory");
           } else if (lane < 8 && count > 0 && a.err) {
             atomicExch(a.err, 1);
           }
+          rows = at < 0 ? 0 : min(16, max(0, count));
+          const int first = __shfl_sync(0xffffffffu, at, lane >> 2) + (lane & 3) * 4;
+          const int on = __shfl_sync(0xffffffffu, rows, lane >> 2) - (lane & 3) * 4;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            ks[i] = i < on ? __ldg(a.k_scale + first + i) : 0.f;
+            vs[i] = i < on ? __ldg(a.v_scale + first + i) : 0.f;
+          }
+        };
+        fetch(w.t0);
+        id = page(w.t0 + 1);
+        for (int t = w.t0; t < w.t1; ++t, ++kn) {
+          const int s = kn % kCkAhead;
+          const float c = kPaLog2e * rsqrtf((float)HD);
+          const float4 kf = make_float4(ks[0] * c, ks[1] * c, ks[2] * c, ks[3] * c), vf = make_float4(vs[0], vs[1], vs[2], vs[3]);
+          const int2 page_rows = make_int2(at, rows);
+          if (t + 1 < w.t1) fetch(t + 1), id = page(t + 2);
           if (kn >= kCkAhead) ok = mbar_wait(&bar.iempty[s], ((kn / kCkAhead) & 1) ^ 1);
           ok = __all_sync(0xffffffffu, ok && !*abort_flag);
           if (!ok) return;
-          if (lane < 8) s_page[s][lane] = make_int2(at, at < 0 ? 0 : min(16, max(0, count)));
+          *reinterpret_cast<float4*>(&s_scale[kn % kCkScales][0][lane * 4]) = kf;
+          *reinterpret_cast<float4*>(&s_scale[kn % kCkScales][1][lane * 4]) = vf;
+          if (lane < 8) s_page[s][lane] = page_rows;
           __syncwarp();
           if (lane == 0) mbar_arrive(&bar.ifull[s]);
-          id = id1;
           if (t == w.t0) queries();
           if (!ok) return;
         }
@@ -584,8 +616,8 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
     if (warp == kCkWarpMma) role(std::integral_constant<int, 0>());
     else role(std::integral_constant<int, 1>());
   } else if (KV8 && warp >= kCkWarpWiden) {
-    // ---------------- int8 cache: bf16(q s) of the key tiles' rows, four warps for K and
-    // four for V.  Thread: 16 codes (chunk c) of every PER-th row.  Each register of codes
+    // ---------------- int8 cache: the codes of the key tiles' rows as bf16, four warps for K
+    // and four for V.  Thread: 16 codes (chunk c) of every PER-th row.  Each register of codes
     // is filled again, for the next tile, as soon as it has been written out: a whole
     // tile's codes, 32 KB an SM, are in flight throughout, across pieces too.
     constexpr int C = HD / 16;                                      // chunks a row
@@ -595,12 +627,10 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
     const int wi = threadIdx.x % (16 * kCkWiden), c = C == 4 ? wi & 3 : (wi & 3) | (wi >> 1 & 4);
     const int rr = C == 4 ? wi >> 2 : (wi >> 4) * 2 + (wi >> 2 & 1);
     const int8_t* pool = (is_v ? a.v8 : a.k8) + c * 16;
-    const float* scale = is_v ? a.v_scale : a.k_scale;
     uint64_t *full = is_v ? bar.vfull : bar.kfull, *empty = is_v ? bar.vempty : bar.kempty;
     uint8_t* tiles = (is_v ? sV : sK) + (rr >> 3) * SBO + (c >> 2) * 1024 + (rr & 7) * 128;
     const int o0 = ((2 * (c & 3)) ^ (rr & 7)) << 4, o1 = ((2 * (c & 3) + 1) ^ (rr & 7)) << 4;
     uint4 cw[N];
-    float sc[N];
     int row[N];  // pool rows (fewer than 2^31) of the tile to be read; -1 reads zeros
     bool ok = true;
     // this thread's rows of tile k; false: there is none (or a wait ran out)
@@ -618,7 +648,6 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
     };
     auto fetch = [&](int i) {
       cw[i] = row[i] >= 0 ? ld_nc16(pool + (long long)row[i] * HD) : make_uint4(0, 0, 0, 0);
-      sc[i] = row[i] >= 0 ? __ldg(scale + row[i]) : 0.f;
     };
     bool more = rows(0);
 #pragma unroll
@@ -631,14 +660,14 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         const uint32_t ww[4] = {cw[i].x ^ 0x80808080u, cw[i].y ^ 0x80808080u, cw[i].z ^ 0x80808080u, cw[i].w ^ 0x80808080u};
-        const float2 s2 = make_float2(sc[i], sc[i]), z2 = make_float2(-32896.f, -32896.f);
+        const float2 z2 = make_float2(-32896.f, -32896.f);
         uint32_t o[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {  // codes 2j, 2j + 1: fp32 2^15 + 128 + q
           const uint32_t u = ww[j >> 1];
           const float lo = __uint_as_float(__byte_perm(u, 0x47000000u, (j & 1) ? 0x7424 : 0x7404));
           const float hi = __uint_as_float(__byte_perm(u, 0x47000000u, (j & 1) ? 0x7434 : 0x7414));
-          const float2 f = ck_mul2(ck_add2(make_float2(lo, hi), z2), s2);
+          const float2 f = ck_add2(make_float2(lo, hi), z2);
           o[j] = pa_pack(f.x, f.y);
         }
         uint8_t* rp = tiles + s * TILE + i * (PER / 8 * SBO);
@@ -663,7 +692,7 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
     const float scale = kPaLog2e * rsqrtf((float)HD);
     const int tok = row / a.G;  // of a tile's packed rows
     const bool packed = row < a.tile_tokens * a.G;
-    int sn = 0, on[2] = {0, 0}, mn = 0, left = 0;
+    int sn = 0, on[2] = {0, 0}, mn = 0, left = 0, kb = 0;  // kb: key tiles of the pieces before
     bool ok = true;
     uint8_t* stage = sV + R * TILE + warp * kCkStage;
     constexpr size_t ML = (size_t)kCkRows * HD * 4;
@@ -753,9 +782,19 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
         const bool masked = (t + 1) * kCkKeys > lim0;
         const int seen = lim - t * kCkKeys;  // keys of this tile that are the row's
         float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-        auto maximum = [&](auto cut, int x0) {
+        const float(*scales)[kCkKeys] = s_scale[KV8 ? (kb + t - w.t0) % kCkScales : 0];
+        auto maximum = [&](auto cut, int x0) {  // of 32 scores; int8 cache: times their keys' K scales
           float v[32];
           tc_ld<32>(ts + x0, reinterpret_cast<uint32_t*>(v));
+          if constexpr (KV8) {
+#pragma unroll
+            for (int x = 0; x < 32; x += 4) {
+              const float4 f = *reinterpret_cast<const float4*>(&scales[0][x0 + x]);
+              const float2 p = ck_mul2(make_float2(v[x], v[x + 1]), make_float2(f.x, f.y));
+              const float2 q = ck_mul2(make_float2(v[x + 2], v[x + 3]), make_float2(f.z, f.w));
+              v[x] = p.x, v[x + 1] = p.y, v[x + 2] = q.x, v[x + 3] = q.y;
+            }
+          }
           if constexpr (decltype(cut)::value) {
 #pragma unroll
             for (int x = 0; x < 32; ++x)
@@ -773,7 +812,7 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
 #pragma unroll 1
           for (int x0 = 0; x0 < kCkKeys; x0 += 32) maximum(std::false_type(), x0);
         }
-        const float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * scale;
+        const float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * (KV8 ? 1.f : scale);
         // move the reference when the tile would exceed it by more than 2^kCkSlack
         float corr = 1.f;
         if (mx > m + kCkSlack) {
@@ -794,27 +833,29 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
           }
         }
         const float mref = m == -INFINITY ? 0.f : m;
-        const float2 sc2 = make_float2(scale, scale), nm2 = make_float2(-mref, -mref);
-        auto weights = [&](auto cut, int x0) {  // P of 32 keys
+        const float2 nm2 = make_float2(-mref, -mref);
+        auto weights = [&](auto cut, int x0) {  // P of 32 keys (int8 cache: times their V scales)
           float v[32];
           tc_ld<32>(ts + x0, reinterpret_cast<uint32_t*>(v));
-          if constexpr (decltype(cut)::value) {
+          uint32_t pw[16];
 #pragma unroll
-            for (int x = 0; x < 32; ++x)
-              if (x0 + x >= seen) v[x] = -INFINITY;
-          }
+          for (int x = 0; x < 32; x += 4) {
+            const float4 kf = KV8 ? *reinterpret_cast<const float4*>(&scales[0][x0 + x]) : make_float4(scale, scale, scale, scale);
+            const float4 vf = KV8 ? *reinterpret_cast<const float4*>(&scales[1][x0 + x]) : make_float4(1.f, 1.f, 1.f, 1.f);
 #pragma unroll
-          for (int y = 0; y < 32; y += 32) {
-            uint32_t pw[16];
-#pragma unroll
-            for (int x = 0; x < 32; x += 2) {
-              const float2 e = ck_fma2(make_float2(v[y + x], v[y + x + 1]), sc2, nm2);
-              const float2 p = make_float2(pa_ex2(e.x), pa_ex2(e.y));
-              l2[(x >> 1) & 3] = ck_add2(l2[(x >> 1) & 3], p);
-              pw[x / 2] = pa_pack(p.x, p.y);
+            for (int y = 0; y < 4; y += 2) {
+              float2 e = ck_fma2(make_float2(v[x + y], v[x + y + 1]), y ? make_float2(kf.z, kf.w) : make_float2(kf.x, kf.y), nm2);
+              if constexpr (decltype(cut)::value) {  // masked ones -inf
+                e.x = x0 + x + y < seen ? e.x : -INFINITY;
+                e.y = x0 + x + y + 1 < seen ? e.y : -INFINITY;
+              }
+              float2 p = make_float2(pa_ex2(e.x), pa_ex2(e.y));
+              l2[(x + y) / 2 % 4] = ck_add2(l2[(x + y) / 2 % 4], p);
+              if constexpr (KV8) p = ck_mul2(p, y ? make_float2(vf.z, vf.w) : make_float2(vf.x, vf.y));
+              pw[(x + y) / 2] = pa_pack(p.x, p.y);
             }
-            tc_st16(ts + (x0 & 64) + ((x0 + y) & 32) / 2, pw);
           }
+          tc_st16(ts + (x0 & 64) + (x0 & 32) / 2, pw);
           if ((x0 + 32) % 64 == 0) {  // a half is done
             tc_wait_st();
             tc_fence_before();
@@ -832,6 +873,7 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
       }
       if (!ok) break;
       float l = ((l2[0].x + l2[0].y) + (l2[1].x + l2[1].y)) + ((l2[2].x + l2[2].y) + (l2[3].x + l2[3].y));
+      kb += max(0, w.t1 - w.t0);
       // ---- the piece's output
       const bool whole = w.first() && w.last(), empty = w.empty();
       const bool use0 = w.uses(0), use1 = w.uses(1);

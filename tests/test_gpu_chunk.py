@@ -2,8 +2,8 @@
 
 Tolerance of the attention, element by element, with u = 2^-8 (bf16's half step): the output's own rounding,
 u |o|; the probabilities' rounding before the second product, at most u sum_j p_j |v_j|; scores in fp32 (128 products
-of at most 4 with a scale of hd^-1/2) move a probability by less than 2^-10.  An int8 cache's keys and values are what
-reading it back gives, bf16(code * scale).  So
+of at most 4 with a scale of hd^-1/2) move a probability by less than 2^-10.  An int8 cache's codes are exact in bf16,
+its scales multiply in fp32.  So
     |got - o| <= 2^-8 |o| + (2^-8 + 2^-10) sum_j p_j |v_j|.
 """
 import numpy as np
@@ -77,10 +77,8 @@ class Batch:
         bad = (page < 0) | (page >= self.pages)
         page, slot = np.where(bad, 0, page), t % 16
         x = self.data[w][page, :, slot]
-        if self.kvq:
-            with np.errstate(all="ignore"):
-                x = synth.f32_to_bf16_bits(x.astype(np.float32) * self.data[w + "s"][page, :, slot][..., None])
-        x = quant.bf16_to_f32(x).astype(np.float64)
+        x = quant.bf16_to_f32(x).astype(np.float64) if self.kvq == 0 else \
+            x.astype(np.float64) * self.data[w + "s"][page, :, slot].astype(np.float64)[..., None]
         x[bad] = 0.0
         return x
 
