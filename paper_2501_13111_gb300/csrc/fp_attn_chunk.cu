@@ -31,15 +31,16 @@
 //   warps 12-19 (int8 cache) K and V tiles of the codes as bf16, exact (a byte permute
 //               gives fp32 2^15 + 128 + q, a subtraction q).  A key's K scale multiplies
 //               its score column, its V scale its column of P, both in fp32.  (Tiles of
-//               bf16(q s) took 54 us where this takes 62, 420 where 507, see below, but
-//               were twice as far from the sums in 64 bits, 0.0040 against 0.0023.)
-// Measured (launches in a graph, device time): 32 sequences of 5 rows, 32 heads of 128, at
-// positions to 2100, bf16 cache 23.8 us (2.6 TB/s of its keys and values); 32 of 5, 64 heads
-// over 8, positions to 4096, int8 62 us; chunks of 512 to 2048 rows, 40 heads, bf16 80 us
-// (718 TFLOP/s); of 64 heads over 8, int8 507 us (797 TFLOP/s).  A pair of tiles takes
-// about 4000 cycles where its MMAs need 2080: the scores of a group wait for its P, and P for
-// its scores, and what is in between (tensor memory to registers twice, 128 exponentials
-// a thread) is as long as the other group's products.
+//               bf16(q s) took 54 us where this takes 63, 420 where 507, see below, but
+//               were further from the sums in 64 bits: 0.0040 against 0.0024, relative.)
+// Measured (launches in a graph, heads of 128): 8 sequences of 5 rows to position 612, 32
+// heads, bf16 cache 23.6 us (2.6 TB/s); 32 of 5 rows to 2148, 64 heads on 8, int8 63 us
+// (1.8 TB/s); 4 chunks of 512 rows to 2048, 40 heads, bf16 80 us (714 TFLOP/s); 2 of 1024
+// rows to 8000, 64 heads on 8, int8 507 us (797 TFLOP/s).  A step of two query tiles takes
+// about 4000 cycles where its MMAs need 2080: a group's scores wait for its P, P for the
+// scores, and what is in between (tensor memory to registers twice, 128 exponentials a
+// thread) is as long as the other group's products.  Small batches: about 7000 cycles
+// pass before the first scores and 8000 behind the last.
 // Slots behind the sequence's last position may hold anything: their scores are
 // masked, their V rows are zeroed before the product (int8 cache: read as zeros).
 // Every wait on an mbarrier is bounded (error 2 past the limit).

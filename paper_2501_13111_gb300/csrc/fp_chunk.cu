@@ -45,8 +45,9 @@ FP_DEV uint2 codes8(const float* x, float s) {
 // to their page, an int8 row as q = rint(x / s) with s = max|x| / 127.  One CTA a
 // token: HD / 16 lanes hold a head, 16 bytes of each half, so that a rotated pair
 // and (by shuffles among those lanes) a row's maximum stay in the warp, and each
-// lane reads its cosines once for all heads.  Bound by bytes: qkv in, queries and
-// cache rows out.
+// lane reads its cosines once for all heads.  Bound by bytes (qkv in, queries and
+// cache rows out) for many rows, by latency for few: with the read back below, chunks of
+// 4 x up to 1000 rows of 40 heads take 68 us (5.1 TB/s), 160 rows of 64 heads on 8, int8, 7.4.
 template <int HD, bool KV8>
 __global__ void __launch_bounds__(256)
     rope_kv_chunk_kernel(const uint16_t* qkv, int row_stride, int n_tokens, int B, int H, fp_kv_view kv,
