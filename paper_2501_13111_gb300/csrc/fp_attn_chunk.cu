@@ -12,10 +12,10 @@
 // and its output accumulator.
 //   warps 0-7   softmax, two groups of 4: one query row (TMEM lane) a thread.
 //               P = 2^(s - m) is rounded to bf16 for the second product (2^-8 of each
-//               p, the sums in fp32); the reference m moves only when a tile passes it
-//               by 2^8 (O and the row sum are rescaled then).  P goes out in two halves
-//               of 64 keys, so that the first half's products run while the second
-//               half is computed.  At the end of a piece they write its rows, or the part
+//               p, the sums in fp32), 64 keys at a time from registers, so that the first
+//               half's products run while the second half is computed; the reference m
+//               moves only when a half passes it by 2^8 (O and the row sum are rescaled
+//               then).  At the end of a piece they write its rows, or the part
 //               that this CTA has of them: the last CTA to finish a unit adds its parts up;
 //   warp 8      TMA: the unit's Q tiles (one box per 64 columns: tokens x heads) and,
 //               page by page, the keys.  One box a page, in the order [8 rows][64
@@ -31,15 +31,16 @@
 //   warps 12-19 (int8 cache) K and V tiles of the codes as bf16, exact (a byte permute
 //               gives fp32 2^15 + 128 + q, a subtraction q).  A key's K scale multiplies
 //               its score column, its V scale its column of P, both in fp32.  (Tiles of
-//               bf16(q s) took 54 us where this takes 63, 420 where 507, see below, but
+//               bf16(q s) took 54 us where this takes 63, 420 where 496, see below, but
 //               were further from the sums in 64 bits: 0.0040 against 0.0024, relative.)
 // Measured (launches in a graph, heads of 128): 8 sequences of 5 rows to position 612, 32
 // heads, bf16 cache 23.6 us (2.6 TB/s); 32 of 5 rows to 2148, 64 heads on 8, int8 63 us
-// (1.8 TB/s); 4 chunks of 512 rows to 2048, 40 heads, bf16 80 us (714 TFLOP/s); 2 of 1024
-// rows to 8000, 64 heads on 8, int8 507 us (797 TFLOP/s).  A step of two query tiles takes
-// about 4000 cycles where its MMAs need 2080: a group's scores wait for its P, P for the
-// scores, and what is in between (tensor memory to registers twice, 128 exponentials a
-// thread) is as long as the other group's products.  Small batches: about 7000 cycles
+// (1.8 TB/s); 4 chunks of 512 rows to 2048, 40 heads, bf16 77 us (744 TFLOP/s); 2 of 1024
+// rows to 8000, 64 heads on 8, int8 496 us (814 TFLOP/s).  A step of two query tiles takes
+// about 3800 cycles where its MMAs need 2080: a group's scores wait for its P, P for the
+// scores, and what is in between is as long as the other group's products; with an int8
+// cache the scales' way from shared memory, which the MMAs keep busy, comes on top (chunk
+// int8 406 us with constants instead).  Small batches: about 7000 cycles
 // pass before the first scores and 8000 behind the last.
 // Slots behind the sequence's last position may hold anything: their scores are
 // masked, their V rows are zeroed before the product (int8 cache: read as zeros).
@@ -59,7 +60,8 @@ constexpr int kCkWarpQ = 8, kCkWarpMma = 9, kCkWarpPlan = 11, kCkWarpWiden = 12,
 template <bool KV8>
 constexpr int ck_threads() { return KV8 ? (kCkWarpWiden + kCkWiden) * 32 : 384; }
 // Registers a thread: 384 threads may have 168, which none needs; 640 (int8 cache) launch
-// with 96, moved to the softmax: 256 x 120 + 384 x 80 = 640 x 96
+// with 96, moved to the softmax: 256 x 128 + 384 x 72 < 640 x 96 (with 120 and 80 its row
+// spills more: chunk int8 504 us against 496)
 constexpr int kCkReaders = kCkSoft + 3;           // warps that read each piece's description: softmax, Q, MMA
 constexpr int kCkPieces = 4;                      // pieces described ahead
 constexpr int kCkAhead = 4;                       // int8 cache: key tiles whose pages are known ahead
@@ -285,7 +287,7 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
   constexpr int TILE = ck_tile_bytes<HD>(), NH = HD / 64, SBO = NH * 1024, PAGE = 2 * SBO, R = kCkRing;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   struct Bars {
-    uint64_t kfull[R], vfull[R], kempty[R], vempty[R], qfull, qempty, sfull[2], pfull[2][2], ofull[2], oempty[2], part[2], join, met[4],
+    uint64_t kfull[R], vfull[R], kempty[R], vempty[R], qfull, qempty, sfull[2], hdone[2], pfull[2][2], ofull[2], oempty[2], part[2], join, met[4],
         mma, dfull[kCkPieces], dempty[kCkPieces], done[2], ifull[kCkAhead], iempty[kCkAhead];
   };
   __shared__ Bars bar;
@@ -344,7 +346,7 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
     return !w.done();
   };
 
-  if (KV8 && warp >= kCkSoft) asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+  if (KV8 && warp >= kCkSoft) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
   if (warp == kCkWarpPlan || warp == kCkWarpQ) {
     // ---------------- warp 11: the plan, the pieces, V.  Warp 8: Q tiles and K.  Lanes
     // 0-7 copy a page of a key tile each; the next tile's page ids are read while this
@@ -580,30 +582,35 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
             fence_proxy_async();
           }
           if (more) ok = ok && mbar_wait(&bar.kfull[s1], ((kn + i + di) / R) & 1);
-          ok = __all_sync(0xffffffffu, ok && mbar_wait(&bar.pfull[j][0], pn & 1)) && !*abort_flag;
-          ok = __all_sync(0xffffffffu, ok);
-          if (!ok) break;
-          tc_fence_after();
-          const int u = uniform(s), first = uniform(i == i0);
-          if (elect_one()) values(u, 0, first);
-          __syncwarp();
-          ok = __all_sync(0xffffffffu, mbar_wait(&bar.pfull[j][1], pn & 1));
+          const int u = uniform(s), u1 = uniform(s1), first = uniform(i == i0);
+          // a half of the keys: P V, then the next tile's scores over the columns that P leaves
+          auto half = [&](auto ch) {
+            constexpr int h = decltype(ch)::value;
+            ok = __all_sync(0xffffffffu, ok && mbar_wait(&bar.pfull[j][h], pn & 1)) && !*abort_flag;
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) return;
+            tc_fence_after();
+            if (elect_one()) {
+              values(u, h, h == 0 && first);
+              if (h == 0) {
+                tc_commit(&bar.hdone[j]);
+              } else {
+                release(&bar.vempty[s], alone(i));
+                if (more) {
+                  scores(q, u1);
+                  release(&bar.kempty[s1], alone(i + di));
+                  if (i + 2 * di >= i1) release(&bar.qempty, q_alone);
+                } else {
+                  tc_commit(&bar.ofull[j]);
+                }
+              }
+            }
+            __syncwarp();
+          };
+          half(std::integral_constant<int, 0>());
+          half(std::integral_constant<int, 1>());
           if (!ok) break;
           ++pn;
-          tc_fence_after();
-          const int u1 = uniform(s1);
-          if (elect_one()) {
-            values(u, 1, false);
-            release(&bar.vempty[s], alone(i));
-            if (more) {
-              scores(q, u1);
-              release(&bar.kempty[s1], alone(i + di));
-              if (i + 2 * di >= i1) release(&bar.qempty, q_alone);
-            } else {
-              tc_commit(&bar.ofull[j]);
-            }
-          }
-          __syncwarp();
         }
         if (!ok) break;
         on += i0 < i1;
@@ -686,14 +693,14 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
     if (!ok && lane == 0) fail();
   } else if (warp < kCkSoft) {
     // ---------------- softmax: group j, row 32 quad + lane (TMEM begins at column 0)
-    if (KV8) asm volatile("setmaxnreg.inc.sync.aligned.u32 120;");
+    if (KV8) asm volatile("setmaxnreg.inc.sync.aligned.u32 128;");
     const int j = warp >> 2, quad = warp & 3, row = quad * 32 + lane;
     const uint32_t lane_base = (uint32_t)(quad * 32) << 16;
     const uint32_t ts = lane_base + j * kCkKeys, to = lane_base + kCkO + j * 128;
     const float scale = kPaLog2e * rsqrtf((float)HD);
     const int tok = row / a.G;  // of a tile's packed rows
     const bool packed = row < a.tile_tokens * a.G;
-    int sn = 0, on[2] = {0, 0}, mn = 0, left = 0, kb = 0;  // kb: key tiles of the pieces before
+    int sn = 0, on[2] = {0, 0}, mn = 0, left = 0, kb = 0;
     bool ok = true;
     uint8_t* stage = sV + R * TILE + warp * kCkStage;
     constexpr size_t ML = (size_t)kCkRows * HD * 4;
@@ -768,108 +775,99 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
       float2 l2[4];         // row sum
 #pragma unroll
       for (int y = 0; y < 4; ++y) l2[y] = make_float2(0.f, 0.f);
-      for (int t = t_first; t < t_end; t += stride, ++sn) {
-        ok = __all_sync(0xffffffffu, mbar_wait(&bar.sfull[j], sn & 1));
-        if (!ok) break;
-        if (behind && t > t_first) ticket();
-        if (!on_warp) {
-          if (lane < 2) mbar_arrive(&bar.pfull[j][lane]);
-          continue;
-        }
-        tc_fence_after();
-        // Twice over the scores, rolled up: unrolled over a row held in registers, this
-        // loop, the issuers' and the widening ones were more than the instruction caches
-        // hold, and waiting for instructions the first of the stalls.
-        const bool masked = (t + 1) * kCkKeys > lim0;
-        const int seen = lim - t * kCkKeys;  // keys of this tile that are the row's
-        float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-        const float(*scales)[kCkKeys] = s_scale[KV8 ? (kb + t - w.t0) % kCkScales : 0];
-        auto maximum = [&](auto cut, int x0) {  // of 32 scores; int8 cache: times their keys' K scales
-          float v[32];
-          tc_ld<32>(ts + x0, reinterpret_cast<uint32_t*>(v));
+      // Half a tile of keys at a time: while one half's scores are here, the products of
+      // the other run.
+#pragma unroll 1
+      for (int t = t_first; t < t_end && ok; t += stride, ++sn) {
+#pragma unroll 1
+        for (int h = 0; h < 2; ++h) {
+          if (h == 0) {
+            ok = __all_sync(0xffffffffu, mbar_wait(&bar.sfull[j], sn & 1));
+            if (!ok) break;
+            if (behind && t > t_first) ticket();
+          }
+          if (!on_warp) {
+            if (lane == 0) mbar_arrive(&bar.pfull[j][h]);
+            continue;
+          }
+          tc_fence_after();
+          // The 64 scores stay in registers, the loop over the halves is rolled: the maximum
+          // of all 128 first, and the scores read again, took 80 us where this takes 77
+          // (chunk bf16); all 128 in registers, this loop, the issuers' and the widening ones
+          // were more than the instruction caches hold.
+          const int key0 = t * kCkKeys + h * 64, seen = lim - key0;  // keys of this half that are the row's
+          const bool masked = key0 + 64 > lim0;
+          const uint32_t tsh = ts + h * 64;
+          const float* sc = KV8 ? &s_scale[(kb + t - w.t0) % kCkScales][0][h * 64] : nullptr;  // (V's kCkKeys on)
+          float v[64];  // scores (int8 cache: times their keys' K scales)
+          tc_ld<64>(tsh, reinterpret_cast<uint32_t*>(v));
           if constexpr (KV8) {
 #pragma unroll
-            for (int x = 0; x < 32; x += 4) {
-              const float4 f = *reinterpret_cast<const float4*>(&scales[0][x0 + x]);
+            for (int x = 0; x < 64; x += 4) {
+              const float4 f = *reinterpret_cast<const float4*>(sc + x);
               const float2 p = ck_mul2(make_float2(v[x], v[x + 1]), make_float2(f.x, f.y));
               const float2 q = ck_mul2(make_float2(v[x + 2], v[x + 3]), make_float2(f.z, f.w));
               v[x] = p.x, v[x + 1] = p.y, v[x + 2] = q.x, v[x + 3] = q.y;
             }
           }
-          if constexpr (decltype(cut)::value) {
+          if (masked) {
 #pragma unroll
-            for (int x = 0; x < 32; ++x)
-              if (x0 + x >= seen) v[x] = -INFINITY;
+            for (int x = 0; x < 64; ++x)
+              if (x >= seen) v[x] = -INFINITY;
           }
+          float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-          for (int x = 0; x < 32; x += 8)
+          for (int x = 0; x < 64; x += 8)
 #pragma unroll
             for (int y = 0; y < 4; ++y) m4[y] = ck_max3(m4[y], v[x + 2 * y], v[x + 2 * y + 1]);
-        };
-        if (masked) {
-#pragma unroll 1
-          for (int x0 = 0; x0 < kCkKeys; x0 += 32) maximum(std::true_type(), x0);
-        } else {
-#pragma unroll 1
-          for (int x0 = 0; x0 < kCkKeys; x0 += 32) maximum(std::false_type(), x0);
-        }
-        const float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * (KV8 ? 1.f : scale);
-        // move the reference when the tile would exceed it by more than 2^kCkSlack
-        float corr = 1.f;
-        if (mx > m + kCkSlack) {
-          corr = exp2f(m - mx);  // 0 on the first tile
-          m = mx;
+          const float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * (KV8 ? 1.f : scale);
+          // move the reference when the tile would exceed it by more than 2^kCkSlack
+          float corr = 1.f;
+          if (mx > m + kCkSlack) {
+            corr = exp2f(m - mx);  // 0 on the first tile
+            m = mx;
 #pragma unroll
-          for (int y = 0; y < 4; ++y) l2[y] = ck_mul2(l2[y], make_float2(corr, corr));
-        }
-        if (t > t_first && __any_sync(0xffffffffu, corr != 1.f)) {
-          // O holds P V of the earlier tiles (complete: S(t) was issued after it)
-#pragma unroll 1
-          for (int x = 0; x < HD; x += 16) {
-            uint32_t o[16];
-            tc_ld<16>(to + x, o);
-#pragma unroll
-            for (int y = 0; y < 16; ++y) o[y] = __float_as_uint(__uint_as_float(o[y]) * corr);
-            tc_st16(to + x, o);
+            for (int y = 0; y < 4; ++y) l2[y] = ck_mul2(l2[y], make_float2(corr, corr));
           }
-        }
-        const float mref = m == -INFINITY ? 0.f : m;
-        const float2 nm2 = make_float2(-mref, -mref);
-        auto weights = [&](auto cut, int x0) {  // P of 32 keys (int8 cache: times their V scales)
-          float v[32];
-          tc_ld<32>(ts + x0, reinterpret_cast<uint32_t*>(v));
-          uint32_t pw[16];
+          if ((h || t > t_first) && __any_sync(0xffffffffu, corr != 1.f)) {
+            // O holds P V of the halves before: those of earlier tiles are complete (this one's
+            // scores were issued after them)
+            if (h) ok = __all_sync(0xffffffffu, mbar_wait(&bar.hdone[j], sn & 1));
+            if (!ok) break;
+            tc_fence_after();
+#pragma unroll 1
+            for (int x = 0; x < HD; x += 16) {
+              uint32_t o[16];
+              tc_ld<16>(to + x, o);
 #pragma unroll
-          for (int x = 0; x < 32; x += 4) {
-            const float4 kf = KV8 ? *reinterpret_cast<const float4*>(&scales[0][x0 + x]) : make_float4(scale, scale, scale, scale);
-            const float4 vf = KV8 ? *reinterpret_cast<const float4*>(&scales[1][x0 + x]) : make_float4(1.f, 1.f, 1.f, 1.f);
-#pragma unroll
-            for (int y = 0; y < 4; y += 2) {
-              float2 e = ck_fma2(make_float2(v[x + y], v[x + y + 1]), y ? make_float2(kf.z, kf.w) : make_float2(kf.x, kf.y), nm2);
-              if constexpr (decltype(cut)::value) {  // masked ones -inf
-                e.x = x0 + x + y < seen ? e.x : -INFINITY;
-                e.y = x0 + x + y + 1 < seen ? e.y : -INFINITY;
-              }
-              float2 p = make_float2(pa_ex2(e.x), pa_ex2(e.y));
-              l2[(x + y) / 2 % 4] = ck_add2(l2[(x + y) / 2 % 4], p);
-              if constexpr (KV8) p = ck_mul2(p, y ? make_float2(vf.z, vf.w) : make_float2(vf.x, vf.y));
-              pw[(x + y) / 2] = pa_pack(p.x, p.y);
+              for (int y = 0; y < 16; ++y) o[y] = __float_as_uint(__uint_as_float(o[y]) * corr);
+              tc_st16(to + x, o);
             }
           }
-          tc_st16(ts + (x0 & 64) + (x0 & 32) / 2, pw);
-          if ((x0 + 32) % 64 == 0) {  // a half is done
-            tc_wait_st();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&bar.pfull[j][x0 >> 6]);
+          const float mref = m == -INFINITY ? 0.f : m;
+          const float2 sc2 = make_float2(scale, scale), nm2 = make_float2(-mref, -mref);
+#pragma unroll
+          for (int x0 = 0; x0 < 64; x0 += 32) {  // P (int8 cache: times the V scales)
+            uint32_t pw[16];
+#pragma unroll
+            for (int x = x0; x < x0 + 32; x += 4) {
+              float4 f;
+              if constexpr (KV8) f = *reinterpret_cast<const float4*>(sc + kCkKeys + x);
+#pragma unroll
+              for (int y = 0; y < 4; y += 2) {
+                const float2 s2 = make_float2(v[x + y], v[x + y + 1]), e = KV8 ? ck_add2(s2, nm2) : ck_fma2(s2, sc2, nm2);
+                float2 p = make_float2(pa_ex2(e.x), pa_ex2(e.y));
+                l2[(x + y) / 2 % 4] = ck_add2(l2[(x + y) / 2 % 4], p);
+                if constexpr (KV8) p = ck_mul2(p, y ? make_float2(f.z, f.w) : make_float2(f.x, f.y));
+                pw[(x - x0 + y) / 2] = pa_pack(p.x, p.y);
+              }
+            }
+            tc_st16(tsh + x0 / 2, pw);
           }
-        };
-        if (masked) {
-#pragma unroll 1
-          for (int x0 = 0; x0 < kCkKeys; x0 += 32) weights(std::true_type(), x0);
-        } else {
-#pragma unroll 1
-          for (int x0 = 0; x0 < kCkKeys; x0 += 32) weights(std::false_type(), x0);
+          tc_wait_st();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&bar.pfull[j][h]);
         }
       }
       if (!ok) break;

@@ -232,6 +232,33 @@ def test_attention_peaked_scores(fp, kvq):
     c.check(q, got)
 
 
+@pytest.mark.parametrize("slope", [0.2, 2.0, -0.2])
+@pytest.mark.parametrize("hd,H,Hkv", [(128, 4, 2), (64, 8, 1)])
+@pytest.mark.parametrize("kvq", [0, 1])
+def test_attention_scores_that_rise_with_the_position(fp, kvq, hd, H, Hkv, slope):
+    """The running maximum moves in every 64 keys (or never again): what was summed before is scaled each time."""
+    c = Batch(fp, kvq, hd, H, Hkv, [(6, 700), (200, 300), (1, 63), (3, 127)], 67, tail=3)
+    sign = np.where(np.random.default_rng(5).random(hd) < 0.5, -1.0, 1.0)
+    for b in range(c.B):
+        t = np.arange(c.pps * 16)
+        up = (slope * t if slope > 0 else slope * (t - 700)) / np.sqrt(hd)  # score of a query of 1: slope t
+        page, slot = c.table[b, t // 16], t % 16
+        if kvq:
+            c.data["k"][page, :, slot] = np.where(sign < 0, -100, 100)
+            c.data["ks"][page, :, slot] = (up / 100)[:, None]
+        else:
+            c.data["k"][page, :, slot] = synth.f32_to_bf16_bits((up[:, None] * sign).astype(np.float32))[:, None]
+    for w in c.data:
+        c.dev[w] = dev(c.data[w])
+    c.view = c.make_view(c.table)
+    q = np.empty((c.N, H, hd), np.float32)
+    q[:] = sign * np.array([1.0, 0.5])[np.arange(H) % 2][:, None]
+    q = synth.f32_to_bf16_bits(q).reshape(c.N, H * hd)
+    got, err = c.attend(q)
+    assert err == 0
+    c.check(q, got)
+
+
 @pytest.mark.parametrize("vs", [(1e-7, 3e-7), (50.0, 400.0)])
 def test_attention_int8_value_scales(fp, vs):
     c = Batch(fp, 1, 128, 8, 2, [(5, 400), (200, 100)], 17, vs=vs)
