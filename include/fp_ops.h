@@ -242,7 +242,7 @@ int fp_op_attention_prefill(const uint16_t* q, int q_stride, int B, int S, int n
 /* RoPE + KV-cache append of a chunk: as fp_op_rope_kv, for a ragged batch and
  * with the rotated queries to q_out bf16 [n_tokens][q_out_stride] (head h at
  * h*head_dim; q_out == qkv rotates in place and takes the same stride, else
- * FP_ERR_INVALID_ARG).  qkv bf16
+ * FP_ERR_INVALID_ARG; no other overlap).  qkv bf16
  * [n_tokens][row_stride]: H query heads, Hkv key heads, Hkv value heads.
  * Positions outside the cache set *err = 1 and skip the row, a page id outside
  * the pool sets *err = 1 and skips the row's cache writes.  Two rows must not
@@ -306,7 +306,7 @@ int fp_op_softmax(const float* logits, int M, int V, const float* temperature, f
  * Then one token is drawn: a < k from max(0, p_a - q_a) (q NULL: from p_a without
  * the refused token), a = k from p_k; it is the lowest t whose running sum exceeds
  * u_draw[b] times the whole sum (u in [0, 1); the weights need not add up to 1).
- * If that distribution is all zero, p_a itself is drawn from.
+ * If that distribution is all zero, p_a itself is drawn from; a NaN weighs nothing.
  * out_tokens int32 [n_tokens]: rows 0 .. a-1 of the sequence the accepted drafts,
  * row a the drawn token, -1 behind it; n_out int32 [B]: a + 1 (0: a sequence
  * without rows).  A sum that is zero or not finite draws nothing: row a is -1,
