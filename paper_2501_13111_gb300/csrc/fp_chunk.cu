@@ -47,9 +47,11 @@ FP_DEV uint2 codes8(const float* x, float s) {
 // and (by shuffles among those lanes) a row's maximum stay in the warp, and each
 // lane reads its cosines once for all heads.  Bound by bytes (qkv in, queries and
 // cache rows out) for many rows, by latency for few: with the read back below, chunks of
-// 4 x up to 1000 rows of 40 heads take 68 us (5.1 TB/s), 160 rows of 64 heads on 8, int8, 7.4.
+// 4 x up to 1000 rows of 40 heads take 64 us (5.4 TB/s), 160 rows of 64 heads on 8, int8, 7.4.
+// Four CTAs an SM, for the loads in flight: 64 registers, a few of 74 spilled (three: 68 us,
+// five: 71).
 template <int HD, bool KV8>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(256, 4)
     rope_kv_chunk_kernel(const uint16_t* qkv, int row_stride, int n_tokens, int B, int H, fp_kv_view kv,
                          const int32_t* __restrict__ cu, const int32_t* __restrict__ pos, const float* __restrict__ cs,
                          uint16_t* q_out, int q_out_stride, int32_t* err) {
