@@ -265,7 +265,8 @@ int fp_op_kv_read(const fp_kv_view* kv, int n_tokens, int B, const int32_t* cu, 
  * [n_tokens][n_heads*head_dim].
  * max_new: at least every sequence's number of rows; max_len: at least every
  * pos[b] + rows.  A sequence beyond either sets *err = 1: its rows behind the
- * first max_new are left as they were, keys behind max_len are not read.  A row at
+ * first max_new are left as they were, keys behind max_len are not read (either 0:
+ * nothing is done).  A row at
  * a negative position has no keys: zeros, and *err = 1.  A page id outside the
  * pool reads as zero keys and values and sets *err = 1.
  * An int8 cache enters as its codes, exact in bf16, the scales multiplied in fp32;
