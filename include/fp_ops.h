@@ -270,9 +270,11 @@ int fp_op_kv_read(const fp_kv_view* kv, int n_tokens, int B, const int32_t* cu, 
  * a negative position has no keys: zeros, and *err = 1.  A page id outside the
  * pool reads as zero keys and values and sets *err = 1.
  * An int8 cache enters as its codes, exact in bf16, the scales multiplied in fp32;
- * P is rounded to bf16.  Cache slots behind a sequence's last position may hold
- * anything; its cached values, and an int8 cache's V scales, must be finite (a NaN
- * or an infinity may reach rows before its position, in the same 128).
+ * P is rounded to bf16.  A score that is NaN or +inf (a query or a key that is not
+ * finite) makes the rows that see it NaN, and no others; a row whose scores are all
+ * -inf is zeros.  Cache slots behind a sequence's last position may hold
+ * anything; its cached V, and an int8 cache's V scales, must be finite (a NaN
+ * or an infinity there may reach rows before its position, in the same 128).
  * Batches that could make more than 2^31 tiles of work, by n_tokens, B, the heads
  * and max_len, are FP_ERR_UNSUPPORTED.
  * workspace: 256-byte aligned, at least

@@ -903,7 +903,7 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
       }
       tc_fence_after();
       const bool have = pair ? (j ? use1 : use0) : !empty;  // an accumulator to read
-      const float inv = l > 0.f ? 1.f / l : 0.f;
+      const float inv = l == 0.f ? 0.f : 1.f / l;  // (a row without keys: zeros)
       // pair: this group's tile, all columns; else half of the sum's columns a group
       const int x0 = pair ? 0 : j * (HD / 2), x1 = pair ? HD : x0 + HD / 2;
       const uint32_t src = pair ? to : lane_base + kCkO;
@@ -946,8 +946,14 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
               load(x, r);
               keep(p, rb, x, r);
             }
-          if (x0 == 0)
-            reinterpret_cast<float2*>(p + ML)[rb * 32 + lane] = make_float2(have && l > 0.f ? m : -INFINITY, have ? l : 0.f);
+          // A part without keys of the row has l = 0 and is marked by -inf: the join leaves it
+          // out.  One with a NaN score has a NaN l, and no reference where there was no other:
+          // any finite one hands the NaN on.
+          if (x0 == 0) {
+            const float ls = have ? l : 0.f;
+            reinterpret_cast<float2*>(p + ML)[rb * 32 + lane] =
+                make_float2(ls == 0.f ? -INFINITY : m == -INFINITY ? 0.f : m, ls);
+          }
         }
       }
       if (have) {
@@ -1026,7 +1032,7 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
           } else {
             int at[4];
             begins(w, rb, at);
-            write(w, at, x, r, ll > 0.f ? 1.f / ll : 0.f);
+            write(w, at, x, r, ll == 0.f ? 0.f : 1.f / ll);
           }
         }
         if (turn == 0) {
