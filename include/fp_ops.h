@@ -314,7 +314,8 @@ int fp_op_softmax(const float* logits, int M, int V, const float* temperature, f
  * row a the drawn token, -1 behind it; n_out int32 [B]: a + 1 (0: a sequence
  * without rows).  A sum that is zero or not finite draws nothing: row a is -1,
  * n_out a, *err = 1 (err may be NULL).  A draft outside [0, V) is refused and sets
- * *err = 1.  Sums are held in pairs of fp32 (48 bits).  V to 2^30 and B to
+ * *err = 1; drafts behind the first refused one are not looked at (padding of any
+ * value will do).  Sums are held in pairs of fp32 (48 bits).  V to 2^30 and B to
  * 2^27, else FP_ERR_UNSUPPORTED. */
 int fp_op_verify_draft(const float* p, const float* q, int V, int n_tokens, int B, const int32_t* cu,
                        const int32_t* tokens, const float* u_accept, const float* u_draw, int32_t* out_tokens,

@@ -311,11 +311,10 @@ __global__ void __cluster_dims__(kVfCTAs, 1, 1) __launch_bounds__(kVfThreads)
 #pragma unroll 1
     for (int i0 = 0; i0 < n - 1; i0 += 32) {
       const int i = i0 + lane;
-      bool refused = false;
+      bool refused = false, ok = true;
       if (i < n - 1) {
         const int t = __ldg(tokens + row0 + i + 1);
-        const bool ok = t >= 0 && t < V;
-        if (!ok && rank == 0 && err) atomicExch(err, 1);
+        ok = t >= 0 && t < V;
         const long long at = (long long)(row0 + i) * V + (ok ? t : 0);
         // (both sides of u q < p times 2^80 where the product's error could be lost)
         float qt = q ? __ldg(q + at) : 1.f, pt = __ldg(p + at);
@@ -327,6 +326,7 @@ __global__ void __cluster_dims__(kVfCTAs, 1, 1) __launch_bounds__(kVfThreads)
       const unsigned any = __ballot_sync(0xffffffffu, refused);
       if (any) {
         a = i0 + __ffs(any) - 1;
+        if (i == a && !ok && rank == 0 && err) atomicExch(err, 1);  // (what is behind it may be padding)
         break;
       }
     }
