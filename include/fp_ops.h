@@ -327,9 +327,10 @@ int fp_op_verify_draft(const float* p, const float* q, int V, int n_tokens, int 
  * frees its tensor memory and records status 2 in the error word, which the
  * runtime reports as FP_ERR_DEVICE_ASSERT.  This sets how many polling rounds
  * the prefill GEMM's MMA thread waits for a stage of operands on the current
- * device: rounds >= 0 (0 gives up at once) or < 0 to restore the default;
- * all other waits keep the default.  Synchronous; not for use while kernels
- * of the library are running. */
+ * device, and the MMA warps of fp_op_attention_chunk for a tile of values in the
+ * launches that follow: rounds >= 0 (0 gives up at once) or < 0 to restore the
+ * default; all other waits keep the default.  Synchronous; not for use while
+ * kernels of the library are running. */
 int fp_debug_set_wait_limit(long long rounds);
 
 /* Greedy choice out[m] = argmax logits[m][:V] (fp32); ties to the lowest id. */

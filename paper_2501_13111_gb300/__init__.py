@@ -395,7 +395,7 @@ def fp_op_verify_draft(p, q, V, n_tokens, B, cu, tokens, u_accept, u_draw, out_t
 
 
 def fp_debug_set_wait_limit(rounds):
-    """Test hook: polling rounds of the prefill GEMM's stage wait (< 0: default)."""
+    """Test hook: polling rounds of the prefill GEMM's stage wait and the chunk attention's V wait (< 0: default)."""
     return _check(_lib.fp_debug_set_wait_limit(rounds))
 
 

@@ -46,6 +46,7 @@
 // masked, their V rows are zeroed before the product (int8 cache: read as zeros).
 // Every wait on an mbarrier is bounded (error 2 past the limit).
 #include <algorithm>
+#include <atomic>
 #include <type_traits>
 
 #include "attn_tc.cuh"
@@ -140,6 +141,7 @@ struct CkArgs {
   uint16_t* out;
   uint8_t* ws;
   int32_t* err;
+  long long wait_limit;  // rounds of the issuers' wait for a V tile
 };
 
 // A piece of a unit, as the planning warp describes it.
@@ -432,7 +434,7 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
           return __ldg(pt + key0 / 16);
         };
         int id = page(w.t0);
-        for (int t = w.t0; t < w.t1; ++t, ++kn) {
+        for (int t = w.t0; t < w.t1; ++t) {
           const int s = kn % R, next_id = page(t + 1);
           const bool there = id >= 0 && id < a.n_pages;
           if (!there && !is_v && lane < 8 && t * kCkKeys + lane * 16 < w.end && a.err) atomicExch(a.err, 1);
@@ -443,6 +445,7 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
           if (lane == 0) mbar_expect_tx(&full[s], TILE);
           __syncwarp();
           if (lane < 8) ck_tma_4d(dst + s * TILE + lane * PAGE, map, 0, 0, 0, group, &full[s]);
+          ++kn;  // in flight from here on, wherever this ends: the drain below waits for it
           id = next_id;
           if (!is_v && t == w.t0) queries();
           if (!ok) return;
@@ -568,7 +571,7 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
           const int s = (kn + i) % R, s1 = (kn + i + di) % R;
           const bool more = i + di < i1;
           // V is there; (first tile) the last unit's output has been read
-          ok = mbar_wait(&bar.vfull[s], ((kn + i) / R) & 1) &&
+          ok = mbar_wait_n(&bar.vfull[s], ((kn + i) / R) & 1, a.wait_limit) &&
                (i > i0 || on == 0 || mbar_wait(&bar.oempty[j], (on - 1) & 1));
           // V rows behind the sequence's last position, zeroed before they are multiplied
           // (by both issuers where both read them)
@@ -1123,6 +1126,11 @@ static cudaError_t launch_ck(const uint16_t* q, int q_stride, const fp_kv_view& 
                 (size_t)ck_smem<HD>(), s, mq, mk, mv, a);
 }
 
+// Of the launches that follow (lowered by tests of the failure path; other waits keep
+// kTcSpinLimit, so that copies and MMAs in flight are drained).
+static std::atomic<long long> g_ck_wait_limit{kTcSpinLimit};
+void attention_chunk_wait_limit(long long rounds) { g_ck_wait_limit.store(rounds, std::memory_order_relaxed); }
+
 cudaError_t launch_attention_chunk(const uint16_t* q, int q_stride, int n_tokens, int B, int n_heads,
                                    const fp_kv_view& kv, const int32_t* cu, const int32_t* pos, int max_new, int max_len,
                                    uint16_t* out, void* ws, int32_t* err, cudaStream_t s) {
@@ -1130,7 +1138,7 @@ cudaError_t launch_attention_chunk(const uint16_t* q, int q_stride, int n_tokens
   const int G = n_heads / kv.n_kv_heads;
   const CkArgs a = {cu, pos, n_tokens, B, n_heads, kv.n_kv_heads, G, max_new, max_len, ck_tile_tokens(G), kv.page_table,
                     kv.pages_per_seq, kv.n_pages, (const int8_t*)kv.k_pool, (const int8_t*)kv.v_pool, kv.k_scale, kv.v_scale,
-                    out, (uint8_t*)ws, err};
+                    out, (uint8_t*)ws, err, g_ck_wait_limit.load(std::memory_order_relaxed)};
   if (kv.head_dim == 64)
     return kv.kvquant == FP_KV_INT8 ? launch_ck<64, true>(q, q_stride, kv, a, s) : launch_ck<64, false>(q, q_stride, kv, a, s);
   return kv.kvquant == FP_KV_INT8 ? launch_ck<128, true>(q, q_stride, kv, a, s) : launch_ck<128, false>(q, q_stride, kv, a, s);

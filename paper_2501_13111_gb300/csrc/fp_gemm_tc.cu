@@ -628,5 +628,6 @@ cudaError_t launch_gemm_tc(int wquant, int epi, const uint16_t* x, int M, int N,
 
 extern "C" int fp_debug_set_wait_limit(long long rounds) {
   const long long v = rounds < 0 ? fpk::kTcSpinLimit : std::min(rounds, fpk::kTcSpinLimit);
+  fpk::attention_chunk_wait_limit(v);
   return cudaMemcpyToSymbol(g_stage_wait_limit, &v, sizeof v) == cudaSuccess ? FP_OK : FP_ERR_CUDA;
 }

@@ -64,6 +64,7 @@ size_t attention_chunk_ws_bytes(int B, int n_heads, int n_kv_heads, int head_dim
 cudaError_t launch_attention_chunk(const uint16_t* q, int q_stride, int n_tokens, int B, int n_heads,
                                    const fp_kv_view& kv, const int32_t* cu, const int32_t* pos, int max_new, int max_len,
                                    uint16_t* out, void* ws, int32_t* err, cudaStream_t s);
+void attention_chunk_wait_limit(long long rounds);  // fp_debug_set_wait_limit
 
 // ---- probabilities and draft verification (fp_verify.cu)
 cudaError_t launch_softmax(const float* logits, int M, int V, const float* temp, float* probs, int32_t* err,
