@@ -316,10 +316,11 @@ __global__ void __cluster_dims__(kVfCTAs, 1, 1) __launch_bounds__(kVfThreads)
         const int t = __ldg(tokens + row0 + i + 1);
         ok = t >= 0 && t < V;
         const long long at = (long long)(row0 + i) * V + (ok ? t : 0);
-        // (both sides of u q < p times 2^80 where the product's error could be lost)
+        // u q < p exactly: the rounded product, and where that is p its error.  Both sides
+        // times 2^80 where the error of a product near p could underflow.
         float qt = q ? __ldg(q + at) : 1.f, pt = __ldg(p + at);
         const float ui = __ldg(u + row0 + i);
-        if (qt < 1e-15f && pt < 1e-15f) qt *= 0x1p80f, pt *= 0x1p80f;
+        if (pt < 1e-15f && qt < 0x1p40f) qt *= 0x1p80f, pt *= 0x1p80f;
         const float x = __fmul_rn(ui, qt), e = __fmaf_rn(ui, qt, -x);
         refused = !ok || !(x < pt || (x == pt && e < 0.f));
       }

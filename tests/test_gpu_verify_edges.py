@@ -34,3 +34,26 @@ def test_padding_behind_the_first_refusal_is_not_looked_at(fp, k, refused, oneho
     assert cnt.tolist() == [refused + 1, k + 1]
     tokens[refused + 1] = V
     _check_verify(fp, p, q, tokens, u, r, cu)  # (the oracle says: reported)
+
+
+def test_products_that_underflow(fp):
+    """u q < p where p is the fp32 next to u q, and what tells them apart is below the least fp32: accepted
+    where the exact product is the smaller, refused where it is not."""
+    rng = np.random.default_rng(6)
+    V, want, parts = 8, [], []
+    while len(want) < 64:
+        u, qt = np.float32((1 + rng.random()) * 2.0 ** -126), np.float32(0.5 + rng.random() / 2)
+        exact, pt = float(u) * float(qt), np.float32(float(u) * float(qt))
+        if exact == float(pt) or (exact < float(pt)) != (len(want) % 2 == 0):
+            continue
+        want.append(exact < float(pt))
+        p, q = np.full((2, V), 0.125, np.float32), np.full((2, V), 0.125, np.float32)
+        p[0, 5], q[0, 5] = pt, qt
+        parts.append((p, q, u))
+    B = len(want)
+    p, q = np.concatenate([x[0] for x in parts]), np.concatenate([x[1] for x in parts])
+    u = np.zeros(2 * B, np.float32)
+    u[::2] = [x[2] for x in parts]
+    tokens = np.tile(np.array([0, 5], np.int32), B)
+    out, cnt = _check_verify(fp, p, q, tokens, u, rng.random(B, dtype=np.float32), 2 * np.arange(B + 1))
+    assert (cnt == 2).tolist() == want
