@@ -276,7 +276,8 @@ int fp_op_kv_read(const fp_kv_view* kv, int n_tokens, int B, const int32_t* cu, 
  * anything; its cached V, and an int8 cache's V scales, must be finite (a NaN
  * or an infinity there may reach rows before its position, in the same 128).
  * Batches that could make more than 2^31 tiles of work, by n_tokens, B, the heads
- * and max_len, are FP_ERR_UNSUPPORTED.
+ * and max_len, are FP_ERR_UNSUPPORTED, as are heads so many that T output rows, T
+ * twice the largest power of two up to 128 / (H/Hkv), have 2^31 elements.
  * workspace: 256-byte aligned, at least
  * fp_op_attention_chunk_workspace_bytes(B, n_heads, n_kv_heads, head_dim, max_new)
  * bytes (0: a shape that is refused).  Its leading 64 KB hold ticket counters that

@@ -1096,8 +1096,10 @@ static int ck_sms() {
   return sms;
 }
 
-bool attention_chunk_fits(int n_tokens, int B, int n_heads, int n_kv_heads, int max_len) {
-  return ck_fits(n_tokens, B, max_len, n_kv_heads, ck_tile_tokens(n_heads / n_kv_heads));
+// The plan's places and a unit's places in the output are 32-bit.
+bool attention_chunk_fits(int n_tokens, int B, int n_heads, int n_kv_heads, int head_dim, int max_len) {
+  const int T = ck_tile_tokens(n_heads / n_kv_heads);
+  return ck_fits(n_tokens, B, max_len, n_kv_heads, T) && 2LL * T * n_heads * head_dim < (1LL << 31);
 }
 
 size_t attention_chunk_ws_bytes(int B, int n_heads, int n_kv_heads, int head_dim, int max_new) {

@@ -247,7 +247,7 @@ int fp_op_attention_chunk(const uint16_t* q, int q_stride, int n_tokens, int B, 
   if (q_stride < (long long)n_heads * kv->head_dim) return FP_ERR_INVALID_ARG;
   if (!chunk_group_ok(n_heads, kv->n_kv_heads)) return FP_ERR_UNSUPPORTED;
   if (q_stride % 8 || !aligned16(q) || !aligned16(out)) return FP_ERR_UNSUPPORTED;
-  if (!attention_chunk_fits(n_tokens, B, n_heads, kv->n_kv_heads, max_len)) return FP_ERR_UNSUPPORTED;
+  if (!attention_chunk_fits(n_tokens, B, n_heads, kv->n_kv_heads, kv->head_dim, max_len)) return FP_ERR_UNSUPPORTED;
   if (max_len > (long long)kv->pages_per_seq * kv->page_size) return FP_ERR_CAPACITY;
   if (n_tokens == 0 || B == 0 || max_new == 0 || max_len == 0) return FP_OK;
   if (!workspace || ((uintptr_t)workspace & 255) ||

@@ -59,7 +59,7 @@ cudaError_t launch_rope_kv_chunk(const uint16_t* qkv, int row_stride, int n_toke
                                  uint16_t* q_out, int q_out_stride, int32_t* err, cudaStream_t s);
 cudaError_t launch_kv_read(const fp_kv_view& kv, int n_tokens, int B, const int32_t* cu, const int32_t* pos,
                            uint16_t* k_out, uint16_t* v_out, int out_stride, int32_t* err, cudaStream_t s);
-bool attention_chunk_fits(int n_tokens, int B, int n_heads, int n_kv_heads, int max_len);
+bool attention_chunk_fits(int n_tokens, int B, int n_heads, int n_kv_heads, int head_dim, int max_len);
 size_t attention_chunk_ws_bytes(int B, int n_heads, int n_kv_heads, int head_dim, int max_new);
 cudaError_t launch_attention_chunk(const uint16_t* q, int q_stride, int n_tokens, int B, int n_heads,
                                    const fp_kv_view& kv, const int32_t* cu, const int32_t* pos, int max_new, int max_len,
