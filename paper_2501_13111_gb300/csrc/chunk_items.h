@@ -45,7 +45,7 @@ struct CkSeq {
   FP_CK bool set(int first, int count, int p, int tile_tokens, int max_new, int max_len) {
     row0 = first;
     n = count < max_new ? count : max_new;
-    pos = p;
+    pos = p < max_len ? p : max_len;  // (behind the bound every row sees the same keys)
     const long long e = (long long)p + n;
     end = (int)(e < 0 ? 0 : e > max_len ? max_len : e);
     bad = n > 0 && (p < 0 || e > max_len);
