@@ -1,5 +1,5 @@
-// Pieces shared by the tcgen05 prefill attention kernels (fp_attn_tc.cu,
-// fp_attn_short.cu): operand descriptors, conversions, launch limits.
+// Pieces shared by the tcgen05 attention kernels (fp_attn_tc.cu,
+// fp_attn_short.cu, fp_attn_chunk.cu): operand descriptors, conversions, launch limits.
 #pragma once
 
 #include "attn_items.h"
@@ -15,13 +15,13 @@ constexpr int kPaStage = 32 * 64;            // a warp's 32 output rows, 32 colu
 constexpr float kPaLog2e = 1.4426950408889634f;
 
 // Shared-memory descriptor of an MN-major operand with 128-byte swizzle:
-// 64-element atoms along MN `lbo` bytes apart, 8-row groups along K 1024
+// 64-element atoms along MN `lbo` bytes apart, 8-row groups along K `sbo`
 // bytes apart.
-FP_DEV uint64_t sdesc_mn(uint32_t saddr, uint32_t lbo) {
+FP_DEV uint64_t sdesc_mn(uint32_t saddr, uint32_t lbo, uint32_t sbo = 1024) {
   uint64_t d = 0;
   d |= (uint64_t)((saddr & 0x3FFFF) >> 4);
   d |= (uint64_t)((lbo >> 4) & 0x3FFF) << 16;
-  d |= (uint64_t)(1024 >> 4) << 32;
+  d |= (uint64_t)(sbo >> 4) << 32;
   d |= (uint64_t)1 << 46;
   d |= (uint64_t)2 << 61;
   return d;
@@ -47,6 +47,32 @@ FP_DEV uint32_t pa_pack_h(float lo, float hi) {
   uint32_t r;
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
   return r;
+}
+
+// Two fp32 lanes at once: a b + c, a b, a + b.
+FP_DEV float2 pa_fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{\n .reg .b64 a, b, c, d;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n mov.b64 c, {%6, %7};\n"
+      " fma.rn.f32x2 d, a, b, c;\n mov.b64 {%0, %1}, d;\n}\n"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+FP_DEV float2 pa_mul2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n .reg .b64 a, b, d;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n"
+      " mul.rn.f32x2 d, a, b;\n mov.b64 {%0, %1}, d;\n}\n"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+FP_DEV float2 pa_add2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n .reg .b64 a, b, d;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n"
+      " add.rn.f32x2 d, a, b;\n mov.b64 {%0, %1}, d;\n}\n"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
 }
 
 // Signed bytes a and b of w as the fp16 pair (q_a, q_b), exact: the byte

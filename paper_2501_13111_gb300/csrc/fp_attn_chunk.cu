@@ -96,34 +96,12 @@ FP_DEV uint64_t ck_sdesc_k(uint32_t saddr, uint32_t sbo) {
   return (uint64_t)((saddr & 0x3FFFF) >> 4) | (uint64_t)1 << 16 | (uint64_t)(sbo >> 4) << 32 | (uint64_t)1 << 46 |
          (uint64_t)2 << 61;
 }
-// The same atoms MN-major: 64 columns on `lbo` bytes, 8-row groups along K `sbo`.
-FP_DEV uint64_t ck_sdesc_mn(uint32_t saddr, uint32_t lbo, uint32_t sbo) {
-  return (uint64_t)((saddr & 0x3FFFF) >> 4) | (uint64_t)(lbo >> 4) << 16 | (uint64_t)(sbo >> 4) << 32 |
-         (uint64_t)1 << 46 | (uint64_t)2 << 61;
-}
 FP_DEV void ck_tma_4d(void* dst, const CUtensorMap* map, int x, int y, int z, int w, uint64_t* bar) {
   asm volatile(
       "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
       ::"r"(smem_u32(dst)), "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(smem_u32(bar))
       : "memory");
 }
-#define CK_F32X2(name, op, args, ...)                                                                       \
-  FP_DEV float2 name args {                                                                                 \
-    float2 d;                                                                                               \
-    asm("{\n .reg .b64 a, b, c, d;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n mov.b64 c, {%6, %7};\n " \
-        op "\n mov.b64 {%0, %1}, d;\n}\n"                                                                  \
-        : "=f"(d.x), "=f"(d.y)                                                                              \
-        : __VA_ARGS__);                                                                                     \
-    return d;                                                                                               \
-  }
-// Two fp32 lanes at once: a b + c, a b, a + b.
-CK_F32X2(ck_fma2, "fma.rn.f32x2 d, a, b, c;", (float2 a, float2 b, float2 c), "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y),
-         "f"(c.x), "f"(c.y))
-CK_F32X2(ck_mul2, "mul.rn.f32x2 d, a, b;", (float2 a, float2 b), "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(0.f),
-         "f"(0.f))
-CK_F32X2(ck_add2, "add.rn.f32x2 d, a, b;", (float2 a, float2 b), "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(0.f),
-         "f"(0.f))
-#undef CK_F32X2
 FP_DEV float ck_max3(float a, float b, float c) {
   float d;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
@@ -513,7 +491,7 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
       constexpr int j = decltype(cj)::value;
       constexpr uint32_t idesc_s = tc_idesc(kCkKeys, kCkKeys), idesc_o = tc_idesc(kCkKeys, HD) | (1u << 16);
       const uint64_t qd = sdesc(smem_u32(sQ)), kd = ck_sdesc_k(smem_u32(sK), SBO),
-                     vd = ck_sdesc_mn(smem_u32(sV), 1024, SBO);
+                     vd = sdesc_mn(smem_u32(sV), 1024, SBO);
       int n = 0, kn = 0, pn = 0, on = 0;
       bool ok = true;
       // A vote's result is in a uniform register, and so is all that follows from it.
@@ -678,7 +656,7 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
           const uint32_t u = ww[j >> 1];
           const float lo = __uint_as_float(__byte_perm(u, 0x47000000u, (j & 1) ? 0x7424 : 0x7404));
           const float hi = __uint_as_float(__byte_perm(u, 0x47000000u, (j & 1) ? 0x7434 : 0x7414));
-          const float2 f = ck_add2(make_float2(lo, hi), z2);
+          const float2 f = pa_add2(make_float2(lo, hi), z2);
           o[j] = pa_pack(f.x, f.y);
         }
         uint8_t* rp = tiles + s * TILE + i * (PER / 8 * SBO);
@@ -808,8 +786,8 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
 #pragma unroll
             for (int x = 0; x < 64; x += 4) {
               const float4 f = *reinterpret_cast<const float4*>(sc + x);
-              const float2 p = ck_mul2(make_float2(v[x], v[x + 1]), make_float2(f.x, f.y));
-              const float2 q = ck_mul2(make_float2(v[x + 2], v[x + 3]), make_float2(f.z, f.w));
+              const float2 p = pa_mul2(make_float2(v[x], v[x + 1]), make_float2(f.x, f.y));
+              const float2 q = pa_mul2(make_float2(v[x + 2], v[x + 3]), make_float2(f.z, f.w));
               v[x] = p.x, v[x + 1] = p.y, v[x + 2] = q.x, v[x + 3] = q.y;
             }
           }
@@ -830,7 +808,7 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
             corr = exp2f(m - mx);  // 0 on the first tile
             m = mx;
 #pragma unroll
-            for (int y = 0; y < 4; ++y) l2[y] = ck_mul2(l2[y], make_float2(corr, corr));
+            for (int y = 0; y < 4; ++y) l2[y] = pa_mul2(l2[y], make_float2(corr, corr));
           }
           if ((h || t > t_first) && __any_sync(0xffffffffu, corr != 1.f)) {
             // O holds P V of the halves before: those of earlier tiles are complete (this one's
@@ -858,10 +836,10 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
               if constexpr (KV8) f = *reinterpret_cast<const float4*>(sc + kCkKeys + x);
 #pragma unroll
               for (int y = 0; y < 4; y += 2) {
-                const float2 s2 = make_float2(v[x + y], v[x + y + 1]), e = KV8 ? ck_add2(s2, nm2) : ck_fma2(s2, sc2, nm2);
+                const float2 s2 = make_float2(v[x + y], v[x + y + 1]), e = KV8 ? pa_add2(s2, nm2) : pa_fma2(s2, sc2, nm2);
                 float2 p = make_float2(pa_ex2(e.x), pa_ex2(e.y));
-                l2[(x + y) / 2 % 4] = ck_add2(l2[(x + y) / 2 % 4], p);
-                if constexpr (KV8) p = ck_mul2(p, y ? make_float2(f.z, f.w) : make_float2(f.x, f.y));
+                l2[(x + y) / 2 % 4] = pa_add2(l2[(x + y) / 2 % 4], p);
+                if constexpr (KV8) p = pa_mul2(p, y ? make_float2(f.z, f.w) : make_float2(f.x, f.y));
                 pw[(x - x0 + y) / 2] = pa_pack(p.x, p.y);
               }
             }

@@ -91,32 +91,6 @@ constexpr int kPaScl = 4;                    // tiles of int8 scales
 constexpr int kPaSmem = (2 + 2 * kPaRing) * kPaTile + 8 * kPaStage + 1024;  // Q, K, V, output, alignment
 constexpr float kPaSlack = 8.f;  // log2 of the largest P allowed before the reference maximum moves
 
-// Two fp32 lanes at once: a b + c, a b, a + b.
-FP_DEV float2 pa_fma2(float2 a, float2 b, float2 c) {
-  float2 d;
-  asm("{\n .reg .b64 a, b, c, d;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n mov.b64 c, {%6, %7};\n"
-      " fma.rn.f32x2 d, a, b, c;\n mov.b64 {%0, %1}, d;\n}\n"
-      : "=f"(d.x), "=f"(d.y)
-      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
-  return d;
-}
-FP_DEV float2 pa_mul2(float2 a, float2 b) {
-  float2 d;
-  asm("{\n .reg .b64 a, b, d;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n"
-      " mul.rn.f32x2 d, a, b;\n mov.b64 {%0, %1}, d;\n}\n"
-      : "=f"(d.x), "=f"(d.y)
-      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-  return d;
-}
-FP_DEV float2 pa_add2(float2 a, float2 b) {
-  float2 d;
-  asm("{\n .reg .b64 a, b, d;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n"
-      " add.rn.f32x2 d, a, b;\n mov.b64 {%0, %1}, d;\n}\n"
-      : "=f"(d.x), "=f"(d.y)
-      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-  return d;
-}
-
 // split: the two softmax groups share a query tile (plan.pair == 0)
 template <bool KV8, bool split>
 __global__ void __launch_bounds__(pa_threads<KV8>(), 1)
