@@ -280,7 +280,8 @@ int fp_op_kv_read(const fp_kv_view* kv, int n_tokens, int B, const int32_t* cu, 
  * twice the largest power of two up to 128 / (H/Hkv), have 2^31 elements.
  * workspace: 256-byte aligned, at least
  * fp_op_attention_chunk_workspace_bytes(B, n_heads, n_kv_heads, head_dim, max_new)
- * bytes (0: a shape that is refused).  Its leading 64 KB hold ticket counters that
+ * bytes (0: a shape that is refused; else by head_dim alone: 21 MB for 64, 41 MB
+ * for 128).  Its leading 64 KB hold ticket counters that
  * must be zero before the first call; every call leaves them zero again, so one
  * workspace serves any sequence of calls of its shape or smaller ones on one
  * stream (calls that overlap on the GPU need separate workspaces; zero it again
@@ -294,7 +295,8 @@ size_t fp_op_attention_chunk_workspace_bytes(int B, int n_heads, int n_kv_heads,
  * T = temperature[m] (fp32 [M]; NULL: 1).  T = 0 is the greedy choice: 1 at the
  * lowest index of the largest logit, else 0.  -inf masks a token; a row that
  * masks all of them gives zeros.  A NaN or +inf in a row with T > 0 gives NaN
- * throughout.  A T that is negative, infinite or NaN gives a row of zeros and
+ * throughout (at T = 0 a NaN is passed over; a row of nothing else gives zeros).
+ * A T that is negative, infinite or NaN gives a row of zeros and
  * sets *err = 1 (err may be NULL).  probs may be logits.  M to 2^27 and V to 2^30,
  * else FP_ERR_UNSUPPORTED. */
 int fp_op_softmax(const float* logits, int M, int V, const float* temperature, float* probs, int32_t* err,

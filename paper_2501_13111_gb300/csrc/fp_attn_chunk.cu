@@ -34,9 +34,9 @@
 //               bf16(q s) took 54 us where this takes 63, 420 where 496, see below, but
 //               were further from the sums in 64 bits: 0.0040 against 0.0024, relative.)
 // Measured (launches in a graph, heads of 128): 8 sequences of 5 rows to position 612, 32
-// heads, bf16 cache 23.6 us (2.6 TB/s); 32 of 5 rows to 2148, 64 heads on 8, int8 63 us
-// (1.8 TB/s); 4 chunks of 512 rows to 2048, 40 heads, bf16 77 us (744 TFLOP/s); 2 of 1024
-// rows to 8000, 64 heads on 8, int8 496 us (814 TFLOP/s).  A step of two query tiles takes
+// heads, bf16 cache 23.1 us (2.7 TB/s); 32 of 5 rows to 2148, 64 heads on 8, int8 63 us
+// (1.8 TB/s); 4 chunks of 512 rows to 2048, 40 heads, bf16 77 us (747 TFLOP/s); 2 of 1024
+// rows to 8000, 64 heads on 8, int8 496 us (815 TFLOP/s).  A step of two query tiles takes
 // about 3800 cycles where its MMAs need 2080: a group's scores wait for its P, P for the
 // scores, and what is in between is as long as the other group's products; with an int8
 // cache the scales' way from shared memory, which the MMAs keep busy, comes on top (chunk
@@ -60,8 +60,8 @@ constexpr int kCkSoft = 8;                        // softmax warps
 constexpr int kCkWarpQ = 8, kCkWarpMma = 9, kCkWarpPlan = 11, kCkWarpWiden = 12, kCkWiden = 8;
 template <bool KV8>
 constexpr int ck_threads() { return KV8 ? (kCkWarpWiden + kCkWiden) * 32 : 384; }
-// Registers a thread: 384 threads may have 168, which none needs; 640 (int8 cache) launch
-// with 96, moved to the softmax: 256 x 128 + 384 x 72 < 640 x 96 (with 120 and 80 its row
+// Registers a thread: 384 threads may have 168, and take 163 or 167 (heads of 128, 64);
+// 640 (int8 cache) launch with 96, moved to the softmax: 256 x 128 + 384 x 72 < 640 x 96 (with 120 and 80 its row
 // spills more: chunk int8 504 us against 496)
 constexpr int kCkReaders = kCkSoft + 3;           // warps that read each piece's description: softmax, Q, MMA
 constexpr int kCkPieces = 4;                      // pieces described ahead

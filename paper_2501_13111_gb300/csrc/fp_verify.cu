@@ -23,8 +23,10 @@ namespace fpk {
 // e 2^((m_warp - m) c) / sum: one read, one write, one meeting.  Rows of more than
 // 262144 values (512 threads x 16 groups x 8 CTAs) are read a second time instead.
 // Groups are aligned in memory: the row's first and last may be part of a neighbour's.
-// Bound by latency and bytes one after the other: all CTAs read, meet and write at the
-// same time; 160 rows of 32000 take 15 us (2.7 TB/s), 3 of 128001 6.3.
+// Bound by latency and bytes one after the other (CTAs read, meet and write in step) and
+// by the waves: two CTAs an SM are 304 places, so 152 rows of 32000, in clusters of two,
+// take 11.1 us (3.5 TB/s) and 160 rows, whose last eight start when others have ended,
+// 15.4 (2.7 TB/s).  3 rows of 128001 6.3.
 constexpr int kSmThreads = 512, kSmWarps = kSmThreads / 32, kSmItems = 16, kSmMaxCTAs = 8;
 
 FP_DEV float sm_ex2(float x) {
@@ -227,7 +229,8 @@ cudaError_t launch_softmax(const float* logits, int M, int V, const float* temp,
 // fp64 is slow here (an addition takes about 300 cycles, and there were forty one
 // after another: 21 us for 32 sequences of 32000 tokens).  So sums are pairs of fp32,
 // hi + lo, the error of every addition carried along: good to 2^-46 or better.
-// Differences p - q and products u q are exact as pairs.
+// Differences p - q and products u q are exact as pairs (the error-free sum of Knuth, TAOCP
+// vol. 2, 4.2.2, and Dekker's renormalisation, Numer. Math. 18, 1971).
 // A cluster of 8 CTAs a sequence: every warp sums a run of consecutive weights, the
 // CTAs' totals meet through distributed shared memory, and the warp whose run holds
 // the border looks through it again (from L2): 32 pieces, then the piece's tokens.
