@@ -324,13 +324,144 @@ int fp_op_verify_draft(const float* p, const float* q, int V, int n_tokens, int 
                        const int32_t* tokens, const float* u_accept, const float* u_draw, int32_t* out_tokens,
                        int32_t* n_out, int32_t* err, void* stream);
 
+/* ---- Trees of drafted tokens: several continuations of each sequence verified in
+ * one pass.  The batch is ragged as above.  A sequence's rows are its tree: row 0 its
+ * last accepted token, every other row a drafted token whose parent, an earlier row,
+ * is the token before it.  Row i stands in the cache at position pos[b] + i until the
+ * accepted path is known, but is rotated by pos[b] + its depth.  A step: plan the tree
+ * once; in every layer append, then attend; draw and accept; in every layer commit the
+ * path.  For a chain (each row's parent the row before) all of this is the chunk's. */
+
+/* Rows of a tree that fp_op_tree_plan takes. */
+#define FP_TREE_MAX_ROWS 1024
+
+/* The plan of a batch of trees.  parent int32 [n_tokens]: the row, within its own
+ * sequence, of the token before, less than the row's own, or -1 for none (the cached
+ * prefix is before it; rows other than 0 may have none).  depth int32 [n_tokens]:
+ * each row's number of ancestors.  mask uint32 [n_tokens][mask_stride]: bit j % 32 of
+ * word j / 32 is set where row j of the sequence is the row itself or an ancestor; the
+ * words' other bits are clear.  mask_stride at least ceil(max_new / 32), at most 65536;
+ * max_new: at least every sequence's rows, at most FP_TREE_MAX_ROWS.  Another parent
+ * is taken for -1 and sets *err = 1 (err may be NULL); so does a sequence of more than
+ * max_new rows, whose rows behind those are left as they were. */
+int fp_op_tree_plan(const int32_t* parent, int n_tokens, int B, const int32_t* cu, int max_new, int32_t* depth,
+                    uint32_t* mask, int mask_stride, int32_t* err, void* stream);
+
+/* RoPE + KV-cache append of a batch of trees: as fp_op_rope_kv_chunk (row i goes to
+ * position pos[b] + i), with row i rotated by position pos[b] + depth[row] (depth
+ * int32 [n_tokens]).  A rotated position outside the cache's positions sets *err = 1
+ * and skips the row too. */
+int fp_op_rope_kv_tree(const uint16_t* qkv, int row_stride, int n_tokens, int B, int n_heads, const fp_kv_view* kv,
+                       const int32_t* cu, const int32_t* pos, const int32_t* depth, const float* rope_cs,
+                       uint16_t* q_out, int q_out_stride, int32_t* err, void* stream);
+
+/* Attention of a batch of trees: as fp_op_attention_chunk, but row i of sequence b
+ * sees positions 0 .. pos[b] - 1 and, of the sequence's own rows, those whose bit its
+ * mask words have set (mask uint32 [n_tokens][mask_stride], as fp_op_tree_plan writes
+ * them; any mask will do, rows may see later rows).  Bits behind the sequence's last
+ * row do not count.  mask_stride at least ceil(max_new / 32).  A row that sees
+ * nothing (pos[b] = 0 and no bit) is zeros.  A sequence at a negative position has
+ * no keys at all: zeros, and *err = 1.  Cached V that are not finite may reach rows
+ * that do not see them, in the same 128 positions.  All else, bounds, errors,
+ * accuracy and workspace, as there (a workspace may serve both). */
+int fp_op_attention_tree(const uint16_t* q, int q_stride, int n_tokens, int B, int n_heads, const fp_kv_view* kv,
+                         const int32_t* cu, const int32_t* pos, const uint32_t* mask, int mask_stride, int max_new,
+                         int max_len, uint16_t* out, void* workspace, size_t workspace_bytes, int32_t* err,
+                         void* stream);
+size_t fp_op_attention_tree_workspace_bytes(int B, int n_heads, int n_kv_heads, int head_dim, int max_new);
+
+/* Verification of a batch of trees against the target's probabilities, from given
+ * random numbers.  Row i of p fp32 [n_tokens][V] is the target's distribution of the
+ * token after row i; tokens int32 [n_tokens] the drafted tokens (row 0's is not read);
+ * parent as for fp_op_tree_plan.  From row 0 on: a token is drawn from the row's
+ * distribution, the lowest t whose running sum exceeds u[row] times the whole sum (u
+ * fp32 [n_tokens], in [0, 1); the weights need not add up to 1, a NaN or a negative
+ * one weighs nothing).  If a child of the row (the lowest that is behind it and names
+ * it as its parent) has that token, it is accepted and the next row; else the token is
+ * the last.  So what comes out is distributed as the target says, whatever was drafted.
+ * path int32 [n_tokens]: the accepted rows, row 0 first, within the sequence;
+ * out_tokens int32 [n_tokens]: the tokens drawn after each, the accepted ones and the
+ * last; both -1 behind; n_out int32 [B]: their number (0: a sequence without rows).
+ * A sum that is zero or not finite draws nothing: the row is in path, its token -1 and
+ * not counted, *err = 1 (err may be NULL).  Sums are held in pairs of fp32 (48 bits).
+ * V to 2^30 and B to 2^27, else FP_ERR_UNSUPPORTED. */
+int fp_op_verify_tree(const float* p, int V, int n_tokens, int B, const int32_t* cu, const int32_t* parent,
+                      const int32_t* tokens, const float* u, int32_t* path, int32_t* out_tokens, int32_t* n_out,
+                      int32_t* err, void* stream);
+
+/* The accepted path's rows of the cache moved together: position pos[b] + j of
+ * sequence b takes what position pos[b] + path[cu[b] + j] holds (K, V and an int8
+ * cache's scales, bit for bit), for j = 0, 1, .. up to the first -1 or the sequence's
+ * last row.  A path ascends (path as fp_op_verify_tree writes it); an entry that does
+ * not, or is no row of the sequence, sets *err = 1 (err may be NULL) and ends the
+ * sequence's path there.  A position outside the cache or a page id outside the pool
+ * sets *err = 1 and skips the row.  No two sequences may hold these positions in the
+ * same pages. */
+int fp_op_kv_commit(const fp_kv_view* kv, int n_tokens, int B, const int32_t* cu, const int32_t* pos,
+                    const int32_t* path, int32_t* err, void* stream);
+
+/* ---- Beams: B groups of W hypotheses each, W up to FP_BEAM_MAX (else
+ * FP_ERR_UNSUPPORTED), B up to FP_BEAM_MAX_GROUPS (the same).  Beam w of group b is row b * W + w of all buffers,
+ * and a sequence of its own in the paged cache (a row of the page table). */
+#define FP_BEAM_MAX 32
+#define FP_BEAM_MAX_GROUPS 16384
+
+/* The best continuations.  logits fp32 [B*W][V], score fp32 [B*W] (a hypothesis' sum of
+ * log-probabilities; -inf: there is none).  A group's candidates are (w, t) with the
+ * value score[w] + logits[w][t] - log sum_s exp(logits[w][s]); the W largest, in falling
+ * order, ties to the lowest w, then t: parent int32 [B*W] their w, token int32 [B*W]
+ * their t, new_score fp32 [B*W] their values.  A logit of -inf bans its token.  done
+ * int32 [B*W] (NULL: none): where it is not 0 the hypothesis has ended; its logits are
+ * not read, its one candidate is end_token with its score as it is.  new_done int32
+ * [B*W] (may be NULL): 1 where the parent had ended or the token is end_token, else 0.
+ * end_token in [-1, V); -1: none (done must be NULL then).  With fewer than W candidates
+ * the places left are parent -1, token -1, score -inf, done 0.  A logit that is NaN or
+ * +inf (or beyond 2^127) in a row that is read, or such a score, leaves the hypothesis
+ * without candidates and sets *err = 1 (err may be NULL).  Values are ordered by sums in pairs of fp32, the
+ * normaliser good to about 2^-23.  new_score may be score, new_done done; no other
+ * overlap.  V to 2^30.  workspace: 256-byte aligned, at least
+ * fp_op_beam_select_workspace_bytes(B, W, V) bytes (0: a shape that is refused); its
+ * leading 64 KB are ticket counters that must be zero before the first call; every call
+ * leaves them zero again, so one workspace serves any sequence of calls on one stream
+ * that it is large enough for (calls that overlap on the GPU need separate workspaces). */
+int fp_op_beam_select(const float* logits, int V, int B, int W, const float* score, const int32_t* done, int end_token,
+                      int32_t* parent, int32_t* token, float* new_score, int32_t* new_done, void* workspace,
+                      size_t workspace_bytes, int32_t* err, void* stream);
+size_t fp_op_beam_select_workspace_bytes(int B, int W, int V);
+
+/* Page tables that follow the chosen beams.  table_in int32 [B*W][pages_per_seq] is
+ * what the beams had, len int32 [B] their cached positions, parent as
+ * fp_op_beam_select writes it (-1: the beam stays as it is).  In table_out (another
+ * buffer) a beam has its parent's pages for the full blocks of page_size positions, shared,
+ * and its own for the blocks not begun.  The part-filled block (len[b] % page_size > 0)
+ * needs a page of its own for every beam, as table_in must have it: the first of a beam's children
+ * keeps its page, the others take, in order, the pages of the beams without children, in
+ * order, and for those copy_from and copy_to int32 [B*W] are the pages and copy_rows
+ * int32 [B*W] the rows that fp_op_kv_copy has to copy in every layer; all other places
+ * -1, -1, 0.  So pages are neither taken nor given back.  (A prompt's beams start from
+ * one: parent 0 throughout.)  A length outside
+ * [0, pages_per_seq * page_size] leaves the group's rows as they are, a parent outside
+ * [-1, W) is taken for -1; both set *err = 1 (err may be NULL).  page_size 16. */
+int fp_op_beam_reorder(int B, int W, int pages_per_seq, int page_size, const int32_t* len, const int32_t* parent,
+                       const int32_t* table_in, int32_t* table_out, int32_t* copy_from, int32_t* copy_to,
+                       int32_t* copy_rows, int32_t* err, void* stream);
+
+/* Pages copied within the pools: the first rows[i] positions of page from[i] to page
+ * to[i], all KV heads, K, V and an int8 cache's scales, for i < n (int32 [n] each);
+ * from[i] = -1 or rows[i] = 0: nothing.  No page may be written twice or both read and
+ * written in a call.  A page id outside the pool or rows[i] outside [0, page_size] sets
+ * *err = 1 (err may be NULL) and skips the copy.  Pools 16-byte aligned, else
+ * FP_ERR_UNSUPPORTED.  (The view's page table is not read.) */
+int fp_op_kv_copy(const fp_kv_view* kv, int n, const int32_t* from, const int32_t* to, const int32_t* rows,
+                  int32_t* err, void* stream);
+
 /* Test hook for the failure path of the pipelined tensor-core kernels (the
  * paper has no counterpart).  Every wait of those kernels is bounded; a role
  * whose wait runs out stops, the CTA drains its copies and MMAs in flight,
  * frees its tensor memory and records status 2 in the error word, which the
  * runtime reports as FP_ERR_DEVICE_ASSERT.  This sets how many polling rounds
  * the prefill GEMM's MMA thread waits for a stage of operands on the current
- * device, and the MMA warps of fp_op_attention_chunk for a tile of values in the
+ * device, and the MMA warps of fp_op_attention_chunk and fp_op_attention_tree for a tile of values in the
  * launches that follow: rounds >= 0 (0 gives up at once) or < 0 to restore the
  * default; all other waits keep the default.  Synchronous; not for use while
  * kernels of the library are running. */

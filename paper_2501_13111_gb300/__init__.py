@@ -42,6 +42,7 @@ KERNEL_CLASSES = ("embed", "rmsnorm", "lin_qkv", "rope_kv", "attn", "attn_combin
                   "lin_down", "lm_head", "argmax")
 FP_K_COUNT = len(KERNEL_CLASSES)
 FP_EPI_STORE, FP_EPI_RESID, FP_EPI_SWIGLU, FP_EPI_F32 = 0, 1, 2, 3
+FP_TREE_MAX_ROWS, FP_BEAM_MAX, FP_BEAM_MAX_GROUPS = 1024, 32, 16384
 
 
 class FPError(RuntimeError):
@@ -155,6 +156,17 @@ _PROTOS = {
     "fp_op_attention_chunk_workspace_bytes": (_SZ, [_I, _I, _I, _I, _I]),
     "fp_op_softmax": (_I, [_P, _I, _I, _P, _P, _P, _P]),
     "fp_op_verify_draft": (_I, [_P, _P, _I, _I, _I, _P, _P, _P, _P, _P, _P, _P, _P]),
+    "fp_op_tree_plan": (_I, [_P, _I, _I, _P, _I, _P, _P, _I, _P, _P]),
+    "fp_op_rope_kv_tree": (_I, [_P, _I, _I, _I, _I, C.POINTER(fp_kv_view), _P, _P, _P, _P, _P, _I, _P, _P]),
+    "fp_op_attention_tree": (_I, [_P, _I, _I, _I, _I, C.POINTER(fp_kv_view), _P, _P, _P, _I, _I, _I, _P, _P, _SZ, _P,
+                                  _P]),
+    "fp_op_attention_tree_workspace_bytes": (_SZ, [_I, _I, _I, _I, _I]),
+    "fp_op_verify_tree": (_I, [_P, _I, _I, _I, _P, _P, _P, _P, _P, _P, _P, _P, _P]),
+    "fp_op_kv_commit": (_I, [C.POINTER(fp_kv_view), _I, _I, _P, _P, _P, _P, _P]),
+    "fp_op_beam_select": (_I, [_P, _I, _I, _I, _P, _P, _I, _P, _P, _P, _P, _P, _SZ, _P, _P]),
+    "fp_op_beam_select_workspace_bytes": (_SZ, [_I, _I, _I]),
+    "fp_op_beam_reorder": (_I, [_I, _I, _I, _I, _P, _P, _P, _P, _P, _P, _P, _P, _P]),
+    "fp_op_kv_copy": (_I, [C.POINTER(fp_kv_view), _I, _P, _P, _P, _P, _P]),
     "fp_debug_set_wait_limit": (_I, [_LL]),
     "fp_solve_eq1": (_I, [_I, C.c_double, _I, C.c_double, C.POINTER(fp_eq1_fit)]),
     "fp_solve_eq23": (_I, [_I, C.POINTER(fp_eq1_fit), _I, C.POINTER(fp_eq1_fit), C.POINTER(fp_l2_terms)]),
@@ -394,8 +406,57 @@ def fp_op_verify_draft(p, q, V, n_tokens, B, cu, tokens, u_accept, u_draw, out_t
                                           stream))
 
 
+def fp_op_tree_plan(parent, n_tokens, B, cu, max_new, depth, mask, mask_stride, err=None, stream=None):
+    return _check(_lib.fp_op_tree_plan(parent, n_tokens, B, cu, max_new, depth, mask, mask_stride, err, stream))
+
+
+def fp_op_rope_kv_tree(qkv, row_stride, n_tokens, B, n_heads, kv: fp_kv_view, cu, pos, depth, rope_cs, q_out,
+                       q_out_stride, err=None, stream=None):
+    return _check(_lib.fp_op_rope_kv_tree(qkv, row_stride, n_tokens, B, n_heads, C.byref(kv), cu, pos, depth, rope_cs,
+                                          q_out, q_out_stride, err, stream))
+
+
+def fp_op_attention_tree_workspace_bytes(B, n_heads, n_kv_heads, head_dim, max_new):
+    return _lib.fp_op_attention_tree_workspace_bytes(B, n_heads, n_kv_heads, head_dim, max_new)
+
+
+def fp_op_attention_tree(q, q_stride, n_tokens, B, n_heads, kv: fp_kv_view, cu, pos, mask, mask_stride, max_new, max_len,
+                         out, workspace, workspace_bytes, err=None, stream=None):
+    return _check(_lib.fp_op_attention_tree(q, q_stride, n_tokens, B, n_heads, C.byref(kv), cu, pos, mask, mask_stride,
+                                            max_new, max_len, out, workspace, workspace_bytes, err, stream))
+
+
+def fp_op_verify_tree(p, V, n_tokens, B, cu, parent, tokens, u, path, out_tokens, n_out, err=None, stream=None):
+    return _check(_lib.fp_op_verify_tree(p, V, n_tokens, B, cu, parent, tokens, u, path, out_tokens, n_out, err, stream))
+
+
+def fp_op_kv_commit(kv: fp_kv_view, n_tokens, B, cu, pos, path, err=None, stream=None):
+    return _check(_lib.fp_op_kv_commit(C.byref(kv), n_tokens, B, cu, pos, path, err, stream))
+
+
+def fp_op_beam_select_workspace_bytes(B, W, V):
+    return _lib.fp_op_beam_select_workspace_bytes(B, W, V)
+
+
+def fp_op_beam_select(logits, V, B, W, score, done, end_token, parent, token, new_score, new_done, workspace,
+                      workspace_bytes, err=None, stream=None):
+    return _check(_lib.fp_op_beam_select(logits, V, B, W, score, done, end_token, parent, token, new_score, new_done,
+                                         workspace, workspace_bytes, err, stream))
+
+
+def fp_op_beam_reorder(B, W, pages_per_seq, page_size, lens, parent, table_in, table_out, copy_from, copy_to, copy_rows,
+                       err=None, stream=None):
+    return _check(_lib.fp_op_beam_reorder(B, W, pages_per_seq, page_size, lens, parent, table_in, table_out, copy_from,
+                                          copy_to, copy_rows, err, stream))
+
+
+def fp_op_kv_copy(kv: fp_kv_view, n, copy_from, copy_to, rows, err=None, stream=None):
+    return _check(_lib.fp_op_kv_copy(C.byref(kv), n, copy_from, copy_to, rows, err, stream))
+
+
 def fp_debug_set_wait_limit(rounds):
-    """Test hook: polling rounds of the prefill GEMM's stage wait and the chunk attention's V wait (< 0: default)."""
+    """Test hook: polling rounds of the prefill GEMM's stage wait and the chunk and tree attention's V wait (< 0:
+    default)."""
     return _check(_lib.fp_debug_set_wait_limit(rounds))
 
 

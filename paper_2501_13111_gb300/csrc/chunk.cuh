@@ -1,11 +1,12 @@
 // Ragged batches of new tokens, shared by the chunk kernels (fp_chunk.cu,
-// fp_attn_chunk.cu, fp_verify.cu): sequence b's rows are cu[b] .. cu[b+1]-1 of
+// attn_chunk.cuh, fp_tree.cu, fp_verify.cu): sequence b's rows are cu[b] .. cu[b+1]-1 of
 // the packed buffers, at positions pos[b] on.  cu and pos live on the device,
 // so nothing on the host has seen them: every index taken from them is checked
 // here before it is used.
 #pragma once
 
 #include "common.cuh"
+#include "../../include/fp_ops.h"
 
 namespace fpk {
 
@@ -31,6 +32,15 @@ FP_DEV int chunk_owner(const int32_t* cu, int B, int row) {
     lo += n * step;
   }
   return lo > 0 && row < __ldg(cu + lo) ? lo - 1 : -1;
+}
+
+// Where position p of sequence b lives: the row of head 0 in the pools (heads are
+// page_size rows apart), or -1 for a position outside the cache or a bad page.
+FP_DEV long long cache_row(const fp_kv_view& kv, int b, long long p) {
+  if (p < 0 || p >= (long long)kv.pages_per_seq * kv.page_size) return -1;
+  const int page = __ldg(kv.page_table + (long long)b * kv.pages_per_seq + (int)p / kv.page_size);
+  if (page < 0 || page >= kv.n_pages) return -1;
+  return (long long)page * kv.n_kv_heads * kv.page_size + (int)p % kv.page_size;
 }
 
 // A whole block looks cu over: *err = 1 where it decreases or leaves [0, n_tokens].

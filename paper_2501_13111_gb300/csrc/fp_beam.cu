@@ -1,0 +1,377 @@
+// Beam search over the LM head's logits: the best continuations of each group of beams,
+// page tables that follow the chosen beams, and the copies of part-filled pages.
+#include <algorithm>
+
+#include "chunk.cuh"
+#include "kernels.cuh"
+#include "pair.cuh"
+
+namespace fpk {
+
+// ------------------------------------------------------------------ selection
+// The W best of score_w + x_wt - lse(x_w) over the W beams and V tokens of a group, ties to
+// the lowest (w, t).  A beam's order is its logits' order, so one pass finds both its
+// normaliser and its W candidates: a CTA takes a piece of a row, holds it in registers and
+// leaves the piece's sum of exponentials and its W largest logits, in order; the last CTA
+// of the group to finish merges each beam's pieces, then the beams.
+// Two candidates of different beams must fall as 64 bits would have them, so scores are
+// pairs of fp32.  The normaliser: with an integer reference k (the maximum's log2,
+// rounded up), sum_i 2^(x_i log2 e - k) in fp32, one rounding an exponent; pieces with
+// other references are scaled exactly; lse = (k + exponent of s) ln 2 + log(significand of s).
+constexpr int kBsThreads = 512, kBsWarps = kBsThreads / 32, kBsItems = 8;
+constexpr int kBsPiece = kBsThreads * kBsItems * 4;  // values held at once
+constexpr int kBsSplits = 32;                        // pieces of a row, at most
+constexpr size_t kBsHead = FP_BEAM_MAX_GROUPS * 4;   // tickets, whatever the call's B
+
+// A logit and its token as one number: larger logits first, then lower tokens.  0: none
+// (-inf too: a banned token).
+FP_DEV uint32_t bs_ordered(float x) {
+  const uint32_t u = __float_as_uint(x);
+  return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+FP_DEV float bs_value(uint32_t o) { return __uint_as_float(o & 0x80000000u ? o ^ 0x80000000u : ~o); }
+FP_DEV unsigned long long bs_key(float x, int t) {
+  return x > -INFINITY ? (unsigned long long)bs_ordered(x + 0.f) << 32 | (uint32_t)~t : 0ull;
+}
+FP_DEV unsigned long long bs_warp_max(unsigned long long k) {
+  const uint32_t hi = __reduce_max_sync(0xffffffffu, (uint32_t)(k >> 32));
+  const uint32_t lo = __reduce_max_sync(0xffffffffu, (uint32_t)(k >> 32) == hi ? (uint32_t)k : 0u);
+  return (unsigned long long)hi << 32 | lo;
+}
+FP_DEV float bs_ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// 2^d, d <= 0 an integer
+FP_DEV float bs_pow2(float d) { return d < -126.f ? 0.f : __uint_as_float((uint32_t)(127 + (int)d) << 23); }
+
+// A set's reference and its sum against it (-inf: nothing in it)
+struct BsSum {
+  float k, s;
+};
+FP_DEV BsSum bs_add(BsSum a, BsSum b) {
+  const float k = fmaxf(a.k, b.k);
+  if (k == -INFINITY) return {k, a.s + b.s};
+  return {k, a.s * bs_pow2(a.k - k) + b.s * bs_pow2(b.k - k)};
+}
+
+struct BsArgs {
+  const float* x;
+  int V, B, W, S, per;  // pieces a row, values a piece (a multiple of 4)
+  const float* score;
+  const int32_t* done;
+  int end;
+  int32_t *parent, *token;
+  float* new_score;
+  int32_t* new_done;
+  int32_t* tickets;           // [B]
+  float2* sums;               // [B W S]
+  unsigned long long* best;   // [B W S][W]
+  int32_t* err;
+};
+
+__global__ void __launch_bounds__(kBsThreads) beam_select_kernel(const BsArgs a) {
+  __shared__ unsigned long long s_best[2][kBsWarps], s_list[2][FP_BEAM_MAX];
+  __shared__ BsSum s_sum[kBsWarps];
+  __shared__ int s_last;
+  __shared__ Pair s_off[FP_BEAM_MAX];                                    // score - lse of a beam
+  __shared__ unsigned long long s_row[FP_BEAM_MAX][FP_BEAM_MAX];         // its candidates
+  pdl_trigger();
+  pdl_wait();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, W = a.W, S = a.S;
+  const int row = blockIdx.x / S, piece = blockIdx.x - row * S, b = row / W;
+  const float score = __ldg(a.score + row);
+  const bool ended = a.done && __ldg(a.done + row) != 0;
+  if (!ended && score > -INFINITY) {
+    const float* x = a.x + (long long)row * a.V;
+    const long long lo = (long long)piece * a.per;
+    const int end = (int)min((long long)a.V, lo + a.per);
+    const bool vec = ((uintptr_t)(x + lo) & 15) == 0;
+    BsSum sum = {-INFINITY, 0.f};
+    int list = 0;  // which of the two holds the best so far
+    if (threadIdx.x < FP_BEAM_MAX) s_list[0][threadIdx.x] = 0;
+    __syncthreads();
+    for (long long c0 = lo; c0 < end; c0 += kBsPiece) {
+      // this thread's values: four tokens from c0 + 4 (i kBsThreads + thread) on
+      float v[kBsItems][4];
+#pragma unroll
+      for (int i = 0; i < kBsItems; ++i) {
+        const long long t = c0 + 4 * (i * kBsThreads + (int)threadIdx.x);
+        if (vec && t + 3 < end) {
+          const float4 f = __ldg(reinterpret_cast<const float4*>(x + t));
+          v[i][0] = f.x, v[i][1] = f.y, v[i][2] = f.z, v[i][3] = f.w;
+        } else {
+#pragma unroll
+          for (int y = 0; y < 4; ++y) v[i][y] = t + y < end ? __ldg(x + t + y) : -INFINITY;
+        }
+      }
+      float m = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < kBsItems; ++i) m = fmaxf(m, fmaxf(fmaxf(v[i][0], v[i][1]), fmaxf(v[i][2], v[i][3])));
+      m = warp_max(m);
+      {
+        // x log2 e in two parts (public constant: 1.4426950408889634)
+        constexpr float kHi = 1.44269502162933349609375f, kLo = 1.92596299e-8f;
+        const float k = m == -INFINITY ? 0.f : ceilf(m * kHi);
+        float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < kBsItems; ++i)
+#pragma unroll
+          for (int y = 0; y < 4; ++y) s[y] += bs_ex2(v[i][y] == -INFINITY ? -INFINITY : fmaf(v[i][y], kLo, fmaf(v[i][y], kHi, -k)));
+        const float t = warp_sum((s[0] + s[1]) + (s[2] + s[3]));
+        sum = bs_add(sum, {m == -INFINITY && t == 0.f ? -INFINITY : k, t});
+      }
+      // the W largest of these and of those before, one after the other
+      unsigned long long mine = threadIdx.x < W ? s_list[list][threadIdx.x] : 0ull, best = mine, won = ~0ull;
+      auto look = [&]() {  // the largest below the last winner
+        best = mine < won ? mine : 0ull;
+#pragma unroll
+        for (int i = 0; i < kBsItems; ++i)
+#pragma unroll
+          for (int y = 0; y < 4; ++y) {
+            const unsigned long long k = bs_key(v[i][y], (int)(c0 + 4 * (i * kBsThreads + (int)threadIdx.x)) + y);
+            if (k < won && k > best) best = k;
+          }
+      };
+      look();
+      for (int r = 0; r < W; ++r) {
+        const unsigned long long wm = bs_warp_max(best);
+        if (lane == 0) s_best[r & 1][warp] = wm;
+        __syncthreads();
+        won = bs_warp_max(lane < kBsWarps ? s_best[r & 1][lane] : 0ull);
+        if (threadIdx.x == 0) s_list[list ^ 1][r] = won;
+        if (best == won && won != 0) look();
+      }
+      list ^= 1;
+      __syncthreads();
+    }
+    if (lane == 0) s_sum[warp] = sum;
+    __syncthreads();
+    if (warp == 0) {
+      BsSum p = lane < kBsWarps ? s_sum[lane] : BsSum{-INFINITY, 0.f};
+#pragma unroll
+      for (int o = kBsWarps / 2; o > 0; o >>= 1)
+        p = bs_add(p, {__shfl_xor_sync(0xffffffffu, p.k, o), __shfl_xor_sync(0xffffffffu, p.s, o)});
+      if (lane == 0) a.sums[blockIdx.x] = make_float2(p.k, p.s);
+      if (lane < W) a.best[(long long)blockIdx.x * W + lane] = s_list[list][lane];
+      __threadfence();
+    }
+  }
+  __syncthreads();
+  // the last CTA of the group
+  if (threadIdx.x == 0) {
+    const bool last = atomicAdd(a.tickets + b, 1) == W * S - 1;
+    if (last) a.tickets[b] = 0;
+    s_last = last;
+  }
+  __syncthreads();
+  if (!s_last) return;
+  __threadfence();
+  // each beam: its normaliser, and the W best of its pieces
+  for (int w = warp; w < W; w += kBsWarps) {
+    const int r = b * W + w;
+    const float sc = __ldcg(a.score + r);
+    if (!(sc > -INFINITY && sc < INFINITY) || (a.done && __ldcg(a.done + r) != 0)) {
+      // no candidates, or the one that keeps it as it is
+      const bool kept = sc > -INFINITY && sc < INFINITY;
+      if (!kept && sc != -INFINITY && lane == 0 && a.err) atomicExch(a.err, 1);
+      if (lane < W) s_row[w][lane] = kept && lane == 0 ? 1ull << 32 | (uint32_t)~a.end : 0ull;
+      if (lane == 0) s_off[w] = {sc, 0.f};
+      continue;
+    }
+    BsSum p = {-INFINITY, 0.f};
+    if (lane < S) {
+      const float2 f = __ldcg(a.sums + (long long)r * S + lane);
+      p = {f.x, f.y};
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+      p = bs_add(p, {__shfl_xor_sync(0xffffffffu, p.k, o), __shfl_xor_sync(0xffffffffu, p.s, o)});
+    const bool fine = p.s > 0.f && p.s < INFINITY;  // (a NaN or +inf among the logits: neither)
+    if (!fine && p.k != -INFINITY && lane == 0 && a.err) atomicExch(a.err, 1);
+    if (lane == 0) {
+      const int e = (int)(__float_as_uint(p.s) >> 23) - 127 + 1;  // s = 2^e f, 1/2 <= f < 1 (s >= 2^-126: against its largest)
+      const float f = __uint_as_float((__float_as_uint(p.s) & 0x7fffffu) | 0x3f000000u), n = p.k + (float)e;
+      // n ln 2 as a pair (0.693147180559945309), its error carried along
+      constexpr float kHi = 0.693147182464599609375f, kLo = -1.904654299957767e-9f;
+      const float h = __fmul_rn(n, kHi);
+      const Pair lse = add(tidy(h, __fmaf_rn(n, kLo, __fmaf_rn(n, kHi, -h))), Pair{logf(f), 0.f});
+      s_off[w] = add(Pair{sc, 0.f}, Pair{-lse.hi, -lse.lo});
+    }
+    // lane s holds piece s's list; its head is what the lane offers
+    const unsigned long long* mine = a.best + ((long long)r * S + lane) * W;
+    int at = 0;
+    unsigned long long head = fine && lane < S ? __ldcg(mine) : 0ull;
+    for (int c = 0; c < W; ++c) {
+      const unsigned long long k = bs_warp_max(head);
+      if (lane == 0) s_row[w][c] = k;
+      if (k != 0 && head == k) head = ++at < W ? __ldcg(mine + at) : 0ull;
+    }
+  }
+  __syncthreads();
+  if (warp > 0) return;
+  // the beams, lane w's list being beam w's: scores as pairs, ties to the lowest beam and,
+  // in a beam, the order of its list
+  const Pair off = lane < W ? s_off[lane] : Pair{0.f, 0.f};
+  const bool was = lane < W && a.done && __ldcg(a.done + b * W + lane) != 0;  // (new_done may be done)
+  __syncwarp();
+  int at = 0;
+  uint32_t hi, lo, ft;
+  auto offer = [&]() {
+    const unsigned long long k = lane < W && at < W ? s_row[lane][at] : 0ull;
+    ft = (uint32_t)k;
+    hi = lo = 0;
+    if (k == 0) return;
+    Pair v = off;
+    if (!(k >> 32 == 1)) v = add(sum2(bs_value((uint32_t)(k >> 32)), off.hi), Pair{off.lo, 0.f});
+    hi = bs_ordered(v.hi + 0.f), lo = bs_ordered(v.lo + 0.f);
+  };
+  offer();
+  for (int c = 0; c < W; ++c) {
+    const uint32_t mh = __reduce_max_sync(0xffffffffu, hi);
+    const uint32_t ml = __reduce_max_sync(0xffffffffu, hi == mh ? lo : 0u);
+    const int win = __ffs(__ballot_sync(0xffffffffu, hi == mh && lo == ml)) - 1;
+    if (lane == win) {
+      const int o = b * W + c, t = (int)~ft;
+      const bool none = mh == 0;
+      a.parent[o] = none ? -1 : win;
+      a.token[o] = none ? -1 : t;
+      a.new_score[o] = none ? -INFINITY : bs_value(mh);
+      if (a.new_done) a.new_done[o] = !none && (was || t == a.end);
+      ++at;
+      offer();
+    }
+    __syncwarp();
+  }
+}
+
+// Pieces of a row: as many as it needs to be held in registers, more where the rows do not
+// fill the GPU.
+static int bs_splits(int rows, int V) {
+  int S = std::min(kBsSplits, (V + kBsPiece - 1) / kBsPiece);
+  while (2 * S <= kBsSplits && (long long)rows * S < 152 && V / S >= 4096) S *= 2;
+  return S;
+}
+
+static size_t bs_align(size_t n) { return (n + 255) / 256 * 256; }
+
+size_t beam_select_ws_bytes(int B, int W, int V) {
+  const size_t rows = (size_t)B * W, S = bs_splits((int)rows, V);
+  return kBsHead + bs_align(rows * S * 8) + rows * S * W * 8;
+}
+
+cudaError_t launch_beam_select(const float* logits, int V, int B, int W, const float* score, const int32_t* done, int end,
+                               int32_t* parent, int32_t* token, float* new_score, int32_t* new_done, void* ws, int32_t* err,
+                               cudaStream_t s) {
+  if (B <= 0) return cudaSuccess;
+  const int S = bs_splits(B * W, V);
+  uint8_t* p = (uint8_t*)ws;
+  uint8_t* sums = p + kBsHead;
+  uint8_t* best = sums + bs_align((size_t)B * W * S * 8);
+  const BsArgs a = {logits, V, B, W, S, ((V + S - 1) / S + 3) / 4 * 4, score, done, end, parent, token, new_score, new_done,
+                    (int32_t*)p, (float2*)sums, (unsigned long long*)best, err};
+  return launch(beam_select_kernel, dim3((unsigned)(B * W * S)), dim3(kBsThreads), 0, s, a);
+}
+
+// ------------------------------------------------------------------ reordering
+// Beam w's new row of the page table is its parent's: the pages of full blocks shared, the
+// blocks not begun its own.  The block that is part-filled has a page of its own for every
+// beam: the first of a beam's children takes its page as it is, the others, in order, the
+// pages of the beams without children (there are as many as are needed), into which the
+// parent's rows then have to be copied.  So nothing that is copied from is written to,
+// and no page is taken or given back.  One CTA a beam, its group's parents in a warp's
+// lanes.  Bound by latency.
+__global__ void __launch_bounds__(128)
+    beam_reorder_kernel(int W, int pps, int page_size, const int32_t* __restrict__ len, const int32_t* __restrict__ parent,
+                        const int32_t* __restrict__ in, int32_t* __restrict__ out, int32_t* __restrict__ from,
+                        int32_t* __restrict__ to, int32_t* __restrict__ rows, int32_t* err) {
+  pdl_trigger();
+  pdl_wait();
+  const int b = blockIdx.x / W, w = blockIdx.x - b * W, lane = threadIdx.x & 31;
+  const int32_t* group = in + (long long)b * W * pps;
+  const int n = __ldg(len + b);
+  const bool bad_len = n < 0 || n > (long long)pps * page_size;
+  int p = lane < W ? __ldg(parent + b * W + lane) : -1;
+  const bool bad = p < -1 || p >= W;
+  if (bad) p = -1;
+  if (__any_sync(0xffffffffu, bad || bad_len) && threadIdx.x == 0 && err) atomicExch(err, 1);
+  if (bad_len) p = lane < W ? lane : -1;  // the group stays as it is
+  const unsigned same = __match_any_sync(0xffffffffu, p);
+  const bool keeps = p >= 0 && __ffs(same) - 1 == lane;
+  const unsigned born = __reduce_or_sync(0xffffffffu, p >= 0 ? 1u << p : 0u);
+  unsigned spare = ~born & (W == 32 ? ~0u : (1u << W) - 1);
+  const unsigned others = __ballot_sync(0xffffffffu, lane < W && !keeps);
+  const int mine = __shfl_sync(0xffffffffu, p, w);
+  const bool kept = __shfl_sync(0xffffffffu, (int)keeps, w);
+  for (int i = __popc(others & ((1u << w) - 1)); i > 0; --i) spare &= spare - 1;
+  const int page_of = kept ? mine : __ffs(spare) - 1;  // whose page of the part-filled block this beam takes
+  const int tail = bad_len ? pps : n / page_size, rem = bad_len ? 0 : n % page_size;
+  const int32_t* own = group + (long long)w * pps;
+  const int32_t* came = mine >= 0 ? group + (long long)mine * pps : own;
+  int32_t* o = out + (long long)blockIdx.x * pps;
+  for (int i = threadIdx.x; i < pps; i += 128)
+    o[i] = i < tail ? __ldg(came + i) : i == tail && rem > 0 ? __ldg(group + (long long)page_of * pps + i) : __ldg(own + i);
+  if (threadIdx.x == 0) {
+    const bool copy = rem > 0 && mine >= 0 && !kept;
+    from[blockIdx.x] = copy ? __ldg(came + tail) : -1;
+    to[blockIdx.x] = copy ? __ldg(group + (long long)page_of * pps + tail) : -1;
+    rows[blockIdx.x] = copy ? rem : 0;
+  }
+}
+
+cudaError_t launch_beam_reorder(int B, int W, int pps, int page_size, const int32_t* len, const int32_t* parent,
+                                const int32_t* in, int32_t* out, int32_t* from, int32_t* to, int32_t* rows, int32_t* err,
+                                cudaStream_t s) {
+  if (B <= 0) return cudaSuccess;
+  return launch(beam_reorder_kernel, dim3(B * W), dim3(128), 0, s, W, pps, page_size, len, parent, in, out, from, to, rows,
+                err);
+}
+
+// ------------------------------------------------------------------ copies of pages
+// The first rows of one page to another, all KV heads, K, V and scales.  A head's rows
+// stand together, so a copy is 2 Hkv runs; a warp takes a run, 16 bytes a lane, all of it
+// on its way before the first is written.  Bound by latency, then bytes.
+constexpr int kKcWarps = 8;
+
+template <int RB>  // bytes of a head's row
+__global__ void __launch_bounds__(kKcWarps * 32)
+    kv_copy_kernel(fp_kv_view kv, const int32_t* __restrict__ from, const int32_t* __restrict__ to,
+                   const int32_t* __restrict__ rows, int32_t* err) {
+  pdl_trigger();
+  pdl_wait();
+  const int i = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int src = __ldg(from + i), dst = __ldg(to + i), n = __ldg(rows + i);
+  if (src == -1 || n == 0) return;
+  if (src < 0 || src >= kv.n_pages || dst < 0 || dst >= kv.n_pages || n < 0 || n > kv.page_size) {
+    if (threadIdx.x == 0 && err) atomicExch(err, 1);
+    return;
+  }
+  for (int item = blockIdx.y * kKcWarps + warp; item < 2 * kv.n_kv_heads; item += gridDim.y * kKcWarps) {
+    const bool is_v = item >= kv.n_kv_heads;
+    const int h = is_v ? item - kv.n_kv_heads : item;
+    const long long r0 = ((long long)src * kv.n_kv_heads + h) * kv.page_size, r1 = ((long long)dst * kv.n_kv_heads + h) * kv.page_size;
+    uint8_t* pool = (uint8_t*)(is_v ? kv.v_pool : kv.k_pool);
+    constexpr int N = RB / 32;  // 16-byte pieces a lane has of sixteen rows
+    uint4 v[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+      if ((k * 32 + lane) * 16 < n * RB) v[k] = *reinterpret_cast<const uint4*>(pool + r0 * RB + (k * 32 + lane) * 16);
+    float* scale = kv.kvquant == FP_KV_INT8 ? (is_v ? kv.v_scale : kv.k_scale) : nullptr;
+    if (scale && lane < n) scale[r1 + lane] = scale[r0 + lane];
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+      if ((k * 32 + lane) * 16 < n * RB) *reinterpret_cast<uint4*>(pool + r1 * RB + (k * 32 + lane) * 16) = v[k];
+  }
+}
+
+cudaError_t launch_kv_copy(const fp_kv_view& kv, int n, const int32_t* from, const int32_t* to, const int32_t* rows,
+                           int32_t* err, cudaStream_t s) {
+  if (n <= 0) return cudaSuccess;
+  const dim3 grid(n, std::min((2 * kv.n_kv_heads + kKcWarps - 1) / kKcWarps, 1024));
+  auto go = [&](auto kern) { return launch(kern, grid, dim3(kKcWarps * 32), 0, s, kv, from, to, rows, err); };
+  const int rb = kv.head_dim * (kv.kvquant == FP_KV_INT8 ? 1 : 2);
+  return rb == 64 ? go(kv_copy_kernel<64>) : rb == 128 ? go(kv_copy_kernel<128>) : go(kv_copy_kernel<256>);
+}
+
+}  // namespace fpk

@@ -7,15 +7,6 @@
 
 namespace fpk {
 
-// Where position p of sequence b lives: the row of head 0 in the pools (heads are
-// page_size rows apart), or -1 for a position outside the cache or a bad page.
-FP_DEV long long cache_row(const fp_kv_view& kv, int b, long long p) {
-  if (p < 0 || p >= (long long)kv.pages_per_seq * kv.page_size) return -1;
-  const int page = __ldg(kv.page_table + (long long)b * kv.pages_per_seq + (int)p / kv.page_size);
-  if (page < 0 || page >= kv.n_pages) return -1;
-  return (long long)page * kv.n_kv_heads * kv.page_size + (int)p % kv.page_size;
-}
-
 FP_DEV void unpack8(uint4 v, float* f) {
   const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
@@ -50,11 +41,12 @@ FP_DEV uint2 codes8(const float* x, float s) {
 // 4 x up to 1000 rows of 40 heads take 64 us (5.4 TB/s), 160 rows of 64 heads on 8, int8, 7.4.
 // Four CTAs an SM, for the loads in flight: 64 registers, a few of 74 spilled (three: 68 us,
 // five: 71).
-template <int HD, bool KV8>
+// TREE: a row's place in the cache is pos[b] + i, what it is rotated by pos[b] + depth[row].
+template <int HD, bool KV8, bool TREE>
 __global__ void __launch_bounds__(256, 4)
     rope_kv_chunk_kernel(const uint16_t* qkv, int row_stride, int n_tokens, int B, int H, fp_kv_view kv,
-                         const int32_t* __restrict__ cu, const int32_t* __restrict__ pos, const float* __restrict__ cs,
-                         uint16_t* q_out, int q_out_stride, int32_t* err) {
+                         const int32_t* __restrict__ cu, const int32_t* __restrict__ pos,
+                         const int32_t* __restrict__ depth, const float* __restrict__ cs, uint16_t* q_out, int q_out_stride, int32_t* err) {
   pdl_trigger();
   pdl_wait();
   constexpr int L = HD / 16;  // lanes a head
@@ -67,14 +59,16 @@ __global__ void __launch_bounds__(256, 4)
   const int b = chunk_owner(cu, B, m);
   if (b < 0) return;
   const long long p = (long long)__ldg(pos + b) + (m - __ldg(cu + b));
-  if (p < 0 || p >= (long long)kv.pages_per_seq * kv.page_size) {
+  const long long most = (long long)kv.pages_per_seq * kv.page_size;
+  const long long at = TREE ? (long long)__ldg(pos + b) + __ldg(depth + m) : p;  // the position it is rotated by
+  if (p < 0 || p >= most || (TREE && (at < 0 || at >= most))) {
     if (threadIdx.x == 0 && err) atomicExch(err, 1);
     return;
   }
   const long long row = cache_row(kv, b, p);
   if (row < 0 && threadIdx.x == 0 && err) atomicExch(err, 1);
   float co[8], si[8];
-  const float4* t = reinterpret_cast<const float4*>(cs + p * HD + 16 * c);
+  const float4* t = reinterpret_cast<const float4*>(cs + at * HD + 16 * c);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const float4 f = __ldg(t + i);
@@ -128,17 +122,32 @@ __global__ void __launch_bounds__(256, 4)
   }
 }
 
-cudaError_t launch_rope_kv_chunk(const uint16_t* qkv, int row_stride, int n_tokens, int B, int n_heads,
-                                 const fp_kv_view& kv, const int32_t* cu, const int32_t* pos, const float* rope_cs,
+template <bool TREE>
+static cudaError_t launch_append(const uint16_t* qkv, int row_stride, int n_tokens, int B, int n_heads, const fp_kv_view& kv,
+                                 const int32_t* cu, const int32_t* pos, const int32_t* depth, const float* rope_cs,
                                  uint16_t* q_out, int q_out_stride, int32_t* err, cudaStream_t s) {
   if (n_tokens <= 0 || B <= 0) return cudaSuccess;
   auto go = [&](auto kern) {
-    return launch(kern, dim3(n_tokens), dim3(256), 0, s, qkv, row_stride, n_tokens, B, n_heads, kv, cu, pos, rope_cs,
-                  q_out, q_out_stride, err);
+    return launch(kern, dim3(n_tokens), dim3(256), 0, s, qkv, row_stride, n_tokens, B, n_heads, kv, cu, pos, depth,
+                  rope_cs, q_out, q_out_stride, err);
   };
-  if (kv.head_dim == 64)
-    return kv.kvquant == FP_KV_INT8 ? go(rope_kv_chunk_kernel<64, true>) : go(rope_kv_chunk_kernel<64, false>);
-  return kv.kvquant == FP_KV_INT8 ? go(rope_kv_chunk_kernel<128, true>) : go(rope_kv_chunk_kernel<128, false>);
+  const bool i8 = kv.kvquant == FP_KV_INT8;
+  if (kv.head_dim == 64) return i8 ? go(rope_kv_chunk_kernel<64, true, TREE>) : go(rope_kv_chunk_kernel<64, false, TREE>);
+  return i8 ? go(rope_kv_chunk_kernel<128, true, TREE>) : go(rope_kv_chunk_kernel<128, false, TREE>);
+}
+
+cudaError_t launch_rope_kv_chunk(const uint16_t* qkv, int row_stride, int n_tokens, int B, int n_heads,
+                                 const fp_kv_view& kv, const int32_t* cu, const int32_t* pos, const float* rope_cs,
+                                 uint16_t* q_out, int q_out_stride, int32_t* err, cudaStream_t s) {
+  return launch_append<false>(qkv, row_stride, n_tokens, B, n_heads, kv, cu, pos, nullptr, rope_cs, q_out, q_out_stride,
+                              err, s);
+}
+
+cudaError_t launch_rope_kv_tree(const uint16_t* qkv, int row_stride, int n_tokens, int B, int n_heads,
+                                const fp_kv_view& kv, const int32_t* cu, const int32_t* pos, const int32_t* depth,
+                                const float* rope_cs, uint16_t* q_out, int q_out_stride, int32_t* err, cudaStream_t s) {
+  return launch_append<true>(qkv, row_stride, n_tokens, B, n_heads, kv, cu, pos, depth, rope_cs, q_out, q_out_stride, err,
+                             s);
 }
 
 // ------------------------------------------------------------------ read back

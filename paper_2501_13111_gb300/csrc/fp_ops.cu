@@ -203,9 +203,9 @@ static int check_chunk(const fp_kv_view* kv, int n_tokens, int B, const int32_t*
   return FP_OK;
 }
 
-int fp_op_rope_kv_chunk(const uint16_t* qkv, int row_stride, int n_tokens, int B, int n_heads, const fp_kv_view* kv,
-                        const int32_t* cu, const int32_t* pos, const float* rope_cs, uint16_t* q_out, int q_out_stride,
-                        int32_t* err, void* stream) {
+static int check_append(const uint16_t* qkv, int row_stride, int n_tokens, int B, int n_heads, const fp_kv_view* kv,
+                        const int32_t* cu, const int32_t* pos, const float* rope_cs, const uint16_t* q_out,
+                        int q_out_stride) {
   int st = check_chunk(kv, n_tokens, B, cu, pos);
   if (st) return st;
   if (!qkv || !rope_cs || !q_out || n_heads <= 0 || n_heads % kv->n_kv_heads != 0) return FP_ERR_INVALID_ARG;
@@ -214,6 +214,14 @@ int fp_op_rope_kv_chunk(const uint16_t* qkv, int row_stride, int n_tokens, int B
   if (q_out == qkv && q_out_stride != row_stride) return FP_ERR_INVALID_ARG;  // rows would overlap others'
   if (row_stride % 8 || q_out_stride % 8 || !aligned16(qkv) || !aligned16(q_out) || !aligned16(rope_cs))
     return FP_ERR_UNSUPPORTED;
+  return FP_OK;
+}
+
+int fp_op_rope_kv_chunk(const uint16_t* qkv, int row_stride, int n_tokens, int B, int n_heads, const fp_kv_view* kv,
+                        const int32_t* cu, const int32_t* pos, const float* rope_cs, uint16_t* q_out, int q_out_stride,
+                        int32_t* err, void* stream) {
+  int st = check_append(qkv, row_stride, n_tokens, B, n_heads, kv, cu, pos, rope_cs, q_out, q_out_stride);
+  if (st) return st;
   return cuda_status(launch_rope_kv_chunk(qkv, row_stride, n_tokens, B, n_heads, *kv, cu, pos, rope_cs, q_out,
                                           q_out_stride, err, (cudaStream_t)stream));
 }
@@ -237,9 +245,11 @@ size_t fp_op_attention_chunk_workspace_bytes(int B, int n_heads, int n_kv_heads,
   return attention_chunk_ws_bytes(B, n_heads, n_kv_heads, head_dim, max_new);
 }
 
-int fp_op_attention_chunk(const uint16_t* q, int q_stride, int n_tokens, int B, int n_heads, const fp_kv_view* kv,
-                          const int32_t* cu, const int32_t* pos, int max_new, int max_len, uint16_t* out,
-                          void* workspace, size_t workspace_bytes, int32_t* err, void* stream) {
+// *work: whether there is anything to launch.
+static int check_attention(const uint16_t* q, int q_stride, int n_tokens, int B, int n_heads, const fp_kv_view* kv,
+                           const int32_t* cu, const int32_t* pos, int max_new, int max_len, const uint16_t* out,
+                           const void* workspace, size_t workspace_bytes, bool* work) {
+  *work = false;
   int st = check_chunk(kv, n_tokens, B, cu, pos);
   if (st) return st;
   if (!q || !out || n_heads <= 0 || n_heads % kv->n_kv_heads != 0 || max_new < 0 || max_len < 0)
@@ -253,6 +263,17 @@ int fp_op_attention_chunk(const uint16_t* q, int q_stride, int n_tokens, int B, 
   if (!workspace || ((uintptr_t)workspace & 255) ||
       workspace_bytes < attention_chunk_ws_bytes(B, n_heads, kv->n_kv_heads, kv->head_dim, max_new))
     return FP_ERR_INVALID_ARG;
+  *work = true;
+  return FP_OK;
+}
+
+int fp_op_attention_chunk(const uint16_t* q, int q_stride, int n_tokens, int B, int n_heads, const fp_kv_view* kv,
+                          const int32_t* cu, const int32_t* pos, int max_new, int max_len, uint16_t* out,
+                          void* workspace, size_t workspace_bytes, int32_t* err, void* stream) {
+  bool work;
+  int st = check_attention(q, q_stride, n_tokens, B, n_heads, kv, cu, pos, max_new, max_len, out, workspace,
+                           workspace_bytes, &work);
+  if (st || !work) return st;
   return cuda_status(launch_attention_chunk(q, q_stride, n_tokens, B, n_heads, *kv, cu, pos, max_new, max_len, out,
                                             workspace, err, (cudaStream_t)stream));
 }
@@ -272,6 +293,114 @@ int fp_op_verify_draft(const float* p, const float* q, int V, int n_tokens, int 
   if (V > (1 << 30) || B > (1 << 27)) return FP_ERR_UNSUPPORTED;
   return cuda_status(launch_verify_draft(p, q, V, n_tokens, B, cu, tokens, u_accept, u_draw, out_tokens, n_out, err,
                                          (cudaStream_t)stream));
+}
+
+// ---- trees of drafted tokens
+
+int fp_op_tree_plan(const int32_t* parent, int n_tokens, int B, const int32_t* cu, int max_new, int32_t* depth,
+                    uint32_t* mask, int mask_stride, int32_t* err, void* stream) {
+  if (!parent || n_tokens < 0 || B < 0 || !cu || max_new < 0 || !depth || !mask) return FP_ERR_INVALID_ARG;
+  if (mask_stride < (max_new + 31LL) / 32) return FP_ERR_INVALID_ARG;
+  if (max_new > FP_TREE_MAX_ROWS || mask_stride > (1 << 16) || n_tokens > (1 << 30) || B > (1 << 26))
+    return FP_ERR_UNSUPPORTED;
+  return cuda_status(
+      launch_tree_plan(parent, n_tokens, B, cu, max_new, depth, mask, mask_stride, err, (cudaStream_t)stream));
+}
+
+int fp_op_rope_kv_tree(const uint16_t* qkv, int row_stride, int n_tokens, int B, int n_heads, const fp_kv_view* kv,
+                       const int32_t* cu, const int32_t* pos, const int32_t* depth, const float* rope_cs,
+                       uint16_t* q_out, int q_out_stride, int32_t* err, void* stream) {
+  int st = check_append(qkv, row_stride, n_tokens, B, n_heads, kv, cu, pos, rope_cs, q_out, q_out_stride);
+  if (st) return st;
+  if (!depth) return FP_ERR_INVALID_ARG;
+  return cuda_status(launch_rope_kv_tree(qkv, row_stride, n_tokens, B, n_heads, *kv, cu, pos, depth, rope_cs, q_out,
+                                         q_out_stride, err, (cudaStream_t)stream));
+}
+
+size_t fp_op_attention_tree_workspace_bytes(int B, int n_heads, int n_kv_heads, int head_dim, int max_new) {
+  return fp_op_attention_chunk_workspace_bytes(B, n_heads, n_kv_heads, head_dim, max_new);
+}
+
+int fp_op_attention_tree(const uint16_t* q, int q_stride, int n_tokens, int B, int n_heads, const fp_kv_view* kv,
+                         const int32_t* cu, const int32_t* pos, const uint32_t* mask, int mask_stride, int max_new,
+                         int max_len, uint16_t* out, void* workspace, size_t workspace_bytes, int32_t* err,
+                         void* stream) {
+  if (!mask || max_new < 0 || mask_stride < (max_new + 31LL) / 32) return FP_ERR_INVALID_ARG;
+  bool work;
+  int st = check_attention(q, q_stride, n_tokens, B, n_heads, kv, cu, pos, max_new, max_len, out, workspace,
+                           workspace_bytes, &work);
+  if (st || !work) return st;
+  return cuda_status(launch_attention_tree(q, q_stride, n_tokens, B, n_heads, *kv, cu, pos, mask, mask_stride, max_new,
+                                           max_len, out, workspace, err, (cudaStream_t)stream));
+}
+
+int fp_op_verify_tree(const float* p, int V, int n_tokens, int B, const int32_t* cu, const int32_t* parent,
+                      const int32_t* tokens, const float* u, int32_t* path, int32_t* out_tokens, int32_t* n_out,
+                      int32_t* err, void* stream) {
+  if (!p || V <= 0 || n_tokens < 0 || B < 0 || !cu || !parent || !tokens || !u || !path || !out_tokens || !n_out)
+    return FP_ERR_INVALID_ARG;
+  if (V > (1 << 30) || B > (1 << 27)) return FP_ERR_UNSUPPORTED;
+  return cuda_status(launch_verify_tree(p, V, n_tokens, B, cu, parent, tokens, u, path, out_tokens, n_out, err,
+                                        (cudaStream_t)stream));
+}
+
+int fp_op_kv_commit(const fp_kv_view* kv, int n_tokens, int B, const int32_t* cu, const int32_t* pos,
+                    const int32_t* path, int32_t* err, void* stream) {
+  int st = check_chunk(kv, n_tokens, B, cu, pos);
+  if (st) return st;
+  if (!path) return FP_ERR_INVALID_ARG;
+  return cuda_status(launch_kv_commit(*kv, n_tokens, B, cu, pos, path, err, (cudaStream_t)stream));
+}
+
+// ---- beams
+
+static int check_beams(int B, int W) {
+  if (B < 0 || W <= 0) return FP_ERR_INVALID_ARG;
+  if (W > FP_BEAM_MAX || B > FP_BEAM_MAX_GROUPS) return FP_ERR_UNSUPPORTED;
+  return FP_OK;
+}
+
+size_t fp_op_beam_select_workspace_bytes(int B, int W, int V) {
+  if (B <= 0 || check_beams(B, W) || V <= 0 || V > (1 << 30)) return 0;
+  return beam_select_ws_bytes(B, W, V);
+}
+
+int fp_op_beam_select(const float* logits, int V, int B, int W, const float* score, const int32_t* done, int end_token,
+                      int32_t* parent, int32_t* token, float* new_score, int32_t* new_done, void* workspace,
+                      size_t workspace_bytes, int32_t* err, void* stream) {
+  int st = check_beams(B, W);
+  if (st) return st;
+  if (!logits || V <= 0 || !score || !parent || !token || !new_score || end_token < -1 || end_token >= V)
+    return FP_ERR_INVALID_ARG;
+  if (done && end_token < 0) return FP_ERR_INVALID_ARG;
+  if (V > (1 << 30)) return FP_ERR_UNSUPPORTED;
+  if (B == 0) return FP_OK;
+  if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < beam_select_ws_bytes(B, W, V))
+    return FP_ERR_INVALID_ARG;
+  return cuda_status(launch_beam_select(logits, V, B, W, score, done, end_token, parent, token, new_score, new_done,
+                                        workspace, err, (cudaStream_t)stream));
+}
+
+int fp_op_beam_reorder(int B, int W, int pages_per_seq, int page_size, const int32_t* len, const int32_t* parent,
+                       const int32_t* table_in, int32_t* table_out, int32_t* copy_from, int32_t* copy_to,
+                       int32_t* copy_rows, int32_t* err, void* stream) {
+  int st = check_beams(B, W);
+  if (st) return st;
+  if (pages_per_seq <= 0 || page_size <= 0 || !len || !parent || !table_in || !table_out || table_in == table_out ||
+      !copy_from || !copy_to || !copy_rows)
+    return FP_ERR_INVALID_ARG;
+  if (page_size != 16 || pages_per_seq > (1 << 26)) return FP_ERR_UNSUPPORTED;
+  return cuda_status(launch_beam_reorder(B, W, pages_per_seq, page_size, len, parent, table_in, table_out, copy_from,
+                                         copy_to, copy_rows, err, (cudaStream_t)stream));
+}
+
+int fp_op_kv_copy(const fp_kv_view* kv, int n, const int32_t* from, const int32_t* to, const int32_t* rows,
+                  int32_t* err, void* stream) {
+  int st = fpk_check_kv(kv);
+  if (st) return st;
+  if (n < 0 || !from || !to || !rows) return FP_ERR_INVALID_ARG;
+  if (!aligned16(kv->k_pool) || !aligned16(kv->v_pool)) return FP_ERR_UNSUPPORTED;
+  return cuda_status(launch_kv_copy(*kv, n, from, to, rows, err, (cudaStream_t)stream));
 }
 
 }  // extern "C"

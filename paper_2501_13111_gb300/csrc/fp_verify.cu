@@ -7,6 +7,7 @@
 
 #include "chunk.cuh"
 #include "kernels.cuh"
+#include "pair.cuh"
 
 namespace cg = cooperative_groups;
 
@@ -238,44 +239,6 @@ cudaError_t launch_softmax(const float* logits, int M, int V, const float* temp,
 // second look follow one another.
 constexpr int kVfCTAs = 8, kVfThreads = 512, kVfWarps = kVfThreads / 32, kVfRuns = kVfCTAs * kVfWarps;
 
-struct Pair {
-  float hi, lo;
-};
-// a + b, exactly
-FP_DEV Pair sum2(float a, float b) {
-  const float s = __fadd_rn(a, b), v = __fsub_rn(s, a);
-  return {s, __fadd_rn(__fsub_rn(a, __fsub_rn(s, v)), __fsub_rn(b, v))};
-}
-// hi + lo with hi the nearer fp32 (|hi| >= |lo|)
-FP_DEV Pair tidy(float hi, float lo) {
-  const float s = __fadd_rn(hi, lo);
-  return {s, __fsub_rn(lo, __fsub_rn(s, hi))};
-}
-FP_DEV Pair add(Pair a, Pair b) {
-  const Pair s = sum2(a.hi, b.hi);
-  return tidy(s.hi, __fadd_rn(s.lo, __fadd_rn(a.lo, b.lo)));
-}
-FP_DEV Pair times(Pair a, float r) {
-  const float h = __fmul_rn(a.hi, r);
-  return tidy(h, __fmaf_rn(a.lo, r, __fmaf_rn(a.hi, r, -h)));
-}
-FP_DEV bool greater(Pair a, Pair b) {
-  const Pair d = sum2(a.hi, -b.hi);
-  return __fadd_rn(d.hi, __fadd_rn(d.lo, __fsub_rn(a.lo, b.lo))) > 0.f;
-}
-FP_DEV Pair shfl(Pair v, int l) { return {__shfl_sync(0xffffffffu, v.hi, l), __shfl_sync(0xffffffffu, v.lo, l)}; }
-
-// Inclusive sums over groups of N lanes, lower lanes first.
-template <int N>
-FP_DEV Pair scan(Pair v, int lane) {
-#pragma unroll
-  for (int o = 1; o < N; o <<= 1) {
-    const Pair f = {__shfl_up_sync(0xffffffffu, v.hi, o, N), __shfl_up_sync(0xffffffffu, v.lo, o, N)};
-    if ((lane & (N - 1)) >= o) v = add(f, v);
-  }
-  return v;
-}
-
 // Of the lanes whose weight counts, the first whose sum is past the border; rounding at
 // the very end, an r of 1 or more or a NaN leaves none: the last then.  -1: no weight at all.
 FP_DEV int holder(Pair upto, float w, Pair border) {
@@ -432,6 +395,124 @@ cudaError_t launch_verify_draft(const float* p, const float* q, int V, int n_tok
   if (B <= 0) return cudaSuccess;
   return launch(verify_kernel, dim3(B * kVfCTAs), dim3(kVfThreads), 0, s, p, q, V, n_tokens, B, cu, tokens, u, r, out,
                 n_out, err);
+}
+
+// ------------------------------------------------------------------ verification of a tree
+// From row 0 of a sequence's tree down: a token is drawn from the row's distribution, the
+// lowest t with sum_{s <= t} p_s > u sum p; the row's child with that token is the next
+// row, and where it has none the token is the one after the accepted ones.  What comes
+// out is distributed as p, whatever was drafted.  Each step as in the verification above,
+// the sums in pairs; the warp that finds the token finds the child, and tells the cluster.
+__global__ void __cluster_dims__(kVfCTAs, 1, 1) __launch_bounds__(kVfThreads)
+    verify_tree_kernel(const float* __restrict__ p, int V, int n_tokens, int B, const int32_t* __restrict__ cu,
+                       const int32_t* __restrict__ parent, const int32_t* __restrict__ tokens,
+                       const float* __restrict__ u, int32_t* __restrict__ path, int32_t* __restrict__ out,
+                       int32_t* __restrict__ n_out, int32_t* err) {
+  __shared__ Pair s_sum[kVfWarps], s_cta;
+  __shared__ int s_next;
+  pdl_trigger();
+  pdl_wait();
+  cg::cluster_group cluster = cg::this_cluster();
+  const int rank = (int)cluster.block_rank(), b = blockIdx.x / kVfCTAs;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (blockIdx.x == 0) chunk_check(cu, B, n_tokens, err);
+  int row0, n;
+  chunk_rows(cu, b, n_tokens, &row0, &n);
+  if (n == 0) {  // (the whole cluster leaves)
+    if (rank == 0 && threadIdx.x == 0) n_out[b] = 0;
+    return;
+  }
+  const int run = (V + kVfRuns - 1) / kVfRuns;
+  const int lo = (int)min((long long)V, (long long)(rank * kVfWarps + warp) * run), hi = min(V, lo + run);
+  int cur = 0, a = 0;
+  for (;; ++a) {
+    const float* pr = p + (long long)(row0 + cur) * V;
+    const float r = __ldg(u + row0 + cur);
+    Pair s = {0.f, 0.f};
+#pragma unroll 1
+    for (int t0 = lo + lane; t0 < hi; t0 += 16 * 32) {  // sixteen loads in flight
+      float x[16];
+#pragma unroll
+      for (int k = 0; k < 16; ++k) x[k] = t0 + 32 * k < hi ? __ldg(pr + t0 + 32 * k) : 0.f;
+#pragma unroll
+      for (int k = 0; k < 16; ++k) {
+        const Pair f = sum2(s.hi, x[k] > 0.f ? x[k] : 0.f);
+        s = {f.hi, __fadd_rn(s.lo, f.lo)};
+      }
+    }
+    s = shfl(scan<32>(tidy(s.hi, s.lo), lane), 31);
+    if (lane == 0) s_sum[warp] = s;
+    __syncthreads();
+    const Pair mine = s_sum[lane & (kVfWarps - 1)], upto = scan<kVfWarps>(mine, lane);  // within this CTA
+    if (threadIdx.x == kVfWarps - 1) s_cta = upto;
+    cluster.sync();
+    const Pair theirs = *cluster.map_shared_rank(&s_cta, lane & (kVfCTAs - 1)), all = scan<kVfCTAs>(theirs, lane);
+    const Pair total = shfl(all, kVfCTAs - 1);
+    const bool drawable = total.hi > 0.f && total.hi < INFINITY;
+    if (drawable) {
+      const Pair border = times(total, r);
+      if (holder(all, lane < kVfCTAs ? theirs.hi : 0.f, border) == rank) {
+        const Pair before = rank ? shfl(all, rank - 1) : Pair{0.f, 0.f};
+        const Pair to = add(before, upto);
+        if (holder(to, lane < kVfWarps ? mine.hi : 0.f, border) == warp) {
+          const Pair from = warp ? shfl(to, warp - 1) : before;
+          // within the run: 32 pieces, then the tokens of the piece
+          const int seg = (hi - lo + 31) / 32;
+          Pair ps = {0.f, 0.f};
+#pragma unroll 4
+          for (int t = lo + lane * seg; t < min(hi, lo + (lane + 1) * seg); ++t) ps = add(ps, weight(pr, nullptr, t, -1));
+          const Pair pu = add(from, scan<32>(ps, lane));
+          const int piece = holder(pu, ps.hi, border);
+          Pair at = piece ? shfl(pu, piece - 1) : from;
+          int token = -1;
+          const int t1 = min(hi, lo + (piece + 1) * seg);
+#pragma unroll 1
+          for (int t0 = lo + piece * seg; t0 < t1; t0 += 32) {
+            const Pair w = t0 + lane < t1 ? weight(pr, nullptr, t0 + lane, -1) : Pair{0.f, 0.f};
+            const Pair wu = add(at, scan<32>(w, lane));
+            const int l = holder(wu, w.hi, border);
+            if (l >= 0) token = t0 + l;
+            if (__any_sync(0xffffffffu, w.hi > 0.f && greater(wu, border))) break;
+            at = shfl(wu, 31);
+          }
+          int child = -1;
+#pragma unroll 1
+          for (int i0 = cur + 1; i0 < n && child < 0; i0 += 32) {
+            const int i = i0 + lane;
+            const bool it = i < n && __ldg(parent + row0 + i) == cur && __ldg(tokens + row0 + i) == token;
+            const unsigned any = __ballot_sync(0xffffffffu, it);
+            if (any) child = i0 + __ffs(any) - 1;
+          }
+          if (lane == 0) out[row0 + a] = token, path[row0 + a] = cur;
+          if (lane < kVfCTAs) *cluster.map_shared_rank(&s_next, lane) = child;
+        }
+      }
+    }
+    cluster.sync();
+    if (!drawable) {
+      if (rank == 0 && threadIdx.x == 0) {
+        if (err) atomicExch(err, 1);
+        out[row0 + a] = -1, path[row0 + a] = cur;
+        n_out[b] = a;
+      }
+      break;
+    }
+    if (s_next < 0) {
+      if (rank == 0 && threadIdx.x == 0) n_out[b] = a + 1;
+      break;
+    }
+    cur = s_next;
+  }
+  if (rank == 0)
+    for (int i = a + 1 + (int)threadIdx.x; i < n; i += kVfThreads) out[row0 + i] = -1, path[row0 + i] = -1;
+}
+
+cudaError_t launch_verify_tree(const float* p, int V, int n_tokens, int B, const int32_t* cu, const int32_t* parent,
+                               const int32_t* tokens, const float* u, int32_t* path, int32_t* out, int32_t* n_out,
+                               int32_t* err, cudaStream_t s) {
+  if (B <= 0) return cudaSuccess;
+  return launch(verify_tree_kernel, dim3(B * kVfCTAs), dim3(kVfThreads), 0, s, p, V, n_tokens, B, cu, parent, tokens, u,
+                path, out, n_out, err);
 }
 
 }  // namespace fpk

@@ -65,6 +65,34 @@ cudaError_t launch_attention_chunk(const uint16_t* q, int q_stride, int n_tokens
                                    const fp_kv_view& kv, const int32_t* cu, const int32_t* pos, int max_new, int max_len,
                                    uint16_t* out, void* ws, int32_t* err, cudaStream_t s);
 void attention_chunk_wait_limit(long long rounds);  // fp_debug_set_wait_limit
+long long attention_chunk_wait_limit();
+
+// ---- trees of drafted tokens (fp_tree.cu, fp_chunk.cu, fp_attn_tree.cu, fp_verify.cu)
+cudaError_t launch_tree_plan(const int32_t* parent, int n_tokens, int B, const int32_t* cu, int max_new, int32_t* depth,
+                             uint32_t* mask, int mask_stride, int32_t* err, cudaStream_t s);
+cudaError_t launch_rope_kv_tree(const uint16_t* qkv, int row_stride, int n_tokens, int B, int n_heads,
+                                const fp_kv_view& kv, const int32_t* cu, const int32_t* pos, const int32_t* depth,
+                                const float* rope_cs, uint16_t* q_out, int q_out_stride, int32_t* err, cudaStream_t s);
+// (fits and workspace: as attention_chunk's)
+cudaError_t launch_attention_tree(const uint16_t* q, int q_stride, int n_tokens, int B, int n_heads, const fp_kv_view& kv,
+                                  const int32_t* cu, const int32_t* pos, const uint32_t* mask, int mask_stride, int max_new,
+                                  int max_len, uint16_t* out, void* ws, int32_t* err, cudaStream_t s);
+cudaError_t launch_verify_tree(const float* p, int V, int n_tokens, int B, const int32_t* cu, const int32_t* parent,
+                               const int32_t* tokens, const float* u, int32_t* path, int32_t* out, int32_t* n_out,
+                               int32_t* err, cudaStream_t s);
+cudaError_t launch_kv_commit(const fp_kv_view& kv, int n_tokens, int B, const int32_t* cu, const int32_t* pos,
+                             const int32_t* path, int32_t* err, cudaStream_t s);
+
+// ---- beams (fp_beam.cu)
+size_t beam_select_ws_bytes(int B, int W, int V);
+cudaError_t launch_beam_select(const float* logits, int V, int B, int W, const float* score, const int32_t* done, int end,
+                               int32_t* parent, int32_t* token, float* new_score, int32_t* new_done, void* ws, int32_t* err,
+                               cudaStream_t s);
+cudaError_t launch_beam_reorder(int B, int W, int pps, int page_size, const int32_t* len, const int32_t* parent,
+                                const int32_t* in, int32_t* out, int32_t* from, int32_t* to, int32_t* rows, int32_t* err,
+                                cudaStream_t s);
+cudaError_t launch_kv_copy(const fp_kv_view& kv, int n, const int32_t* from, const int32_t* to, const int32_t* rows,
+                           int32_t* err, cudaStream_t s);
 
 // ---- probabilities and draft verification (fp_verify.cu)
 cudaError_t launch_softmax(const float* logits, int M, int V, const float* temp, float* probs, int32_t* err,
