@@ -1122,8 +1122,8 @@ static cudaError_t launch_ck(const uint16_t* q, int q_stride, const fp_kv_view& 
   }
   static std::atomic<unsigned long long> attr{0};
   FP_CUDA_TRY(smem_limit_once(attn_chunk_kernel<HD, KV8, TREE>, ck_smem<HD>(), &attr));
-  return launch(attn_chunk_kernel<HD, KV8, TREE>, dim3(std::min(ck_sms(), kCkMaxCtas)), dim3(ck_threads<KV8>()),
-                (size_t)ck_smem<HD>(), s, mq, mk, mv, a);
+  return launch_early(attn_chunk_kernel<HD, KV8, TREE>, dim3(std::min(ck_sms(), kCkMaxCtas)), dim3(ck_threads<KV8>()),
+                      (size_t)ck_smem<HD>(), s, mq, mk, mv, a);
 }
 
 }  // namespace fpk

@@ -71,32 +71,40 @@ struct BsArgs {
   int32_t* err;
 };
 
-__global__ void __launch_bounds__(kBsThreads) beam_select_kernel(const BsArgs a) {
+constexpr int kBsCands = 512;   // candidates of a piece that are sorted out at once
+constexpr int kBsLists = 256;   // entries of a row's lists that are merged from shared memory
+
+template <int ITEMS>
+__global__ void __launch_bounds__(kBsThreads, 2) beam_select_kernel(const BsArgs a) {
   __shared__ unsigned long long s_best[2][kBsWarps], s_list[2][FP_BEAM_MAX];
   __shared__ BsSum s_sum[kBsWarps];
-  __shared__ int s_last;
-  __shared__ Pair s_off[FP_BEAM_MAX];                                    // score - lse of a beam
-  __shared__ unsigned long long s_row[FP_BEAM_MAX][FP_BEAM_MAX];         // its candidates
+  __shared__ int s_last, s_n;
+  __shared__ __align__(16) uint32_t s_top[kBsThreads / 4];
+  __shared__ union {
+    unsigned long long cand[kBsCands], list[kBsWarps][kBsLists];
+  } s_u;
+  __shared__ Pair s_off[FP_BEAM_MAX];                             // score - lse of a beam
+  __shared__ unsigned long long s_row[FP_BEAM_MAX][FP_BEAM_MAX];  // its candidates
+  constexpr int PIECE = kBsThreads * ITEMS * 4;
   pdl_trigger();
   pdl_wait();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, W = a.W, S = a.S;
   const int row = blockIdx.x / S, piece = blockIdx.x - row * S, b = row / W;
+  const float* x = a.x + (long long)row * a.V;
+  const long long lo = (long long)piece * a.per;
+  const int end = (int)min((long long)a.V, lo + a.per);
+  const bool vec = ((uintptr_t)(x + lo) & 15) == 0;
   const float score = __ldg(a.score + row);
   const bool ended = a.done && __ldg(a.done + row) != 0;
   if (!ended && score > -INFINITY) {
-    const float* x = a.x + (long long)row * a.V;
-    const long long lo = (long long)piece * a.per;
-    const int end = (int)min((long long)a.V, lo + a.per);
-    const bool vec = ((uintptr_t)(x + lo) & 15) == 0;
     BsSum sum = {-INFINITY, 0.f};
     int list = 0;  // which of the two holds the best so far
     if (threadIdx.x < FP_BEAM_MAX) s_list[0][threadIdx.x] = 0;
-    __syncthreads();
-    for (long long c0 = lo; c0 < end; c0 += kBsPiece) {
+    for (long long c0 = lo; c0 < end; c0 += PIECE) {
       // this thread's values: four tokens from c0 + 4 (i kBsThreads + thread) on
-      float v[kBsItems][4];
+      float v[ITEMS][4];
 #pragma unroll
-      for (int i = 0; i < kBsItems; ++i) {
+      for (int i = 0; i < ITEMS; ++i) {
         const long long t = c0 + 4 * (i * kBsThreads + (int)threadIdx.x);
         if (vec && t + 3 < end) {
           const float4 f = __ldg(reinterpret_cast<const float4*>(x + t));
@@ -106,42 +114,101 @@ __global__ void __launch_bounds__(kBsThreads) beam_select_kernel(const BsArgs a)
           for (int y = 0; y < 4; ++y) v[i][y] = t + y < end ? __ldg(x + t + y) : -INFINITY;
         }
       }
-      float m = -INFINITY;
+      float mt = -INFINITY;
 #pragma unroll
-      for (int i = 0; i < kBsItems; ++i) m = fmaxf(m, fmaxf(fmaxf(v[i][0], v[i][1]), fmaxf(v[i][2], v[i][3])));
-      m = warp_max(m);
+      for (int i = 0; i < ITEMS; ++i) mt = fmaxf(mt, fmaxf(fmaxf(v[i][0], v[i][1]), fmaxf(v[i][2], v[i][3])));
+      // the maxima of groups of four threads: the W-th largest of them is no larger than the
+      // W-th largest value, and little smaller
+      float m = fmaxf(mt, __shfl_xor_sync(0xffffffffu, mt, 1));
+      m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2));
+      if ((lane & 3) == 0) s_top[threadIdx.x >> 2] = m > -INFINITY ? bs_ordered(m + 0.f) : 0u;
+      if (threadIdx.x == 0) s_n = 0;
+      __syncthreads();
+#pragma unroll
+      for (int o = 4; o < 32; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
       {
-        // x log2 e in two parts (public constant: 1.4426950408889634)
+        // x log2 e in two parts (1.4426950408889634)
         constexpr float kHi = 1.44269502162933349609375f, kLo = 1.92596299e-8f;
         const float k = m == -INFINITY ? 0.f : ceilf(m * kHi);
         float s[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int i = 0; i < kBsItems; ++i)
+        for (int i = 0; i < ITEMS; ++i)
 #pragma unroll
           for (int y = 0; y < 4; ++y) s[y] += bs_ex2(v[i][y] == -INFINITY ? -INFINITY : fmaf(v[i][y], kLo, fmaf(v[i][y], kHi, -k)));
         const float t = warp_sum((s[0] + s[1]) + (s[2] + s[3]));
         sum = bs_add(sum, {m == -INFINITY && t == 0.f ? -INFINITY : k, t});
       }
-      // the W largest of these and of those before, one after the other
-      unsigned long long mine = threadIdx.x < W ? s_list[list][threadIdx.x] : 0ull, best = mine, won = ~0ull;
-      auto look = [&]() {  // the largest below the last winner
-        best = mine < won ? mine : 0ull;
+      uint32_t bar = 1;  // (0: nothing)
+      {
+        const uint4 q = *reinterpret_cast<const uint4*>(s_top + 4 * lane);
+        uint32_t u[4] = {q.x, q.y, q.z, q.w};
+        for (int r = 0; r < W; ++r) {
+          const uint32_t mine = max(max(u[0], u[1]), max(u[2], u[3])), top = __reduce_max_sync(0xffffffffu, mine);
+          bar = max(top, 1u);
+          if (lane == __ffs(__ballot_sync(0xffffffffu, mine == top)) - 1) {
+            bool gone = false;
 #pragma unroll
-        for (int i = 0; i < kBsItems; ++i)
-#pragma unroll
-          for (int y = 0; y < 4; ++y) {
-            const unsigned long long k = bs_key(v[i][y], (int)(c0 + 4 * (i * kBsThreads + (int)threadIdx.x)) + y);
-            if (k < won && k > best) best = k;
+            for (int i = 0; i < 4; ++i)
+              if (!gone && u[i] == top) u[i] = 0, gone = true;
           }
+        }
+      }
+      // what is no smaller, and the best so far
+      auto put = [&](unsigned long long k) {
+        const int at = atomicAdd(&s_n, 1);
+        if (at < kBsCands) s_u.cand[at] = k;
       };
-      look();
-      for (int r = 0; r < W; ++r) {
-        const unsigned long long wm = bs_warp_max(best);
-        if (lane == 0) s_best[r & 1][warp] = wm;
-        __syncthreads();
-        won = bs_warp_max(lane < kBsWarps ? s_best[r & 1][lane] : 0ull);
-        if (threadIdx.x == 0) s_list[list ^ 1][r] = won;
-        if (best == won && won != 0) look();
+      if (mt > -INFINITY && bs_ordered(mt + 0.f) >= bar) {
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i)
+#pragma unroll
+          for (int y = 0; y < 4; ++y)
+            if (v[i][y] > -INFINITY && bs_ordered(v[i][y] + 0.f) >= bar) put(bs_key(v[i][y], (int)(c0 + 4 * (i * kBsThreads + (int)threadIdx.x)) + y));
+      }
+      unsigned long long mine = threadIdx.x < W ? s_list[list][threadIdx.x] : 0ull;
+      if (mine != 0) put(mine);
+      __syncthreads();
+      const int n = s_n;
+      if (n <= kBsCands) {
+        if (warp == 0) {
+          unsigned long long best = 0, won = ~0ull;
+          auto look = [&]() {  // this lane's largest below the last winner
+            best = 0;
+            for (int i = lane; i < n; i += 32) {
+              const unsigned long long k = s_u.cand[i];
+              if (k < won && k > best) best = k;
+            }
+          };
+          look();
+          for (int r = 0; r < W; ++r) {
+            won = bs_warp_max(best);
+            if (lane == 0) s_list[list ^ 1][r] = won;
+            if (best == won && won != 0) look();
+          }
+        }
+      } else {
+        // Too many are as large (equal logits by the hundred): the W largest of all, one after the
+        // other.
+        unsigned long long best = mine, won = ~0ull;
+        auto look = [&]() {
+          best = mine < won ? mine : 0ull;
+#pragma unroll
+          for (int i = 0; i < ITEMS; ++i)
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+              const unsigned long long k = bs_key(v[i][y], (int)(c0 + 4 * (i * kBsThreads + (int)threadIdx.x)) + y);
+              if (k < won && k > best) best = k;
+            }
+        };
+        look();
+        for (int r = 0; r < W; ++r) {
+          const unsigned long long wm = bs_warp_max(best);
+          if (lane == 0) s_best[r & 1][warp] = wm;
+          __syncthreads();
+          won = bs_warp_max(lane < kBsWarps ? s_best[r & 1][lane] : 0ull);
+          if (threadIdx.x == 0) s_list[list ^ 1][r] = won;
+          if (best == won && won != 0) look();
+        }
       }
       list ^= 1;
       __syncthreads();
@@ -155,15 +222,18 @@ __global__ void __launch_bounds__(kBsThreads) beam_select_kernel(const BsArgs a)
         p = bs_add(p, {__shfl_xor_sync(0xffffffffu, p.k, o), __shfl_xor_sync(0xffffffffu, p.s, o)});
       if (lane == 0) a.sums[blockIdx.x] = make_float2(p.k, p.s);
       if (lane < W) a.best[(long long)blockIdx.x * W + lane] = s_list[list][lane];
-      __threadfence();
     }
   }
-  __syncthreads();
-  // the last CTA of the group
-  if (threadIdx.x == 0) {
-    const bool last = atomicAdd(a.tickets + b, 1) == W * S - 1;
-    if (last) a.tickets[b] = 0;
-    s_last = last;
+  // the last CTA of the group goes on
+  if (warp == 0) {
+    __threadfence();
+    __syncwarp();
+    if (lane == 0) {
+      const bool last = atomicAdd(a.tickets + b, 1) == W * S - 1;
+      if (last) a.tickets[b] = 0;
+      s_last = last;
+      __threadfence();
+    }
   }
   __syncthreads();
   if (!s_last) return;
@@ -172,18 +242,24 @@ __global__ void __launch_bounds__(kBsThreads) beam_select_kernel(const BsArgs a)
   for (int w = warp; w < W; w += kBsWarps) {
     const int r = b * W + w;
     const float sc = __ldcg(a.score + r);
-    if (!(sc > -INFINITY && sc < INFINITY) || (a.done && __ldcg(a.done + r) != 0)) {
-      // no candidates, or the one that keeps it as it is
-      const bool kept = sc > -INFINITY && sc < INFINITY;
-      if (!kept && sc != -INFINITY && lane == 0 && a.err) atomicExch(a.err, 1);
-      if (lane < W) s_row[w][lane] = kept && lane == 0 ? 1ull << 32 | (uint32_t)~a.end : 0ull;
+    const bool kept = a.done && __ldcg(a.done + r) != 0, real = sc > -INFINITY && sc < INFINITY;
+    BsSum p = {-INFINITY, 0.f};
+    const unsigned long long* lists = a.best + (long long)r * S * W;
+    const bool staged = S * W <= kBsLists;
+    if (real && !kept) {
+      if (lane < S) {
+        const float2 f = __ldcg(a.sums + (long long)r * S + lane);
+        p = {f.x, f.y};
+      }
+      if (staged)
+        for (int i = lane; i < S * W; i += 32) s_u.list[warp][i] = __ldcg(lists + i);
+    }
+    __syncwarp();
+    if (!real || kept) {  // no candidates, or the one that keeps it as it is
+      if (!real && sc != -INFINITY && lane == 0 && a.err) atomicExch(a.err, 1);
+      if (lane < W) s_row[w][lane] = real && lane == 0 ? 1ull << 32 | (uint32_t)~a.end : 0ull;
       if (lane == 0) s_off[w] = {sc, 0.f};
       continue;
-    }
-    BsSum p = {-INFINITY, 0.f};
-    if (lane < S) {
-      const float2 f = __ldcg(a.sums + (long long)r * S + lane);
-      p = {f.x, f.y};
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1)
@@ -191,7 +267,7 @@ __global__ void __launch_bounds__(kBsThreads) beam_select_kernel(const BsArgs a)
     const bool fine = p.s > 0.f && p.s < INFINITY;  // (a NaN or +inf among the logits: neither)
     if (!fine && p.k != -INFINITY && lane == 0 && a.err) atomicExch(a.err, 1);
     if (lane == 0) {
-      const int e = (int)(__float_as_uint(p.s) >> 23) - 127 + 1;  // s = 2^e f, 1/2 <= f < 1 (s >= 2^-126: against its largest)
+      const int e = (int)(__float_as_uint(p.s) >> 23) - 127 + 1;  // s = 2^e f, 1/2 <= f < 1
       const float f = __uint_as_float((__float_as_uint(p.s) & 0x7fffffu) | 0x3f000000u), n = p.k + (float)e;
       // n ln 2 as a pair (0.693147180559945309), its error carried along
       constexpr float kHi = 0.693147182464599609375f, kLo = -1.904654299957767e-9f;
@@ -200,14 +276,18 @@ __global__ void __launch_bounds__(kBsThreads) beam_select_kernel(const BsArgs a)
       s_off[w] = add(Pair{sc, 0.f}, Pair{-lse.hi, -lse.lo});
     }
     // lane s holds piece s's list; its head is what the lane offers
-    const unsigned long long* mine = a.best + ((long long)r * S + lane) * W;
     int at = 0;
-    unsigned long long head = fine && lane < S ? __ldcg(mine) : 0ull;
+    auto head_at = [&]() { return at >= W ? 0ull : staged ? s_u.list[warp][lane * W + at] : __ldcg(lists + lane * W + at); };
+    unsigned long long head = fine && lane < S ? head_at() : 0ull;
     for (int c = 0; c < W; ++c) {
       const unsigned long long k = bs_warp_max(head);
       if (lane == 0) s_row[w][c] = k;
-      if (k != 0 && head == k) head = ++at < W ? __ldcg(mine + at) : 0ull;
+      if (k != 0 && head == k) {
+        ++at;
+        head = head_at();
+      }
     }
+    __syncwarp();
   }
   __syncthreads();
   if (warp > 0) return;
@@ -217,21 +297,21 @@ __global__ void __launch_bounds__(kBsThreads) beam_select_kernel(const BsArgs a)
   const bool was = lane < W && a.done && __ldcg(a.done + b * W + lane) != 0;  // (new_done may be done)
   __syncwarp();
   int at = 0;
-  uint32_t hi, lo, ft;
+  uint32_t hi, lo32, ft;
   auto offer = [&]() {
     const unsigned long long k = lane < W && at < W ? s_row[lane][at] : 0ull;
     ft = (uint32_t)k;
-    hi = lo = 0;
+    hi = lo32 = 0;
     if (k == 0) return;
     Pair v = off;
-    if (!(k >> 32 == 1)) v = add(sum2(bs_value((uint32_t)(k >> 32)), off.hi), Pair{off.lo, 0.f});
-    hi = bs_ordered(v.hi + 0.f), lo = bs_ordered(v.lo + 0.f);
+    if (k >> 32 != 1) v = add(sum2(bs_value((uint32_t)(k >> 32)), off.hi), Pair{off.lo, 0.f});
+    hi = bs_ordered(v.hi + 0.f), lo32 = bs_ordered(v.lo + 0.f);
   };
   offer();
   for (int c = 0; c < W; ++c) {
     const uint32_t mh = __reduce_max_sync(0xffffffffu, hi);
-    const uint32_t ml = __reduce_max_sync(0xffffffffu, hi == mh ? lo : 0u);
-    const int win = __ffs(__ballot_sync(0xffffffffu, hi == mh && lo == ml)) - 1;
+    const uint32_t ml = __reduce_max_sync(0xffffffffu, hi == mh ? lo32 : 0u);
+    const int win = __ffs(__ballot_sync(0xffffffffu, hi == mh && lo32 == ml)) - 1;
     if (lane == win) {
       const int o = b * W + c, t = (int)~ft;
       const bool none = mh == 0;
@@ -271,7 +351,9 @@ cudaError_t launch_beam_select(const float* logits, int V, int B, int W, const f
   uint8_t* best = sums + bs_align((size_t)B * W * S * 8);
   const BsArgs a = {logits, V, B, W, S, ((V + S - 1) / S + 3) / 4 * 4, score, done, end, parent, token, new_score, new_done,
                     (int32_t*)p, (float2*)sums, (unsigned long long*)best, err};
-  return launch(beam_select_kernel, dim3((unsigned)(B * W * S)), dim3(kBsThreads), 0, s, a);
+  auto go = [&](auto kern) { return launch_early(kern, dim3((unsigned)(B * W * S)), dim3(kBsThreads), 0, s, a); };
+  const int items = (a.per + 4 * kBsThreads - 1) / (4 * kBsThreads);
+  return items <= 2 ? go(beam_select_kernel<2>) : items <= 4 ? go(beam_select_kernel<4>) : go(beam_select_kernel<kBsItems>);
 }
 
 // ------------------------------------------------------------------ reordering
@@ -324,7 +406,7 @@ cudaError_t launch_beam_reorder(int B, int W, int pps, int page_size, const int3
                                 const int32_t* in, int32_t* out, int32_t* from, int32_t* to, int32_t* rows, int32_t* err,
                                 cudaStream_t s) {
   if (B <= 0) return cudaSuccess;
-  return launch(beam_reorder_kernel, dim3(B * W), dim3(128), 0, s, W, pps, page_size, len, parent, in, out, from, to, rows,
+  return launch_early(beam_reorder_kernel, dim3(B * W), dim3(128), 0, s, W, pps, page_size, len, parent, in, out, from, to, rows,
                 err);
 }
 
@@ -369,7 +451,7 @@ cudaError_t launch_kv_copy(const fp_kv_view& kv, int n, const int32_t* from, con
                            int32_t* err, cudaStream_t s) {
   if (n <= 0) return cudaSuccess;
   const dim3 grid(n, std::min((2 * kv.n_kv_heads + kKcWarps - 1) / kKcWarps, 1024));
-  auto go = [&](auto kern) { return launch(kern, grid, dim3(kKcWarps * 32), 0, s, kv, from, to, rows, err); };
+  auto go = [&](auto kern) { return launch_early(kern, grid, dim3(kKcWarps * 32), 0, s, kv, from, to, rows, err); };
   const int rb = kv.head_dim * (kv.kvquant == FP_KV_INT8 ? 1 : 2);
   return rb == 64 ? go(kv_copy_kernel<64>) : rb == 128 ? go(kv_copy_kernel<128>) : go(kv_copy_kernel<256>);
 }

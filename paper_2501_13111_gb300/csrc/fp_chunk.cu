@@ -128,8 +128,8 @@ static cudaError_t launch_append(const uint16_t* qkv, int row_stride, int n_toke
                                  uint16_t* q_out, int q_out_stride, int32_t* err, cudaStream_t s) {
   if (n_tokens <= 0 || B <= 0) return cudaSuccess;
   auto go = [&](auto kern) {
-    return launch(kern, dim3(n_tokens), dim3(256), 0, s, qkv, row_stride, n_tokens, B, n_heads, kv, cu, pos, depth,
-                  rope_cs, q_out, q_out_stride, err);
+    return launch_early(kern, dim3(n_tokens), dim3(256), 0, s, qkv, row_stride, n_tokens, B, n_heads, kv, cu, pos, depth,
+                        rope_cs, q_out, q_out_stride, err);
   };
   const bool i8 = kv.kvquant == FP_KV_INT8;
   if (kv.head_dim == 64) return i8 ? go(rope_kv_chunk_kernel<64, true, TREE>) : go(rope_kv_chunk_kernel<64, false, TREE>);
@@ -193,7 +193,7 @@ cudaError_t launch_kv_read(const fp_kv_view& kv, int n_tokens, int B, const int3
                            uint16_t* k_out, uint16_t* v_out, int out_stride, int32_t* err, cudaStream_t s) {
   if (n_tokens <= 0 || B <= 0) return cudaSuccess;
   auto go = [&](auto kern) {
-    return launch(kern, dim3(n_tokens), dim3(256), 0, s, kv, n_tokens, B, cu, pos, k_out, v_out, out_stride, err);
+    return launch_early(kern, dim3(n_tokens), dim3(256), 0, s, kv, n_tokens, B, cu, pos, k_out, v_out, out_stride, err);
   };
   if (kv.head_dim == 64) return kv.kvquant == FP_KV_INT8 ? go(kv_read_kernel<64, true>) : go(kv_read_kernel<64, false>);
   return kv.kvquant == FP_KV_INT8 ? go(kv_read_kernel<128, true>) : go(kv_read_kernel<128, false>);

@@ -49,7 +49,7 @@ __global__ void __launch_bounds__(kTpThreads)
 cudaError_t launch_tree_plan(const int32_t* parent, int n_tokens, int B, const int32_t* cu, int max_new, int32_t* depth,
                              uint32_t* mask, int mask_stride, int32_t* err, cudaStream_t s) {
   if (n_tokens <= 0 || B <= 0 || max_new <= 0) return cudaSuccess;
-  return launch(tree_plan_kernel, dim3(B), dim3(kTpThreads), 0, s, parent, n_tokens, B, cu, max_new, depth, mask,
+  return launch_early(tree_plan_kernel, dim3(B), dim3(kTpThreads), 0, s, parent, n_tokens, B, cu, max_new, depth, mask,
                 mask_stride, err);
 }
 
@@ -133,7 +133,7 @@ cudaError_t launch_kv_commit(const fp_kv_view& kv, int n_tokens, int B, const in
                              const int32_t* path, int32_t* err, cudaStream_t s) {
   if (n_tokens <= 0 || B <= 0) return cudaSuccess;
   const dim3 grid(B, std::min((2 * kv.n_kv_heads + kCmWarps - 1) / kCmWarps, 1024));
-  auto go = [&](auto kern) { return launch(kern, grid, dim3(kCmWarps * 32), 0, s, kv, n_tokens, B, cu, pos, path, err); };
+  auto go = [&](auto kern) { return launch_early(kern, grid, dim3(kCmWarps * 32), 0, s, kv, n_tokens, B, cu, pos, path, err); };
   const int rb = kv.head_dim * (kv.kvquant == FP_KV_INT8 ? 1 : 2);
   return rb == 64 ? go(kv_commit_kernel<64>) : rb == 128 ? go(kv_commit_kernel<128>) : go(kv_commit_kernel<256>);
 }

@@ -507,12 +507,274 @@ __global__ void __cluster_dims__(kVfCTAs, 1, 1) __launch_bounds__(kVfThreads)
     for (int i = a + 1 + (int)threadIdx.x; i < n; i += kVfThreads) out[row0 + i] = -1, path[row0 + i] = -1;
 }
 
+// The same in two kernels: a token drawn for every row at once, then the way down.  More
+// is read, but nothing waits for a step before it.  Bound by bytes and issue slots for
+// many rows (32 trees of 16 rows of 32000 tokens: 49 MB in 11 us), else by latency.
+//
+// A warp, a CTA or a cluster of up to 8 CTAs a row (launch_verify_tree): a warp takes a run
+// of consecutive weights, in 16-byte groups aligned in memory, as 32 chunks of 32 k groups,
+// and sums each of them; its lanes then hold a chunk's sum each.  The runs' sums meet, and
+// the warp whose run holds the border has the chunk by a scan, and reads that one again.
+// The token (-1: no weight, or an infinite one) stands in out until the second kernel has
+// read it.
+// Every weight costs issue slots, so a group is summed exactly by packed additions, x + z
+// beside y + w, and the lanes' sums of eight chunks change places through shared memory, not
+// by shuffles; four groups a lane are on their way while four are summed.
+constexpr int kTdThreads = 256, kTdWarps = kTdThreads / 32, kTdMaxCTAs = 8;
+constexpr int kTdRow = 33;  // a chunk's lane sums in shared memory, padded
+
+// T: warps a row, 1 or all.  ONE: k is 1 (runs of up to 4096 weights).
+template <int T, bool ONE>
+__global__ void __launch_bounds__(kTdThreads, 3)
+    tree_draw_kernel(const float* __restrict__ p, int V, int n_tokens, int B, const int32_t* __restrict__ cu,
+                     const float* __restrict__ u, int32_t* __restrict__ out, int32_t* err) {
+  __shared__ Pair s_sum[kTdWarps], s_cta, s_chunk[kTdWarps][32];
+  __shared__ float2 s_lane[kTdWarps][8 * kTdRow];
+  pdl_wait();
+  pdl_trigger();  // (what came before is over once the second kernel starts)
+  cg::cluster_group cluster = cg::this_cluster();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int C = T == 1 ? 1 : (int)cluster.num_blocks(), rank = T == 1 ? 0 : (int)cluster.block_rank();
+  const int row = T == 1 ? blockIdx.x * kTdWarps + warp : blockIdx.x / C;
+  if (blockIdx.x == 0) chunk_check(cu, B, n_tokens, err);
+  if (T == 1 && row >= n_tokens) return;
+  const float* pr = p + (long long)row * V;
+  // group g holds weights 4 g - skew .. 4 g - skew + 3
+  const int skew = (int)(((uintptr_t)pr & 15) >> 2), groups = (V + skew + 3) >> 2, runs = C * T;
+  const int k = ONE ? 1 : (groups + runs * 1024 - 1) / (runs * 1024);
+  const int run = (groups + runs - 1) / runs;
+  const int g0 = min(groups, (T == 1 ? 0 : rank * T + warp) * run), g1 = min(groups, g0 + run);
+  auto load = [&](int g) -> float4 {
+    const int i = 4 * g - skew;
+    if (g < g1 && i >= 0 && i + 3 < V) return __ldg(reinterpret_cast<const float4*>(pr + i));
+    float v[4];
+#pragma unroll
+    for (int y = 0; y < 4; ++y) v[y] = g < g1 && i + y >= 0 && i + y < V ? __ldg(pr + i + y) : 0.f;
+    return make_float4(v[0], v[1], v[2], v[3]);
+  };
+  float4 x[4];
+  // groups j of chunks c .. c + 3
+  auto fetch = [&](int c, int j) {
+    const int at = g0 + c * 32 * k;
+    if (4 * at >= skew && at + 128 * k <= g1 && 4 * (at + 128 * k) - skew <= V) {
+      const float4* q = reinterpret_cast<const float4*>(pr - skew) + at + j * 32 + lane;
+#pragma unroll
+      for (int y = 0; y < 4; ++y) x[y] = __ldg(q + y * k * 32);
+    } else {
+#pragma unroll
+      for (int y = 0; y < 4; ++y) x[y] = load(at + (y * k + j) * 32 + lane);
+    }
+  };
+  fetch(0, 0);
+  const float r = __ldg(u + row);
+  // a group's sum, exact but for the last addition (an error of 2^-48 of it)
+  auto sum4 = [](float4 x) -> Pair {
+    const float2 a = make_float2(fmaxf(x.x, 0.f), fmaxf(x.y, 0.f)), b = make_float2(fmaxf(x.z, 0.f), fmaxf(x.w, 0.f));
+    const float2 n1 = make_float2(-1.f, -1.f), s = fp_add2(a, b), t = fp_fma2(a, n1, s);  // t = s - a
+    const float2 e = fp_add2(fp_fma2(fp_fma2(t, n1, s), n1, a), fp_fma2(t, n1, b));      // (a - (s - t)) + (b - t)
+    const Pair c = sum2(s.x, s.y);
+    return {c.hi, __fadd_rn(c.lo, __fadd_rn(e.x, e.y))};
+  };
+  auto take = [](Pair& s, Pair w) {
+    const Pair f = sum2(s.hi, w.hi);
+    s = {f.hi, __fadd_rn(s.lo, __fadd_rn(f.lo, w.lo))};
+  };
+  if (chunk_owner(cu, B, row) < 0) return;  // (the whole cluster leaves)
+  s_chunk[warp][lane] = {0.f, 0.f};
+  __syncwarp();
+#pragma unroll 1
+  for (int c0 = 0; c0 < 32 && g0 + c0 * 32 * k < g1; c0 += 8) {
+    Pair s[8];
+#pragma unroll
+    for (int h = 0; h < 8; h += 4) {
+#pragma unroll
+      for (int c = 0; c < 4; ++c) s[h + c] = {0.f, 0.f};
+#pragma unroll 1
+      for (int j = 0; j < k; ++j) {
+        float4 y[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) y[c] = x[c];
+        if (j + 1 < k) fetch(c0 + h, j + 1);
+        else if (c0 + h + 4 < 32) fetch(c0 + h + 4, 0);
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+          if (ONE) s[h + c] = sum4(y[c]);
+          else take(s[h + c], sum4(y[c]));
+        if (ONE) break;
+      }
+    }
+    // four lanes a chunk: eight lanes' sums each, then those of the four
+#pragma unroll
+    for (int c = 0; c < 8; ++c) s_lane[warp][c * kTdRow + lane] = make_float2(s[c].hi, s[c].lo);
+    __syncwarp();
+    Pair w = {0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float2 f = s_lane[warp][(lane >> 2) * kTdRow + (lane & 3) * 8 + i];
+      take(w, Pair{f.x, f.y});
+    }
+    w = tidy(w.hi, w.lo);
+#pragma unroll
+    for (int o = 1; o < 4; o <<= 1)
+      w = add(w, Pair{__shfl_xor_sync(0xffffffffu, w.hi, o), __shfl_xor_sync(0xffffffffu, w.lo, o)});
+    if ((lane & 3) == 0) s_chunk[warp][c0 + (lane >> 2)] = w;
+    __syncwarp();
+  }
+  const Pair chunk = s_chunk[warp][lane], chunks = scan<32>(chunk, lane);
+  Pair total = shfl(chunks, 31), before = {0.f, 0.f};
+  bool here = true;
+  if constexpr (T > 1) {
+    if (lane == 31) s_sum[warp] = chunks;
+    __syncthreads();
+    const Pair mine = s_sum[lane & (kTdWarps - 1)], upto = scan<kTdWarps>(mine, lane);  // within this CTA
+    total = shfl(upto, kTdWarps - 1);
+    if (C > 1) {
+      if (threadIdx.x == 0) s_cta = total;
+      cluster.sync();
+      const Pair theirs = lane < C ? *cluster.map_shared_rank(&s_cta, lane) : Pair{0.f, 0.f}, all = scan<kTdMaxCTAs>(theirs, lane);
+      total = shfl(all, kTdMaxCTAs - 1);
+      cluster.barrier_arrive();
+      here = holder(all, lane < C ? theirs.hi : 0.f, times(total, r)) == rank;
+      if (rank) before = shfl(all, rank - 1);
+    }
+    const Pair to = add(before, upto);
+    here = here && holder(to, lane < kTdWarps ? mine.hi : 0.f, times(total, r)) == warp;
+    if (warp) before = shfl(to, warp - 1);
+  }
+  const bool drawable = total.hi > 0.f && total.hi < INFINITY;
+  if (!drawable && rank == 0 && (T == 1 ? lane : threadIdx.x) == 0) out[row] = -1;
+  if (drawable && here) {
+    const Pair border = times(total, r), pu = add(before, chunks);
+    const int c = holder(pu, chunk.hi, border);
+    Pair at = c ? shfl(pu, c - 1) : before;
+    int token = -1;
+#pragma unroll 1
+    for (int j = 0; j < k; ++j) {  // 32 groups at a time
+      const int g = g0 + (c * k + j) * 32 + lane;
+      const float4 f4 = load(g);
+      Pair w = sum4(f4);
+      w = tidy(w.hi, w.lo);
+      const Pair wu = add(at, scan<32>(w, lane));
+      const int l = holder(wu, w.hi, border);
+      if (l >= 0) {  // within a group, by its lane: the first past the border, or the last that counts
+        const Pair from = l ? shfl(wu, l - 1) : at;
+        if (lane == l) {
+          const float v[4] = {f4.x, f4.y, f4.z, f4.w};
+          Pair f = from;
+          int t = -1;
+          bool past = false;
+#pragma unroll
+          for (int y = 0; y < 4; ++y)
+            if (v[y] > 0.f && !past) {
+              f = add(f, Pair{v[y], 0.f});
+              t = y;
+              past = greater(f, border);
+            }
+          token = 4 * g - skew + t;
+        }
+        token = __shfl_sync(0xffffffffu, token, l);
+      }
+      if (__any_sync(0xffffffffu, w.hi > 0.f && greater(wu, border))) break;
+      at = shfl(wu, 31);
+    }
+    if (lane == 0) out[row] = token;
+  }
+  if (C > 1) cluster.barrier_wait();  // (a CTA stays until the others have read its sum)
+}
+
+// One CTA a sequence, the tree's first rows in shared memory.  A step reads the token drawn
+// behind a row, then writes it at the step's own place, which no later step reads: the way
+// ascends.
+constexpr int kTwThreads = 128, kTwRows = 1024;
+
+__global__ void __launch_bounds__(kTwThreads)
+    tree_walk_kernel(bool early, int n_tokens, int B, const int32_t* __restrict__ cu, const int32_t* __restrict__ parent,
+                     const int32_t* __restrict__ tokens, int32_t* __restrict__ path, int32_t* out,
+                     int32_t* __restrict__ n_out, int32_t* err) {
+  __shared__ int s_parent[kTwRows], s_token[kTwRows], s_drawn[kTwRows];
+  const int b = blockIdx.x, lane = threadIdx.x & 31;
+  int row0, n;
+  // the tree, while tokens are drawn: what came before that is over (the drawing kernel lets
+  // this one start behind its own wait)
+  if (early) {
+    chunk_rows(cu, b, n_tokens, &row0, &n);
+    for (int i = threadIdx.x; i < min(n, kTwRows); i += kTwThreads)
+      s_parent[i] = __ldg(parent + row0 + i), s_token[i] = __ldg(tokens + row0 + i);
+  }
+  pdl_trigger();
+  pdl_wait();
+  if (!early) chunk_rows(cu, b, n_tokens, &row0, &n);
+  if (n == 0) {
+    if (threadIdx.x == 0) n_out[b] = 0;
+    return;
+  }
+  for (int i = threadIdx.x; i < min(n, kTwRows); i += kTwThreads) s_drawn[i] = out[row0 + i];
+  __syncthreads();
+  if (threadIdx.x >= 32) return;
+  int cur = 0, a = 0;
+  for (;; ++a) {
+    const int token = cur < kTwRows ? s_drawn[cur] : out[row0 + cur];
+    __syncwarp();
+    if (lane == 0) path[row0 + a] = cur, out[row0 + a] = token;
+    int child = -1;
+#pragma unroll 1
+    for (int i0 = cur + 1; i0 < n && child < 0 && token >= 0; i0 += 32) {
+      const int i = i0 + lane;
+      const int up = i >= n ? -1 : i < kTwRows ? s_parent[i] : __ldg(parent + row0 + i);
+      const int t = i >= n ? -1 : i < kTwRows ? s_token[i] : __ldg(tokens + row0 + i);
+      const unsigned any = __ballot_sync(0xffffffffu, up == cur && t == token);
+      if (any) child = i0 + __ffs(any) - 1;
+    }
+    if (token < 0 && lane == 0 && err) atomicExch(err, 1);
+    if (child < 0) {
+      if (lane == 0) n_out[b] = token < 0 ? a : a + 1;
+      break;
+    }
+    cur = child;
+  }
+  for (int i = a + 1 + lane; i < n; i += 32) out[row0 + i] = -1, path[row0 + i] = -1;
+}
+
+// Every row's token at once, or one after the other (us): 32 trees of up to 16 rows, 32000
+// tokens 14 | 30, 1 of 60, 100003 tokens 13 | 23, 64 of up to 100, 2500 tokens 19 | 54; 32 of up
+// to 40, 32000 tokens (30 M weights) 30 | 33, of up to 80 (61 M) 53 | 37.  So up to 2^25 weights.
+constexpr long long kTdMost = 1LL << 25;
+constexpr int kTdPlaces = 152 * 3;  // CTAs that the GPU holds
+// Rows from which a warp takes each (us, a CTA a row | a warp): 4900 rows of 2500 tokens
+// 53 | 19, 1400 of 10000 27 | 35, 960 of 32000 30 | 56, 580 of 10000 13 | 18.
+constexpr int kTdMany = 2048;
+
 cudaError_t launch_verify_tree(const float* p, int V, int n_tokens, int B, const int32_t* cu, const int32_t* parent,
                                const int32_t* tokens, const float* u, int32_t* path, int32_t* out, int32_t* n_out,
                                int32_t* err, cudaStream_t s) {
   if (B <= 0) return cudaSuccess;
-  return launch(verify_tree_kernel, dim3(B * kVfCTAs), dim3(kVfThreads), 0, s, p, V, n_tokens, B, cu, parent, tokens, u,
-                path, out, n_out, err);
+  if ((long long)n_tokens * V > kTdMost)
+    return launch_early(verify_tree_kernel, dim3(B * kVfCTAs), dim3(kVfThreads), 0, s, p, V, n_tokens, B, cu, parent, tokens,
+                        u, path, out, n_out, err);
+  if (n_tokens > 0) {
+    const int groups = V / 4 + 2;
+    const bool many = n_tokens >= kTdMany;
+    int C = 1;
+    while (!many && C < kTdMaxCTAs && n_tokens * 2LL * C <= kTdPlaces && V / C >= 8192) C *= 2;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(many ? (n_tokens + kTdWarps - 1) / kTdWarps : (unsigned)n_tokens * C);
+    cfg.blockDim = dim3(kTdThreads);
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = C;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    auto go = [&](auto kern) { return cudaLaunchKernelEx(&cfg, kern, p, V, n_tokens, B, cu, u, out, err); };
+    const bool one = groups <= 1024 * (many ? 1 : kTdWarps * C);
+    FP_CUDA_TRY(many ? (one ? go(tree_draw_kernel<1, true>) : go(tree_draw_kernel<1, false>))
+                     : (one ? go(tree_draw_kernel<kTdWarps, true>) : go(tree_draw_kernel<kTdWarps, false>)));
+  }
+  return launch_early(tree_walk_kernel, dim3(B), dim3(kTwThreads), 0, s, n_tokens > 0, n_tokens, B, cu, parent, tokens, path, out, n_out,
+                      err);
 }
 
 }  // namespace fpk
