@@ -72,16 +72,31 @@ struct BsArgs {
 };
 
 constexpr int kBsCands = 512;   // candidates of a piece that are sorted out at once
-constexpr int kBsLists = 256;   // entries of a row's lists that are merged from shared memory
+constexpr int kBsLists = 128;   // entries of a row's lists: pieces times W, at most
+
+// W sorted lists, ordered by their heads: entry e of the list with the r-th largest head has
+// r + e larger ones, so the W largest of all are among the W (W + 1) / 2 with r + e < W.
+// The first of list r's among those:
+constexpr int kBsTriangle = FP_BEAM_MAX * (FP_BEAM_MAX + 1) / 2;
+FP_DEV int bs_first(int r, int W) { return r * W - r * (r - 1) / 2; }
 
 template <int ITEMS>
 __global__ void __launch_bounds__(kBsThreads, 2) beam_select_kernel(const BsArgs a) {
   __shared__ unsigned long long s_best[2][kBsWarps], s_list[2][FP_BEAM_MAX];
   __shared__ BsSum s_sum[kBsWarps];
   __shared__ int s_last, s_n;
-  __shared__ __align__(16) uint32_t s_top[kBsThreads / 4];
+  __shared__ uint32_t s_bar;
+  __shared__ __align__(16) uint32_t s_top[32];
+  __shared__ int s_done[FP_BEAM_MAX];
   __shared__ union {
-    unsigned long long cand[kBsCands], list[kBsWarps][kBsLists];
+    unsigned long long cand[kBsCands];
+    struct {
+      unsigned long long list[kBsLists], some[kBsLists];
+    } row[kBsWarps];
+    struct {
+      unsigned long long score[FP_BEAM_MAX][FP_BEAM_MAX], some[kBsTriangle];
+      int place[kBsTriangle];
+    } beam;
   } s_u;
   __shared__ Pair s_off[FP_BEAM_MAX];                             // score - lse of a beam
   __shared__ unsigned long long s_row[FP_BEAM_MAX][FP_BEAM_MAX];  // its candidates
@@ -117,42 +132,45 @@ __global__ void __launch_bounds__(kBsThreads, 2) beam_select_kernel(const BsArgs
       float mt = -INFINITY;
 #pragma unroll
       for (int i = 0; i < ITEMS; ++i) mt = fmaxf(mt, fmaxf(fmaxf(v[i][0], v[i][1]), fmaxf(v[i][2], v[i][3])));
-      // the maxima of groups of four threads: the W-th largest of them is no larger than the
+      // the maxima of 32 groups of threads: the W-th largest of them is no larger than the
       // W-th largest value, and little smaller
-      float m = fmaxf(mt, __shfl_xor_sync(0xffffffffu, mt, 1));
-      m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2));
-      if ((lane & 3) == 0) s_top[threadIdx.x >> 2] = m > -INFINITY ? bs_ordered(m + 0.f) : 0u;
+      float m = mt;
+#pragma unroll
+      for (int o = 1; o < 16; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+      if ((lane & 15) == 0) s_top[threadIdx.x >> 4] = m > -INFINITY ? bs_ordered(m + 0.f) : 0u;
       if (threadIdx.x == 0) s_n = 0;
       __syncthreads();
+      if (warp == 0) {  // (by one warp: all of them took the issue slots of the exponentials)
+        const uint32_t mine = s_top[lane];
+        int rank = 0;
 #pragma unroll
-      for (int o = 4; o < 32; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+        for (int i = 0; i < 32; i += 4) {
+          const uint4 q = *reinterpret_cast<const uint4*>(s_top + i);
+          const uint32_t u[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+          for (int y = 0; y < 4; ++y) rank += u[y] > mine || (u[y] == mine && i + y < lane);
+        }
+        if (rank == W - 1) s_bar = max(mine, 1u);  // (0: nothing)
+      }
+      m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
       {
         // x log2 e in two parts (1.4426950408889634)
         constexpr float kHi = 1.44269502162933349609375f, kLo = 1.92596299e-8f;
         const float k = m == -INFINITY ? 0.f : ceilf(m * kHi);
-        float s[4] = {0.f, 0.f, 0.f, 0.f};
+        const float2 hi2 = make_float2(kHi, kHi), lo2 = make_float2(kLo, kLo), k2 = make_float2(-k, -k);
+        float2 s[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i)
 #pragma unroll
-          for (int y = 0; y < 4; ++y) s[y] += bs_ex2(v[i][y] == -INFINITY ? -INFINITY : fmaf(v[i][y], kLo, fmaf(v[i][y], kHi, -k)));
-        const float t = warp_sum((s[0] + s[1]) + (s[2] + s[3]));
+          for (int y = 0; y < 4; y += 2) {
+            const float2 x2 = make_float2(v[i][y], v[i][y + 1]), e = fp_fma2(x2, lo2, fp_fma2(x2, hi2, k2));
+            s[y / 2] = fp_add2(s[y / 2], make_float2(bs_ex2(e.x), bs_ex2(e.y)));
+          }
+        const float t = warp_sum((s[0].x + s[0].y) + (s[1].x + s[1].y));
         sum = bs_add(sum, {m == -INFINITY && t == 0.f ? -INFINITY : k, t});
       }
-      uint32_t bar = 1;  // (0: nothing)
-      {
-        const uint4 q = *reinterpret_cast<const uint4*>(s_top + 4 * lane);
-        uint32_t u[4] = {q.x, q.y, q.z, q.w};
-        for (int r = 0; r < W; ++r) {
-          const uint32_t mine = max(max(u[0], u[1]), max(u[2], u[3])), top = __reduce_max_sync(0xffffffffu, mine);
-          bar = max(top, 1u);
-          if (lane == __ffs(__ballot_sync(0xffffffffu, mine == top)) - 1) {
-            bool gone = false;
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              if (!gone && u[i] == top) u[i] = 0, gone = true;
-          }
-        }
-      }
+      __syncthreads();
+      const uint32_t bar = s_bar;
       // what is no smaller, and the best so far
       auto put = [&](unsigned long long k) {
         const int at = atomicAdd(&s_n, 1);
@@ -170,21 +188,15 @@ __global__ void __launch_bounds__(kBsThreads, 2) beam_select_kernel(const BsArgs
       __syncthreads();
       const int n = s_n;
       if (n <= kBsCands) {
-        if (warp == 0) {
-          unsigned long long best = 0, won = ~0ull;
-          auto look = [&]() {  // this lane's largest below the last winner
-            best = 0;
-            for (int i = lane; i < n; i += 32) {
-              const unsigned long long k = s_u.cand[i];
-              if (k < won && k > best) best = k;
-            }
-          };
-          look();
-          for (int r = 0; r < W; ++r) {
-            won = bs_warp_max(best);
-            if (lane == 0) s_list[list ^ 1][r] = won;
-            if (best == won && won != 0) look();
-          }
+        // each one's place in the order is the number of larger ones
+        if (threadIdx.x < n) {
+          const unsigned long long k = s_u.cand[threadIdx.x];
+          int rank = 0;
+#pragma unroll 4
+          for (int i = 0; i < n; ++i) rank += s_u.cand[i] > k;
+          if (rank < W) s_list[list ^ 1][rank] = k;
+        } else if (threadIdx.x < W) {
+          s_list[list ^ 1][threadIdx.x] = 0;
         }
       } else {
         // Too many are as large (equal logits by the hundred): the W largest of all, one after the
@@ -243,22 +255,25 @@ __global__ void __launch_bounds__(kBsThreads, 2) beam_select_kernel(const BsArgs
     const int r = b * W + w;
     const float sc = __ldcg(a.score + r);
     const bool kept = a.done && __ldcg(a.done + r) != 0, real = sc > -INFINITY && sc < INFINITY;
+    // (all that is needed at once, of beams that left nothing too)
     BsSum p = {-INFINITY, 0.f};
-    const unsigned long long* lists = a.best + (long long)r * S * W;
-    const bool staged = S * W <= kBsLists;
-    if (real && !kept) {
-      if (lane < S) {
-        const float2 f = __ldcg(a.sums + (long long)r * S + lane);
-        p = {f.x, f.y};
-      }
-      if (staged)
-        for (int i = lane; i < S * W; i += 32) s_u.list[warp][i] = __ldcg(lists + i);
+    if (lane < S) {
+      const float2 f = __ldcg(a.sums + (long long)r * S + lane);
+      p = {f.x, f.y};
     }
+    const unsigned long long* lists = a.best + (long long)r * S * W;
+#pragma unroll
+    for (int i = 0; i < kBsLists; i += 32)
+      if (i + lane < S * W) s_u.row[warp].list[i + lane] = __ldcg(lists + i + lane);
+    if (lane == 0) s_done[w] = kept;
+    if (lane < W) s_row[w][lane] = 0;
     __syncwarp();
     if (!real || kept) {  // no candidates, or the one that keeps it as it is
       if (!real && sc != -INFINITY && lane == 0 && a.err) atomicExch(a.err, 1);
-      if (lane < W) s_row[w][lane] = real && lane == 0 ? 1ull << 32 | (uint32_t)~a.end : 0ull;
-      if (lane == 0) s_off[w] = {sc, 0.f};
+      if (lane == 0) {
+        if (real) s_row[w][0] = 1ull << 32 | (uint32_t)~a.end;
+        s_off[w] = {sc, 0.f};
+      }
       continue;
     }
 #pragma unroll
@@ -275,69 +290,110 @@ __global__ void __launch_bounds__(kBsThreads, 2) beam_select_kernel(const BsArgs
       const Pair lse = add(tidy(h, __fmaf_rn(n, kLo, __fmaf_rn(n, kHi, -h))), Pair{logf(f), 0.f});
       s_off[w] = add(Pair{sc, 0.f}, Pair{-lse.hi, -lse.lo});
     }
-    // lane s holds piece s's list; its head is what the lane offers
-    int at = 0;
-    auto head_at = [&]() { return at >= W ? 0ull : staged ? s_u.list[warp][lane * W + at] : __ldcg(lists + lane * W + at); };
-    unsigned long long head = fine && lane < S ? head_at() : 0ull;
-    for (int c = 0; c < W; ++c) {
-      const unsigned long long k = bs_warp_max(head);
-      if (lane == 0) s_row[w][c] = k;
-      if (k != 0 && head == k) {
-        ++at;
-        head = head_at();
+    // the pieces' lists, those that count side by side; each one's place is the number of
+    // larger ones
+    const unsigned long long* list = s_u.row[warp].list;
+    unsigned long long* some = s_u.row[warp].some;
+    const unsigned long long head = fine && lane < S ? list[lane * W] : 0ull;
+    const int alive = __popc(__ballot_sync(0xffffffffu, head != 0));
+    int r2 = 0;
+#pragma unroll 8
+    for (int i = 0; i < S; ++i) r2 += list[i * W] > head;
+    if (head != 0)
+      for (int i = 0; i < W - r2; ++i) some[bs_first(r2, W) + i] = list[lane * W + i];
+    __syncwarp();
+    const int n = bs_first(min(alive, W), W);
+    for (int i0 = 0; i0 < n; i0 += 64) {
+      const unsigned long long k = i0 + lane < n ? some[i0 + lane] : 0ull, k1 = i0 + 32 + lane < n ? some[i0 + 32 + lane] : 0ull;
+      int rank = 0, rank1 = 0;
+#pragma unroll 8
+      for (int i = 0; i < n; ++i) {
+        const unsigned long long u = some[i];
+        rank += u > k, rank1 += u > k1;
       }
+      if (k != 0 && rank < W) s_row[w][rank] = k;
+      if (k1 != 0 && rank1 < W) s_row[w][rank1] = k1;
     }
     __syncwarp();
   }
   __syncthreads();
-  if (warp > 0) return;
-  // the beams, lane w's list being beam w's: scores as pairs, ties to the lowest beam and,
-  // in a beam, the order of its list
-  const Pair off = lane < W ? s_off[lane] : Pair{0.f, 0.f};
-  const bool was = lane < W && a.done && __ldcg(a.done + b * W + lane) != 0;  // (new_done may be done)
-  __syncwarp();
-  int at = 0;
-  uint32_t hi, lo32, ft;
-  auto offer = [&]() {
-    const unsigned long long k = lane < W && at < W ? s_row[lane][at] : 0ull;
-    ft = (uint32_t)k;
-    hi = lo32 = 0;
-    if (k == 0) return;
-    Pair v = off;
-    if (k >> 32 != 1) v = add(sum2(bs_value((uint32_t)(k >> 32)), off.hi), Pair{off.lo, 0.f});
-    hi = bs_ordered(v.hi + 0.f), lo32 = bs_ordered(v.lo + 0.f);
-  };
-  offer();
-  for (int c = 0; c < W; ++c) {
-    const uint32_t mh = __reduce_max_sync(0xffffffffu, hi);
-    const uint32_t ml = __reduce_max_sync(0xffffffffu, hi == mh ? lo32 : 0u);
-    const int win = __ffs(__ballot_sync(0xffffffffu, hi == mh && lo32 == ml)) - 1;
-    if (lane == win) {
-      const int o = b * W + c, t = (int)~ft;
-      const bool none = mh == 0;
-      a.parent[o] = none ? -1 : win;
-      a.token[o] = none ? -1 : t;
-      a.new_score[o] = none ? -INFINITY : bs_value(mh);
-      if (a.new_done) a.new_done[o] = !none && (was || t == a.end);
-      ++at;
-      offer();
+  // the beams' lists in the same way: scores as pairs (0: none), ties to the lowest beam and, in
+  // a beam, the order of its list
+  int valid = 0;
+  for (int i = threadIdx.x; i < W * W; i += kBsThreads) {
+    const int w = i / W;
+    const unsigned long long k = s_row[w][i - w * W];
+    unsigned long long score = 0;
+    if (k != 0) {
+      Pair v = s_off[w];
+      if (k >> 32 != 1) v = add(sum2(bs_value((uint32_t)(k >> 32)), v.hi), Pair{v.lo, 0.f});
+      score = (unsigned long long)bs_ordered(v.hi + 0.f) << 32 | bs_ordered(v.lo + 0.f);
+      ++valid;
     }
-    __syncwarp();
+    s_u.beam.score[w][i - w * W] = score;
+  }
+  if (threadIdx.x == 0) s_n = 0;
+  __syncthreads();
+  if (valid) atomicAdd(&s_n, valid);
+  for (int i = threadIdx.x; i < W * W; i += kBsThreads) {
+    const int w = i / W, e = i - w * W;
+    const unsigned long long head = s_u.beam.score[w][0];
+    int r = 0;
+#pragma unroll 4
+    for (int o = 0; o < W; ++o) {
+      const unsigned long long v = s_u.beam.score[o][0];
+      r += v > head || (v == head && o < w);
+    }
+    if (r + e < W) {
+      s_u.beam.some[bs_first(r, W) + e] = s_u.beam.score[w][e];
+      s_u.beam.place[bs_first(r, W) + e] = i;
+    }
+  }
+  const int n = bs_first(W, W);
+  __syncthreads();
+  for (int i = threadIdx.x; i < n; i += kBsThreads) {
+    const unsigned long long v = s_u.beam.some[i];
+    const int at = s_u.beam.place[i];
+    int rank = 0, same = 0;
+#pragma unroll 8
+    for (int o = 0; o < n; ++o) {
+      const unsigned long long u = s_u.beam.some[o];
+      rank += u > v, same += u == v;
+    }
+    if (v == 0) continue;
+    if (same > 1)
+      for (int o = 0; o < n; ++o) rank += s_u.beam.some[o] == v && s_u.beam.place[o] < at;
+    if (rank < W) {
+      const int w = at / W, c = b * W + rank, t = (int)~(uint32_t)s_row[w][at - w * W];
+      a.parent[c] = w;
+      a.token[c] = t;
+      a.new_score[c] = bs_value((uint32_t)(v >> 32));
+      if (a.new_done) a.new_done[c] = s_done[w] || t == a.end;
+    }
+  }
+  __syncthreads();
+  for (int i = s_n + threadIdx.x; i < W; i += kBsThreads) {  // fewer candidates than places
+    const int c = b * W + i;
+    a.parent[c] = -1;
+    a.token[c] = -1;
+    a.new_score[c] = -INFINITY;
+    if (a.new_done) a.new_done[c] = 0;
   }
 }
 
 // Pieces of a row: as many as it needs to be held in registers, more where the rows do not
-// fill the GPU.
-static int bs_splits(int rows, int V) {
-  int S = std::min(kBsSplits, (V + kBsPiece - 1) / kBsPiece);
-  while (2 * S <= kBsSplits && (long long)rows * S < 152 && V / S >= 4096) S *= 2;
+// fill the GPU, and no more than the lists' room.
+static int bs_splits(int rows, int W, int V) {
+  const int most = std::min(kBsSplits, kBsLists / W);
+  int S = std::min(most, (V + kBsPiece - 1) / kBsPiece);
+  while (2 * S <= most && (long long)rows * S < 152 && V / S >= 4096) S *= 2;
   return S;
 }
 
 static size_t bs_align(size_t n) { return (n + 255) / 256 * 256; }
 
 size_t beam_select_ws_bytes(int B, int W, int V) {
-  const size_t rows = (size_t)B * W, S = bs_splits((int)rows, V);
+  const size_t rows = (size_t)B * W, S = bs_splits((int)rows, W, V);
   return kBsHead + bs_align(rows * S * 8) + rows * S * W * 8;
 }
 
@@ -345,7 +401,7 @@ cudaError_t launch_beam_select(const float* logits, int V, int B, int W, const f
                                int32_t* parent, int32_t* token, float* new_score, int32_t* new_done, void* ws, int32_t* err,
                                cudaStream_t s) {
   if (B <= 0) return cudaSuccess;
-  const int S = bs_splits(B * W, V);
+  const int S = bs_splits(B * W, W, V);
   uint8_t* p = (uint8_t*)ws;
   uint8_t* sums = p + kBsHead;
   uint8_t* best = sums + bs_align((size_t)B * W * S * 8);
