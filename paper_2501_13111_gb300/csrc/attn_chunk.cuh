@@ -269,6 +269,23 @@ struct CkWalk {
   }
 };
 
+// A row's sums so far (reference, sum of P) and another part's: the factors of what they hold
+// for the reference of both.  In operations of one rounding each, so that the order of the
+// parts alone decides the bits, wherever they are added.
+struct CkSum {
+  float m, l;
+  FP_DEV float2 add(float2 ml) {
+    const float m2 = fmaxf(m, ml.x), c0 = exp2f(m - m2), c1 = exp2f(ml.x - m2);
+    m = m2;
+    l = __fmaf_rn(ml.y, c1, __fmul_rn(l, c0));
+    return make_float2(c0, c1);
+  }
+};
+FP_DEV float4 ck_add(float4 r, float4 f, float2 c) {
+  return make_float4(__fmaf_rn(f.x, c.y, __fmul_rn(r.x, c.x)), __fmaf_rn(f.y, c.y, __fmul_rn(r.y, c.x)),
+                     __fmaf_rn(f.z, c.y, __fmul_rn(r.z, c.x)), __fmaf_rn(f.w, c.y, __fmul_rn(r.w, c.x)));
+}
+
 // Which of the 64 keys from tree row j0 on (below 0: the prefix, seen by every row) a row
 // with these mask words sees, of the first `count` that the cache holds.
 FP_DEV unsigned long long ck_tree_seen(const uint32_t* words, int stride, int j0, int count) {
@@ -291,14 +308,14 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   struct Bars {
     uint64_t kfull[R], vfull[R], kempty[R], vempty[R], qfull, qempty, sfull[2], hdone[2], pfull[2][2], ofull[2], oempty[2], part[2], join, met[4],
-        mma, dfull[kCkPieces], dempty[kCkPieces], done[2], ifull[kCkAhead], iempty[kCkAhead];
+        mma, dfull[kCkPieces], dempty[kCkPieces], done[2], sfill[kCkScales], ask, ifull[kCkAhead], iempty[kCkAhead];
   };
   __shared__ Bars bar;
   __shared__ CkPiece s_piece[kCkPieces];
   __shared__ float2 s_ml[2][2][kCkKeys];         // [parity][group][row]: maximum and sum, units of one tile
   __shared__ uint32_t tmem_base;
   __shared__ CkPiece s_left[2];                  // units that other CTAs have a part of
-  __shared__ int abort_word, s_last[2];
+  __shared__ int abort_word, s_last[2], s_alone;
   __shared__ int2 s_page[KV8 ? kCkAhead : 1][8];  // int8: pool row of a tile's pages, and how many of their rows count
   __shared__ __align__(16) float s_scale[KV8 ? kCkScales : 1][2][kCkKeys];  // int8: K's (by hd^-1/2 log2 e) and V's
   volatile int* abort_flag = &abort_word;
@@ -360,6 +377,8 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
     uint8_t* dst = is_v ? sV : sK;
     int n = 0, kn = 0;
     bool ok = true;
+    CkPiece end;  // (warp 8) the stretch's last piece
+    end.flags = 6;
     auto copy = [&](const CkPiece& w) {
       const int32_t* pt = a.page_table + (long long)w.b * a.pages_per_seq;
       // The Q tiles, behind the first key tile: that one goes out (and the widening of the
@@ -413,20 +432,25 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
         id = page(w.t0 + 1);
         for (int t = w.t0; t < w.t1; ++t, ++kn) {
           const int s = kn % kCkAhead;
-          const float c = kPaLog2e * rsqrtf((float)HD);
-          const float4 kf = make_float4(ks[0] * c, ks[1] * c, ks[2] * c, ks[3] * c), vf = make_float4(vs[0], vs[1], vs[2], vs[3]);
           const int2 page_rows = make_int2(at, rows);
+          float k0[4], v0[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) k0[i] = ks[i], v0[i] = vs[i];
           if (t + 1 < w.t1) fetch(t + 1), id = page(t + 2);
           if (kn >= kCkAhead) ok = mbar_wait(&bar.iempty[s], ((kn / kCkAhead) & 1) ^ 1);
           ok = __all_sync(0xffffffffu, ok && !*abort_flag);
           if (!ok) return;
-          *reinterpret_cast<float4*>(&s_scale[kn % kCkScales][0][lane * 4]) = kf;
-          *reinterpret_cast<float4*>(&s_scale[kn % kCkScales][1][lane * 4]) = vf;
+          // (the pages first: the codes need not wait for the scales)
           if (lane < 8) s_page[s][lane] = page_rows;
           __syncwarp();
           if (lane == 0) mbar_arrive(&bar.ifull[s]);
           if (t == w.t0) queries();
           if (!ok) return;
+          const float c = kPaLog2e * rsqrtf((float)HD);
+          *reinterpret_cast<float4*>(&s_scale[kn % kCkScales][0][lane * 4]) = make_float4(k0[0] * c, k0[1] * c, k0[2] * c, k0[3] * c);
+          *reinterpret_cast<float4*>(&s_scale[kn % kCkScales][1][lane * 4]) = make_float4(v0[0], v0[1], v0[2], v0[3]);
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&bar.sfill[kn % kCkScales]);
         }
       } else {
         auto page = [&](int t) {
@@ -481,6 +505,7 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
       CkPiece w;
       while (next(w, ok)) {
         if (!w.empty()) copy(w);
+        end = w;
         if (!ok) break;
       }
       if (KV8 && ok) {  // no more tiles
@@ -491,6 +516,18 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
           mbar_arrive(&bar.ifull[s]);
         }
       }
+    }
+    if (!is_v && lane == 0) {
+      // The last unit, if other CTAs go on with it: have they all left their parts?  Then this
+      // CTA adds them to its own as it writes the rows.
+      bool alone = false;
+      if (ok && end.first() && !end.last() && end.parts <= kCkGroup) {
+        int n;
+        asm volatile("ld.acquire.gpu.global.s32 %0, [%1];" : "=r"(n) : "l"(reinterpret_cast<int*>(a.ws) + end.own * kCkTickets) : "memory");
+        alone = n == end.parts - 1;
+      }
+      s_alone = alone;
+      mbar_arrive(&bar.ask);
     }
     if (!ok && lane == 0) fail();
     if (lane == 0) {  // copies still in flight land before the CTA leaves
@@ -754,6 +791,7 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
       if (warp == 0) {
         ok = __all_sync(0xffffffffu, mbar_wait(&bar.part[left - 1], 0));
         if (lane == 0 && ok) {
+          __threadfence();  // (the other warps' rows too: they arrived behind them)
           const CkPiece& p = s_left[left - 1];
           const int mine = (blockIdx.x - p.own) / kCkGroup;
           int* t = reinterpret_cast<int*>(a.ws) + p.own * kCkTickets + mine;
@@ -790,6 +828,11 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
           if (h == 0) {
             ok = __all_sync(0xffffffffu, mbar_wait(&bar.sfull[j], sn & 1));
             if (!ok) break;
+            if constexpr (KV8) {
+              const int x = kb + t - w.t0;
+              ok = __all_sync(0xffffffffu, mbar_wait(&bar.sfill[x % kCkScales], (x / kCkScales) & 1));
+              if (!ok) break;
+            }
             if (behind && t > t_first) ticket();
           }
           if (!on_warp) {
@@ -886,6 +929,12 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
       kb += max(0, w.t1 - w.t0);
       // ---- the piece's output
       const bool whole = w.first() && w.last(), empty = w.empty();
+      bool alone = false;  // the others' parts are there: this CTA's is the last
+      if (w.first() && !w.last()) {
+        ok = __all_sync(0xffffffffu, mbar_wait(&bar.ask, 0));
+        if (!ok) break;
+        alone = s_alone;
+      }
       const bool use0 = w.uses(0), use1 = w.uses(1);
       float a0 = 1.f, a1 = 0.f;  // factors of O_0 and O_1 (units of one tile)
       if (pair) {
@@ -948,6 +997,40 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
             load(x, r);
             write(w, at, x, r, inv);
           }
+        } else if (alone) {
+          // this part, then the others in their order, as the join below has them
+          int at[4];
+          begins(w, rb, at);
+          const float ls = have ? l : 0.f;
+          const float2 own = make_float2(ls == 0.f ? -INFINITY : m == -INFINITY ? 0.f : m, ls);
+#pragma unroll 1
+          for (int x = x0; x < x1; x += 32) {
+            CkSum sum = {-INFINITY, 0.f};
+            float r[32];
+            load(x, r);
+            if (own.x == -INFINITY) {
+#pragma unroll
+              for (int y = 0; y < 32; ++y) r[y] = 0.f;
+            } else {
+              sum.add(own);
+            }
+#pragma unroll 1
+            for (int i = 1; i < w.parts; ++i) {
+              const uint8_t* p = slot(w, i);
+              const float2 ml = __ldcg(reinterpret_cast<const float2*>(p + ML) + rb * 32 + lane);
+              float4 f[8];
+#pragma unroll
+              for (int y = 0; y < 8; ++y) f[y] = __ldcg(reinterpret_cast<const float4*>(p) + (size_t)(x / 4 + y) * kCkRows + rb * 32 + lane);
+              if (ml.x == -INFINITY) continue;  // (its O may not have been written)
+              const float2 c = sum.add(ml);
+#pragma unroll
+              for (int y = 0; y < 8; ++y) {
+                const float4 o = ck_add(make_float4(r[4 * y], r[4 * y + 1], r[4 * y + 2], r[4 * y + 3]), f[y], c);
+                r[4 * y] = o.x, r[4 * y + 1] = o.y, r[4 * y + 2] = o.z, r[4 * y + 3] = o.w;
+              }
+            }
+            write(w, at, x, r, sum.l == 0.f ? 0.f : 1.f / sum.l);
+          }
         } else {
           uint8_t* p = slot(w, blockIdx.x - w.own);
           if (have)
@@ -980,12 +1063,13 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
           }
         }
       }
-      if (!whole) {
+      if (alone) {
+        if (threadIdx.x == 0) reinterpret_cast<int*>(a.ws)[w.own * kCkTickets] = 0;
+      } else if (!whole) {
         if (behind) ticket();
         if (threadIdx.x == 0) s_left[left] = w;
         ++left;
         // (the ticket waits for a tile of the next piece, by when every warp is here)
-        __threadfence();
         __syncwarp();
         if (lane == 0) mbar_arrive(&bar.part[left - 1]);
         behind = true;
@@ -1017,7 +1101,8 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
 #pragma unroll 1
         for (int item = warp; item < (rows + 31) / 32 * (HD / 32); item += kCkSoft) {
           const int rb = item / (HD / 32), x = item % (HD / 32) * 32;
-          float mm = -INFINITY, ll = 0.f, r[32];
+          CkSum sum = {-INFINITY, 0.f};
+          float r[32];
 #pragma unroll
           for (int y = 0; y < 32; ++y) r[y] = 0.f;
 #pragma unroll 2
@@ -1028,22 +1113,20 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
 #pragma unroll
             for (int y = 0; y < 8; ++y) f[y] = __ldcg(reinterpret_cast<const float4*>(p) + (size_t)(x / 4 + y) * kCkRows + rb * 32 + lane);
             if (ml.x == -INFINITY) continue;  // (its O may not have been written)
-            const float m2 = fmaxf(mm, ml.x), c0 = exp2f(mm - m2), c1 = exp2f(ml.x - m2);
-            mm = m2;
-            ll = ll * c0 + ml.y * c1;
+            const float2 c = sum.add(ml);
 #pragma unroll
             for (int y = 0; y < 8; ++y) {
-              r[4 * y] = r[4 * y] * c0 + f[y].x * c1, r[4 * y + 1] = r[4 * y + 1] * c0 + f[y].y * c1;
-              r[4 * y + 2] = r[4 * y + 2] * c0 + f[y].z * c1, r[4 * y + 3] = r[4 * y + 3] * c0 + f[y].w * c1;
+              const float4 o = ck_add(make_float4(r[4 * y], r[4 * y + 1], r[4 * y + 2], r[4 * y + 3]), f[y], c);
+              r[4 * y] = o.x, r[4 * y + 1] = o.y, r[4 * y + 2] = o.z, r[4 * y + 3] = o.w;
             }
           }
           if (turn == 0) {
             keep(slot(w, i0), rb, x, r);
-            if (x == 0) reinterpret_cast<float2*>(slot(w, i0) + ML + kCkRows * 8)[rb * 32 + lane] = make_float2(mm, ll);
+            if (x == 0) reinterpret_cast<float2*>(slot(w, i0) + ML + kCkRows * 8)[rb * 32 + lane] = make_float2(sum.m, sum.l);
           } else {
             int at[4];
             begins(w, rb, at);
-            write(w, at, x, r, ll == 0.f ? 0.f : 1.f / ll);
+            write(w, at, x, r, sum.l == 0.f ? 0.f : 1.f / sum.l);
           }
         }
         if (turn == 0) {
