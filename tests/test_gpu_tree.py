@@ -565,9 +565,19 @@ def test_verify(fp, ns, V):
         _same(_verify(fp, p, cu, parent, tokens, u), _expected(p, cu, parent, tokens, u))
 
 
-def test_verify_goes_all_the_way_down(fp):
-    """A chain of 200 whose every draft is certain."""
-    n, V = 200, 300
+@pytest.mark.parametrize("ns,V", [([64] * 40, 517), ([300] * 7, 5003), ([1], 1 << 20), ([3], 300001), ([20, 21], 850001),
+                                  ([7] * 30, 200003)])
+def test_verify_every_way_of_drawing(fp, ns, V):
+    """Thousands of rows (a warp each), rows of a million tokens (clusters, several groups a lane and chunk), and more
+    than 2^25 weights in all (one row after the other)."""
+    p, cu, parent, tokens, u = _problem(11, ns, V, lead=1, tail=2)
+    _same(_verify(fp, p, cu, parent, tokens, u), _expected(p, cu, parent, tokens, u))
+
+
+@pytest.mark.parametrize("n", [200, 1500])
+def test_verify_goes_all_the_way_down(fp, n):
+    """A chain whose every draft is certain; 1500 rows are more than are staged at once."""
+    V = 300
     rng = np.random.default_rng(1)
     tokens = rng.integers(0, V, n)
     p = np.zeros((n, V), np.float32)
@@ -612,6 +622,33 @@ def test_verify_reports_what_cannot_be_drawn(fp):
     _same(_verify(fp, p, cu, parent, tokens, u), want)
     for bad in ([0, 5, 3, 13], [0, 9, 13, 14], [-2, 1, 7, 13]):
         assert _verify(fp, p, bad, parent, tokens, u)[3] == 1
+
+
+def test_cache_offsets_past_32_bits(fp):
+    """A pool of more than 2^32 elements: append, commit and copy at its far end."""
+    torch = torch_mod()
+    if torch.cuda.mem_get_info()[0] < 24 << 30:
+        pytest.skip("needs 24 GB of device memory")
+    hd, H, Hkv, n = 128, 4, 2, 20
+    pages = (1 << 32) // (Hkv * 16 * hd) + 64  # 8.6 GB a pool
+    pool = torch.zeros((2, pages, Hkv, 16, hd), dtype=torch.bfloat16, device="cuda")
+    table = np.array([[pages - 1, 3, pages - 17]], np.int32)
+    view = fp.fp_kv_view(0, Hkv, hd, 16, 3, pages, pool[0].data_ptr(), pool[1].data_ptr(), None, None, ptr(dev(table)))
+    qkv = synth.uniform_bf16(5, 1, (n, (H + 2 * Hkv) * hd), -2, 2)
+    cu, pos, err = dev(np.array([0, n], np.int32)), dev(np.array([13], np.int32)), empty(1, np.int32)
+    path = [0, 2, 3, 9, 15, 19]
+    fp.fp_op_rope_kv_tree(ptr(dev(qkv)), qkv.shape[1], n, 1, H, view, ptr(cu), ptr(pos), ptr(dev(np.zeros(n, np.int32))),
+                          ptr(_table(fp, 3, hd)), ptr(empty((n, H * hd), np.uint16)), H * hd, ptr(err))
+    fp.fp_op_kv_commit(view, n, 1, ptr(cu), ptr(pos), ptr(dev(np.array(path + [-1] * 14, np.int32))), ptr(err))
+    fp.fp_op_kv_copy(view, 1, ptr(dev(np.array([pages - 1], np.int32))), ptr(dev(np.array([pages - 5], np.int32))),
+                     ptr(dev(np.array([16], np.int32))), ptr(err))
+    assert host(err, np.int32)[0] == 0
+    v = qkv.reshape(n, -1, hd)[:, H + Hkv :]
+    for j, r in enumerate(path):
+        page, slot = int(table[0, (13 + j) // 16]), (13 + j) % 16
+        assert np.array_equal(pool[1, page, :, slot].view(torch.int16).cpu().numpy().view(np.uint16), v[r]), j
+        if page == pages - 1:
+            assert torch.equal(pool[:, pages - 5, :, slot], pool[:, page, :, slot])
 
 
 # ------------------------------------------------------------------ a whole step
