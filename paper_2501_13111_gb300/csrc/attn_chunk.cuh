@@ -381,8 +381,9 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
     end.flags = 6;
     auto copy = [&](const CkPiece& w) {
       const int32_t* pt = a.page_table + (long long)w.b * a.pages_per_seq;
-      // The Q tiles, behind the first key tile: that one goes out (and the widening of the
-      // last unit's last tile, which looks a tile ahead, goes on) while Q is still in use.
+      // The Q tiles: the first piece's at once, others behind their first key tile: that one
+      // goes out (and the widening of the last unit's last tile, which looks a tile ahead, goes
+      // on) while Q is still in use.
       auto queries = [&]() {
         if (n > 0) ok = mbar_wait(&bar.qempty, (n - 1) & 1) && !*abort_flag;
         ok = __all_sync(0xffffffffu, ok);
@@ -398,6 +399,8 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
         }
         ++n;
       };
+      const bool at_once = !is_v && n == 0;
+      if (at_once) queries();
       if constexpr (KV8) {
         // the tile's pages to the widening warps, its codes and scales to L2
         auto page = [&](int t) {
@@ -444,7 +447,7 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
           if (lane < 8) s_page[s][lane] = page_rows;
           __syncwarp();
           if (lane == 0) mbar_arrive(&bar.ifull[s]);
-          if (t == w.t0) queries();
+          if (t == w.t0 && !at_once) queries();
           if (!ok) return;
           const float c = kPaLog2e * rsqrtf((float)HD);
           *reinterpret_cast<float4*>(&s_scale[kn % kCkScales][0][lane * 4]) = make_float4(k0[0] * c, k0[1] * c, k0[2] * c, k0[3] * c);
@@ -472,7 +475,7 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
           if (lane < 8) ck_tma_4d(dst + s * TILE + lane * PAGE, map, 0, 0, 0, group, &full[s]);
           ++kn;  // in flight from here on, wherever this ends: the drain below waits for it
           id = next_id;
-          if (!is_v && t == w.t0) queries();
+          if (!is_v && t == w.t0 && !at_once) queries();
           if (!ok) return;
         }
       }
