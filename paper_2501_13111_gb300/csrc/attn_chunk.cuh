@@ -1,7 +1,10 @@
 // Attention of a chunk of new tokens over the paged cache, on the tcgen05 tensor
 // cores: row i of sequence b (position pos[b] + i) attends over positions
 // 0 .. pos[b] + i, o = softmax(q K^T / sqrt(hd)) V, for ragged chunks of one token to
-// thousands (chunked prefill, drafted tokens, decoding, mixed).
+// thousands (chunked prefill, drafted tokens, decoding, mixed).  TREE (fp_attn_tree.cu): over
+// the prefix and those of the sequence's own rows that its mask words name; then every unit
+// takes all of the sequence's key tiles, and a row's 64 bits of a half tile behind the prefix
+// come from its words by two funnel shifts.
 //
 // One persistent CTA per SM takes an equal stretch of the line of units that
 // chunk_items.h lays out: tiles of 128 packed rows (the heads of a KV head's group
@@ -16,7 +19,10 @@
 //               half's products run while the second half is computed; the reference m
 //               moves only when a half passes it by 2^8 (O and the row sum are rescaled
 //               then).  At the end of a piece they write its rows, or the part
-//               that this CTA has of them: the last CTA to finish a unit adds its parts up;
+//               that this CTA has of them: the last CTA to finish a unit adds its parts up.
+//               The CTA that begins a unit mostly is: the others have that unit first in their
+//               stretches, it last, so it asks before it writes and adds the others' parts to its
+//               rows on their way out (written, fenced and read back: long trees 107 us, not 100);
 //   warp 8      TMA: the unit's Q tiles (one box per 64 columns: tokens x heads) and,
 //               page by page, the keys.  One box a page, in the order [8 rows][64
 //               columns] the descriptors step through.  (int8 cache: it finds the pages
@@ -34,14 +40,18 @@
 //               bf16(q s) took 54 us where this takes 63, 420 where 496, see below, but
 //               were further from the sums in 64 bits: 0.0040 against 0.0024, relative.)
 // Measured (launches in a graph, heads of 128): 8 sequences of 5 rows to position 612, 32
-// heads, bf16 cache 23.1 us (2.7 TB/s); 32 of 5 rows to 2148, 64 heads on 8, int8 63 us
-// (1.8 TB/s); 4 chunks of 512 rows to 2048, 40 heads, bf16 77 us (747 TFLOP/s); 2 of 1024
-// rows to 8000, 64 heads on 8, int8 496 us (815 TFLOP/s).  A step of two query tiles takes
-// about 3800 cycles where its MMAs need 2080: a group's scores wait for its P, P for the
-// scores, and what is in between is as long as the other group's products; with an int8
+// heads, bf16 cache 23.7 us (2.6 TB/s); 32 of 5 rows to 2148, 64 heads on 8, int8 63 us
+// (1.8 TB/s); 4 chunks of 512 rows to 2048, 40 heads, bf16 69 us (834 TFLOP/s); 2 of 1024
+// rows to 8000, 64 heads on 8, int8 487 us (830 TFLOP/s).  Trees: 8 of up to 26 rows to 612,
+// 32 heads, bf16 24.9 us (3.0 TB/s); 32 of up to 16 rows to 2148, 64 heads on 8, int8 65.5 us
+// (1.9 TB/s), bf16 49 us (4.7 TB/s); 8 of up to 64 rows to 8000, 64 heads on 8, bf16 99 us (828
+// TFLOP/s).  A step of two query tiles takes 3000 to 3800 cycles where its MMAs need 2150: a
+// group's scores wait for its P, P for the scores, and what is in between (1900 cycles) is as
+// long as the other group's products; with an int8
 // cache the scales' way from shared memory, which the MMAs keep busy, comes on top (chunk
-// int8 406 us with constants instead).  Small batches: about 7000 cycles
-// pass before the first scores and 8000 behind the last.
+// int8 406 us with constants instead), and half a tile's softmax takes 2200 cycles, not 950,
+// beside the widening.  Small batches: 6 to 9 us pass between the launch and the first scores
+// (the plan 1.9, the pages 1.1, the first tiles of all SMs at once 2.8), 2 us behind the last.
 // Slots behind the sequence's last position may hold anything: their scores are
 // masked, their V rows are zeroed before the product (int8 cache: read as zeros).
 // Every wait on an mbarrier is bounded (error 2 past the limit).

@@ -1,5 +1,5 @@
 // Pieces shared by the tcgen05 attention kernels (fp_attn_tc.cu,
-// fp_attn_short.cu, fp_attn_chunk.cu): operand descriptors, conversions, launch limits.
+// fp_attn_short.cu, attn_chunk.cuh): operand descriptors, conversions, launch limits.
 #pragma once
 
 #include "attn_items.h"

@@ -1,4 +1,4 @@
-// How the attention of a chunk is cut up (fp_attn_chunk.cu).  Host and device.
+// How the attention of a chunk is cut up (attn_chunk.cuh).  Host and device.
 //
 // The G query heads of a KV head read the same keys, so their rows are packed:
 // row r of a query tile is token r / G, head r % G; a tile holds the largest power of
@@ -9,7 +9,7 @@
 // starting it costs, and for each of its key tiles as many as it has query tiles, one
 // or two.  CTA c of g takes an equal stretch of that line, so every SM has as much to
 // do whatever the lengths are; a unit that a border cuts leaves a partial result with
-// every CTA, and the last of them to finish adds them (fp_attn_chunk.cu).
+// every CTA, and the last of them to finish adds them (attn_chunk.cuh).
 #pragma once
 
 #include <algorithm>

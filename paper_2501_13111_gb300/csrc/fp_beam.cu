@@ -18,6 +18,13 @@ namespace fpk {
 // pairs of fp32.  The normaliser: with an integer reference k (the maximum's log2,
 // rounded up), sum_i 2^(x_i log2 e - k) in fp32, one rounding an exponent; pieces with
 // other references are scaled exactly; lse = (k + exponent of s) ln 2 + log(significand of s).
+// Sorting is by counting: a value's place is the number of larger ones, found by comparisons
+// that wait for nothing.  (One maximum after the other took 12 us where this takes 10.)  A
+// piece's candidates are the few values that reach the W-th largest of 32 groups' maxima; of
+// sorted lists, ordered by their heads, entry e of the r-th counts only if r + e < W.
+// Measured: 32 groups of 4 beams, 32000 tokens 10.2 us (1.6 TB/s), 1 of 8, 128001 tokens
+// 10.1.  Bound by latency: loads 2.5 us, exponentials 0.7, candidates 1.5, the group's ticket 1.2,
+// lists 1.5, beams 1.
 constexpr int kBsThreads = 512, kBsWarps = kBsThreads / 32, kBsItems = 8;
 constexpr int kBsPiece = kBsThreads * kBsItems * 4;  // values held at once
 constexpr int kBsSplits = 32;                        // pieces of a row, at most
@@ -382,7 +389,8 @@ __global__ void __launch_bounds__(kBsThreads, 2) beam_select_kernel(const BsArgs
 }
 
 // Pieces of a row: as many as it needs to be held in registers, more where the rows do not
-// fill the GPU, and no more than the lists' room.
+// fill the GPU, and no more than the lists' room (us: 8 rows of 128001 as 8 | 16 pieces 12.4 |
+// 11.3, 128 rows of 32000 as 1 | 2 | 4 pieces 17 | 11.6 | 14).
 static int bs_splits(int rows, int W, int V) {
   const int most = std::min(kBsSplits, kBsLists / W);
   int S = std::min(most, (V + kBsPiece - 1) / kBsPiece);
@@ -419,7 +427,7 @@ cudaError_t launch_beam_select(const float* logits, int V, int B, int W, const f
 // pages of the beams without children (there are as many as are needed), into which the
 // parent's rows then have to be copied.  So nothing that is copied from is written to,
 // and no page is taken or given back.  One CTA a beam, its group's parents in a warp's
-// lanes.  Bound by latency.
+// lanes.  Bound by latency: 128 beams of 135 pages 2.0 us.
 __global__ void __launch_bounds__(128)
     beam_reorder_kernel(int W, int pps, int page_size, const int32_t* __restrict__ len, const int32_t* __restrict__ parent,
                         const int32_t* __restrict__ in, int32_t* __restrict__ out, int32_t* __restrict__ from,
@@ -469,7 +477,8 @@ cudaError_t launch_beam_reorder(int B, int W, int pps, int page_size, const int3
 // ------------------------------------------------------------------ copies of pages
 // The first rows of one page to another, all KV heads, K, V and scales.  A head's rows
 // stand together, so a copy is 2 Hkv runs; a warp takes a run, 16 bytes a lane, all of it
-// on its way before the first is written.  Bound by latency, then bytes.
+// on its way before the first is written.  Bound by latency, then bytes: 128 beams, 8 int8
+// heads 2.0 us, 40 beams, 40 bf16 heads 2.1 us.
 constexpr int kKcWarps = 8;
 
 template <int RB>  // bytes of a head's row

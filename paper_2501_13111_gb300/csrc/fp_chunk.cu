@@ -38,10 +38,12 @@ FP_DEV uint2 codes8(const float* x, float s) {
 // and (by shuffles among those lanes) a row's maximum stay in the warp, and each
 // lane reads its cosines once for all heads.  Bound by bytes (qkv in, queries and
 // cache rows out) for many rows, by latency for few: with the read back below, chunks of
-// 4 x up to 1000 rows of 40 heads take 64 us (5.4 TB/s), 160 rows of 64 heads on 8, int8, 7.4.
+// 4 x up to 1000 rows of 40 heads take 63 us (5.5 TB/s), 160 rows of 64 heads on 8, int8, 6.6.
 // Four CTAs an SM, for the loads in flight: 64 registers, a few of 74 spilled (three: 68 us,
 // five: 71).
 // TREE: a row's place in the cache is pos[b] + i, what it is rotated by pos[b] + depth[row].
+// 32 trees of up to 16 rows, 64 heads on 8, int8, 7.3 us; 8 of up to 64, 40 heads, bf16 6.7: three
+// chains of loads (sequence, position and depth, page and cosines) one behind the other.
 template <int HD, bool KV8, bool TREE>
 __global__ void __launch_bounds__(256, 4)
     rope_kv_chunk_kernel(const uint16_t* qkv, int row_stride, int n_tokens, int B, int H, fp_kv_view kv,
