@@ -69,7 +69,7 @@
 namespace fpk {
 
 constexpr int kCkSoft = 8;                        // softmax warps
-constexpr int kCkWarpQ = 8, kCkWarpMma = 9, kCkWarpPlan = 11, kCkWarpWiden = 12, kCkWiden = 8;
+constexpr int kCkWarpQ = 8, kCkWarpMma = 9, kCkWarpPlan = 11, kCkWarpWiden = 12, kCkWiden = 4;
 template <bool KV8>
 constexpr int ck_threads() { return KV8 ? (kCkWarpWiden + kCkWiden) * 32 : 384; }
 // Registers a thread: 384 threads may have 168, and take 163 or 167 (heads of 128, 64);
@@ -376,7 +376,7 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
     return !w.done();
   };
 
-  if (KV8 && warp >= kCkSoft) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+  if (KV8 && warp >= kCkSoft) asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
   if (warp == kCkWarpPlan || warp == kCkWarpQ) {
     // ---------------- warp 11: the plan, the pieces, V.  Warp 8: Q tiles and K.  Lanes
     // 0-7 copy a page of a key tile each; the next tile's page ids are read while this
@@ -683,7 +683,7 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
     // is filled again, for the next tile, as soon as it has been written out: a whole
     // tile's codes, 32 KB an SM, are in flight throughout, across pieces too.
     constexpr int C = HD / 16;                                      // chunks a row
-    constexpr int PER = 16 * kCkWiden / C, N = kCkKeys / PER;       // rows at a time, turns a tile
+    constexpr int PER = 16 * kCkWiden / C, N = 8, H = kCkKeys / PER / N;  // rows at a time, turns a part, parts a tile
     const bool is_v = warp >= kCkWarpWiden + kCkWiden / 2;
     // four chunks of two rows go out at a time, whose swizzles differ: eight banks of 16 bytes
     const int wi = threadIdx.x % (16 * kCkWiden), c = C == 4 ? wi & 3 : (wi & 3) | (wi >> 1 & 4);
@@ -693,16 +693,16 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
     uint8_t* tiles = (is_v ? sV : sK) + (rr >> 3) * SBO + (c >> 2) * 1024 + (rr & 7) * 128;
     const int o0 = ((2 * (c & 3)) ^ (rr & 7)) << 4, o1 = ((2 * (c & 3) + 1) ^ (rr & 7)) << 4;
     uint4 cw[N];
-    int row[N];  // pool rows (fewer than 2^31) of the tile to be read; -1 reads zeros
+    int row[N];  // pool rows (fewer than 2^31) of the part to be read; -1 reads zeros
     bool ok = true;
-    // this thread's rows of tile k; false: there is none (or a wait ran out)
-    auto rows = [&](int k) {
+    // this thread's rows of part h of tile k; false: there is none (or a wait ran out)
+    auto rows = [&](int k, int h) {
       const int s = k % kCkAhead;
-      ok = __all_sync(0xffffffffu, mbar_wait(&bar.ifull[s], (k / kCkAhead) & 1));
+      if (h == 0) ok = __all_sync(0xffffffffu, ok && mbar_wait(&bar.ifull[s], (k / kCkAhead) & 1));
       const bool there = ok && s_page[s][0].x != -2;
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        const int r = i * PER + rr;
+        const int r = (h * N + i) * PER + rr;
         const int2 p = s_page[s][r >> 4];
         row[i] = there && (r & 15) < p.y ? p.x + (r & 15) : -1;
       }
@@ -711,32 +711,37 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
     auto fetch = [&](int i) {
       cw[i] = row[i] >= 0 ? ld_nc16(pool + (long long)row[i] * HD) : make_uint4(0, 0, 0, 0);
     };
-    bool more = rows(0);
+    bool more = rows(0, 0);
 #pragma unroll
     for (int i = 0; i < N; ++i) fetch(i);
-    for (int kn = 0; more; ++kn) {
+    for (int kn = 0; more && ok; ++kn) {
       const int s = kn % R;
-      more = rows(kn + 1);
-      if (kn >= R) ok = __all_sync(0xffffffffu, ok && mbar_wait(&empty[s], ((kn / R) & 1) ^ 1));
-      if (!ok) break;
+#pragma unroll 1
+      for (int h = 0; h < H && ok; ++h) {
+        if (h + 1 < H) rows(kn, h + 1);
+        else more = rows(kn + 1, 0);
+        if (h == 0 && kn >= R) ok = __all_sync(0xffffffffu, ok && mbar_wait(&empty[s], ((kn / R) & 1) ^ 1));
+        if (!ok) break;
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const uint32_t ww[4] = {cw[i].x ^ 0x80808080u, cw[i].y ^ 0x80808080u, cw[i].z ^ 0x80808080u, cw[i].w ^ 0x80808080u};
-        const float2 z2 = make_float2(-32896.f, -32896.f);
-        uint32_t o[8];
+        for (int i = 0; i < N; ++i) {
+          const uint32_t ww[4] = {cw[i].x ^ 0x80808080u, cw[i].y ^ 0x80808080u, cw[i].z ^ 0x80808080u, cw[i].w ^ 0x80808080u};
+          const float2 z2 = make_float2(-32896.f, -32896.f);
+          uint32_t o[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {  // codes 2j, 2j + 1: fp32 2^15 + 128 + q
-          const uint32_t u = ww[j >> 1];
-          const float lo = __uint_as_float(__byte_perm(u, 0x47000000u, (j & 1) ? 0x7424 : 0x7404));
-          const float hi = __uint_as_float(__byte_perm(u, 0x47000000u, (j & 1) ? 0x7434 : 0x7414));
-          const float2 f = pa_add2(make_float2(lo, hi), z2);
-          o[j] = pa_pack(f.x, f.y);
+          for (int j = 0; j < 8; ++j) {  // codes 2j, 2j + 1: fp32 2^15 + 128 + q
+            const uint32_t u = ww[j >> 1];
+            const float lo = __uint_as_float(__byte_perm(u, 0x47000000u, (j & 1) ? 0x7424 : 0x7404));
+            const float hi = __uint_as_float(__byte_perm(u, 0x47000000u, (j & 1) ? 0x7434 : 0x7414));
+            const float2 f = pa_add2(make_float2(lo, hi), z2);
+            o[j] = pa_pack(f.x, f.y);
+          }
+          uint8_t* rp = tiles + s * TILE + (h * N + i) * (PER / 8 * SBO);
+          *reinterpret_cast<uint4*>(rp + o0) = make_uint4(o[0], o[1], o[2], o[3]);
+          *reinterpret_cast<uint4*>(rp + o1) = make_uint4(o[4], o[5], o[6], o[7]);
+          fetch(i);
         }
-        uint8_t* rp = tiles + s * TILE + i * (PER / 8 * SBO);
-        *reinterpret_cast<uint4*>(rp + o0) = make_uint4(o[0], o[1], o[2], o[3]);
-        *reinterpret_cast<uint4*>(rp + o1) = make_uint4(o[4], o[5], o[6], o[7]);
-        fetch(i);
       }
+      if (!ok) break;
       fence_proxy_async();  // the MMAs read the tile through the async proxy
       __syncwarp();
       if (lane == 0) {
@@ -747,7 +752,7 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
     if (!ok && lane == 0) fail();
   } else if (warp < kCkSoft) {
     // ---------------- softmax: group j, row 32 quad + lane (TMEM begins at column 0)
-    if (KV8) asm volatile("setmaxnreg.inc.sync.aligned.u32 128;");
+    if (KV8) asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
     const int j = warp >> 2, quad = warp & 3, row = quad * 32 + lane;
     const uint32_t lane_base = (uint32_t)(quad * 32) << 16;
     const uint32_t ts = lane_base + j * kCkKeys, to = lane_base + kCkO + j * 128;
