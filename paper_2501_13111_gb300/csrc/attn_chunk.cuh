@@ -34,7 +34,7 @@
 //               there were five in a row.)  Warp 9 owns the TMEM;
 //   warp 11     plans the CTA's stretch, describes its pieces of units to the others,
 //               and (bf16 cache) copies the values;
-//   warps 12-19 (int8 cache) K and V tiles of the codes as bf16, exact (a byte permute
+//   warps 12-15, or 12-19 (int8 cache) K and V tiles of the codes as bf16, exact (a byte permute
 //               gives fp32 2^15 + 128 + q, a subtraction q).  A key's K scale multiplies
 //               its score column, its V scale its column of P, both in fp32.  (Tiles of
 //               bf16(q s) took 54 us where this takes 63, 420 where 496, see below, but
@@ -69,12 +69,15 @@
 namespace fpk {
 
 constexpr int kCkSoft = 8;                        // softmax warps
-constexpr int kCkWarpQ = 8, kCkWarpMma = 9, kCkWarpPlan = 11, kCkWarpWiden = 12, kCkWiden = 4;
-template <bool KV8>
-constexpr int ck_threads() { return KV8 ? (kCkWarpWiden + kCkWiden) * 32 : 384; }
-// Registers a thread: 384 threads may have 168, and take 163 or 167 (heads of 128, 64);
-// 640 (int8 cache) launch with 96, moved to the softmax: 256 x 128 + 384 x 72 < 640 x 96 (with 120 and 80 its row
-// spills more: chunk int8 504 us against 496)
+constexpr int kCkWarpQ = 8, kCkWarpMma = 9, kCkWarpPlan = 11, kCkWarpWiden = 12;
+// W: widening warps, 0 without an int8 cache, else 4 or 8 (launch_ck).
+constexpr int ck_threads(int W) { return (kCkWarpWiden + W) * 32; }
+// Registers a thread: 384 threads may have 168, and take 165 or 168 (heads of 128, 64).  With
+// an int8 cache all that the launch brings (512 x 128, 640 x 96) goes to the softmax and the
+// others, 256 x 168 + 256 x 88 or 256 x 144 + 384 x 64.  (Eight warps a whole tile of codes
+// ahead, 128 and 72, took 488 us for int8 chunks where four half a tile ahead take 446.)
+constexpr int ck_regs_soft(int W) { return W == 4 ? 168 : 144; }
+constexpr int ck_regs_other(int W) { return W == 4 ? 88 : 64; }
 constexpr int kCkReaders = kCkSoft + 3;           // warps that read each piece's description: softmax, Q, MMA
 constexpr int kCkPieces = 4;                      // pieces described ahead
 constexpr int kCkAhead = 4;                       // int8 cache: key tiles whose pages are known ahead
@@ -310,10 +313,11 @@ FP_DEV unsigned long long ck_tree_seen(const uint32_t* words, int stride, int j0
   return seen;
 }
 
-template <int HD, bool KV8, bool TREE>
-__global__ void __launch_bounds__(ck_threads<KV8>(), 1)
+template <int HD, int W, bool TREE>
+__global__ void __launch_bounds__(ck_threads(W), 1)
     attn_chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                       const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CkArgs a) {
+  constexpr bool KV8 = W > 0;
   constexpr int TILE = ck_tile_bytes<HD>(), NH = HD / 64, SBO = NH * 1024, PAGE = 2 * SBO, R = kCkRing;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   struct Bars {
@@ -344,17 +348,17 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
     // arrivals of each barrier, in their order
     constexpr int NB = sizeof(Bars) / 8;
     uint64_t* p = reinterpret_cast<uint64_t*>(&bar);
-    for (int i = threadIdx.x; i < NB; i += ck_threads<KV8>()) {
+    for (int i = threadIdx.x; i < NB; i += ck_threads(W)) {
       const uint64_t* q = p + i;
       int n = 1;
-      if (q < bar.kempty) n = KV8 ? kCkWiden / 2 : 1;
+      if (q < bar.kempty) n = KV8 ? W / 2 : 1;
       else if (q < &bar.qfull) n = 2;
       else if (q == &bar.qempty || q == &bar.mma) n = 2;
       else if (q >= &bar.pfull[0][0] && q < bar.ofull) n = 4;
       else if (q >= bar.oempty && q < bar.met) n = 8;  // oempty, part, join
       else if (q >= bar.met && q < &bar.mma) n = 2;
       else if (q >= bar.dempty && q < bar.done) n = kCkReaders;
-      else if (q >= bar.iempty) n = kCkWiden;
+      else if (q >= bar.iempty) n = max(W, 1);
       mbar_init(p + i, n);
     }
     if (threadIdx.x == 0) *abort_flag = 0;
@@ -376,7 +380,8 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
     return !w.done();
   };
 
-  if (KV8 && warp >= kCkSoft) asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+  if constexpr (KV8)
+    if (warp >= kCkSoft) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(ck_regs_other(W)));
   if (warp == kCkWarpPlan || warp == kCkWarpQ) {
     // ---------------- warp 11: the plan, the pieces, V.  Warp 8: Q tiles and K.  Lanes
     // 0-7 copy a page of a key tile each; the next tile's page ids are read while this
@@ -678,15 +683,17 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
     if (warp == kCkWarpMma) role(std::integral_constant<int, 0>());
     else role(std::integral_constant<int, 1>());
   } else if (KV8 && warp >= kCkWarpWiden) {
-    // ---------------- int8 cache: the codes of the key tiles' rows as bf16, four warps for K
-    // and four for V.  Thread: 16 codes (chunk c) of every PER-th row.  Each register of codes
-    // is filled again, for the next tile, as soon as it has been written out: a whole
-    // tile's codes, 32 KB an SM, are in flight throughout, across pieces too.
+    // ---------------- int8 cache: the codes of the key tiles' rows as bf16, half of the
+    // warps for K, half for V.  Thread: 16 codes (chunk c) of every PER-th row.  Each register of
+    // codes is filled again, for the tile's other half or the next tile, as soon as it has been
+    // written out: half a tile's codes, 16 KB an SM, are in flight throughout, across pieces too
+    // (from L2, where the pages' warp sends them earlier).
     constexpr int C = HD / 16;                                      // chunks a row
-    constexpr int PER = 16 * kCkWiden / C, N = 8, H = kCkKeys / PER / N;  // rows at a time, turns a part, parts a tile
-    const bool is_v = warp >= kCkWarpWiden + kCkWiden / 2;
+    // rows at a time, turns a part, parts a tile
+    constexpr int PER = KV8 ? 16 * W / C : 1, N = KV8 ? 32 / W : 1, H = kCkKeys / PER / N;
+    const bool is_v = warp >= kCkWarpWiden + W / 2;
     // four chunks of two rows go out at a time, whose swizzles differ: eight banks of 16 bytes
-    const int wi = threadIdx.x % (16 * kCkWiden), c = C == 4 ? wi & 3 : (wi & 3) | (wi >> 1 & 4);
+    const int wi = threadIdx.x % (16 * W), c = C == 4 ? wi & 3 : (wi & 3) | (wi >> 1 & 4);
     const int rr = C == 4 ? wi >> 2 : (wi >> 4) * 2 + (wi >> 2 & 1);
     const int8_t* pool = (is_v ? a.v8 : a.k8) + c * 16;
     uint64_t *full = is_v ? bar.vfull : bar.kfull, *empty = is_v ? bar.vempty : bar.kempty;
@@ -752,7 +759,7 @@ __global__ void __launch_bounds__(ck_threads<KV8>(), 1)
     if (!ok && lane == 0) fail();
   } else if (warp < kCkSoft) {
     // ---------------- softmax: group j, row 32 quad + lane (TMEM begins at column 0)
-    if (KV8) asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
+    if constexpr (KV8) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(ck_regs_soft(W)));
     const int j = warp >> 2, quad = warp & 3, row = quad * 32 + lane;
     const uint32_t lane_base = (uint32_t)(quad * 32) << 16;
     const uint32_t ts = lane_base + j * kCkKeys, to = lane_base + kCkO + j * 128;
@@ -1205,15 +1212,15 @@ static int ck_sms() {
   return sms;
 }
 
-template <int HD, bool KV8, bool TREE>
-static cudaError_t launch_ck(const uint16_t* q, int q_stride, const fp_kv_view& kv, const CkArgs& a, cudaStream_t s) {
+template <int HD, int W, bool TREE>
+static cudaError_t launch_ck_as(const uint16_t* q, int q_stride, const fp_kv_view& kv, const CkArgs& a, cudaStream_t s) {
   CUtensorMap mq, mk, mv;
   // q [tokens][heads][halves][64], box [tile tokens][G][1][64]
   if (!make_tensor_map_4d(&mq, q, {64, HD / 64, a.H, a.n_tokens}, {128, HD * 2, 2LL * q_stride},
                           {64, 1, a.G, a.tile_tokens}))
     return cudaErrorInvalidValue;
   mk = mv = mq;
-  if (!KV8) {
+  if (W == 0) {
     // pools [row / 8][halves][8 rows][64] of rows of HD, box: a page's 16 rows of a head
     const long long groups = (long long)kv.n_pages * kv.n_kv_heads * 2;
     for (int i = 0; i < 2; ++i)
@@ -1221,10 +1228,30 @@ static cudaError_t launch_ck(const uint16_t* q, int q_stride, const fp_kv_view& 
                               {64, 8, HD / 64, 2}))
         return cudaErrorInvalidValue;
   }
+  if (W > 0) {  // the launch brings the registers that its warps take (they would wait for others for ever)
+    static const bool covered = [] {
+      cudaFuncAttributes f;
+      return cudaFuncGetAttributes(&f, attn_chunk_kernel<HD, W, TREE>) == cudaSuccess &&
+             (f.numRegs + 7) / 8 * 8 * ck_threads(W) >= 32 * (kCkSoft * ck_regs_soft(W) + (ck_threads(W) / 32 - kCkSoft) * ck_regs_other(W));
+    }();
+    if (!covered) return cudaErrorInvalidKernelImage;
+  }
   static std::atomic<unsigned long long> attr{0};
-  FP_CUDA_TRY(smem_limit_once(attn_chunk_kernel<HD, KV8, TREE>, ck_smem<HD>(), &attr));
-  return launch_early(attn_chunk_kernel<HD, KV8, TREE>, dim3(std::min(ck_sms(), kCkMaxCtas)), dim3(ck_threads<KV8>()),
+  FP_CUDA_TRY(smem_limit_once(attn_chunk_kernel<HD, W, TREE>, ck_smem<HD>(), &attr));
+  return launch_early(attn_chunk_kernel<HD, W, TREE>, dim3(std::min(ck_sms(), kCkMaxCtas)), dim3(ck_threads(W)),
                       (size_t)ck_smem<HD>(), s, mq, mk, mv, a);
+}
+
+
+// Widening warps: where every unit is one tile of rows, the keys come twice as fast for the
+// same products and eight warps feed them better than four; with two tiles the softmax needs
+// the registers (us, eight | four: 32 x 16 rows of 64 heads on 8 to 2148 62.6 | 65.2, 8 x 26 of 32
+// heads to 612 34.0 | 35.6, 2 x 1024 rows of 64 heads on 8 to 8000 490 | 446).
+template <int HD, bool TREE>
+static cudaError_t launch_ck(const uint16_t* q, int q_stride, const fp_kv_view& kv, const CkArgs& a, cudaStream_t s) {
+  if (kv.kvquant != FP_KV_INT8) return launch_ck_as<HD, 0, TREE>(q, q_stride, kv, a, s);
+  return a.max_new <= a.tile_tokens ? launch_ck_as<HD, 8, TREE>(q, q_stride, kv, a, s)
+                                    : launch_ck_as<HD, 4, TREE>(q, q_stride, kv, a, s);
 }
 
 }  // namespace fpk

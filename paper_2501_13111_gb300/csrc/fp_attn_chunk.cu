@@ -28,9 +28,7 @@ cudaError_t launch_attention_chunk(const uint16_t* q, int q_stride, int n_tokens
   const CkArgs a = {cu, pos, n_tokens, B, n_heads, kv.n_kv_heads, G, max_new, max_len, ck_tile_tokens(G), nullptr, 0, kv.page_table,
                     kv.pages_per_seq, kv.n_pages, (const int8_t*)kv.k_pool, (const int8_t*)kv.v_pool, kv.k_scale, kv.v_scale,
                     out, (uint8_t*)ws, err, g_ck_wait_limit.load(std::memory_order_relaxed)};
-  if (kv.head_dim == 64)
-    return kv.kvquant == FP_KV_INT8 ? launch_ck<64, true, false>(q, q_stride, kv, a, s) : launch_ck<64, false, false>(q, q_stride, kv, a, s);
-  return kv.kvquant == FP_KV_INT8 ? launch_ck<128, true, false>(q, q_stride, kv, a, s) : launch_ck<128, false, false>(q, q_stride, kv, a, s);
+  return kv.head_dim == 64 ? launch_ck<64, false>(q, q_stride, kv, a, s) : launch_ck<128, false>(q, q_stride, kv, a, s);
 }
 
 }  // namespace fpk
