@@ -703,7 +703,10 @@ __global__ void __launch_bounds__(kTwThreads)
   }
   pdl_trigger();
   pdl_wait();
-  if (!early) chunk_rows(cu, b, n_tokens, &row0, &n);
+  if (!early) {
+    if (b == 0) chunk_check(cu, B, n_tokens, err);
+    chunk_rows(cu, b, n_tokens, &row0, &n);
+  }
   if (n == 0) {
     if (threadIdx.x == 0) n_out[b] = 0;
     return;

@@ -612,6 +612,19 @@ def test_verify_weighs_nan_and_negative_as_nothing(fp):
     _same(_verify(fp, p, cu, parent, tokens, u), _expected(p, cu, parent, tokens, u))
 
 
+def test_verify_of_no_rows(fp):
+    """Sequences without rows, in a buffer that has some and in none at all; a cu that leaves the latter is reported."""
+    p = np.ones((3, 5), np.float32)
+    got = _verify(fp, p, [2, 2, 2], [-1] * 3, [0] * 3, [0.5] * 3)
+    assert got[2].tolist() == [0, 0] and got[3] == 0 and np.all(got[0] == 55) and np.all(got[1] == 55)
+    one = dev(np.zeros(4, np.float32))
+    for cu, want in (([0, 0, 0], 0), ([0, 1, 0], 1)):
+        cnt, err = dev(np.full(2, 55, np.int32)), empty(1, np.int32)
+        fp.fp_op_verify_tree(ptr(one), 4, 0, 2, ptr(dev(np.array(cu, np.int32))), ptr(one), ptr(one), ptr(one), ptr(one), ptr(one),
+                             ptr(cnt), ptr(err))
+        assert host(cnt, np.int32).tolist() == [0, 0] and host(err, np.int32)[0] == want
+
+
 def test_verify_reports_what_cannot_be_drawn(fp):
     """No weight, or an infinite one: the row is accepted, its token is none; the other sequences as ever."""
     p, cu, parent, tokens, u = _problem(5, [1, 6, 6], 300)
