@@ -341,7 +341,8 @@ int fp_op_verify_draft(const float* p, const float* q, int V, int n_tokens, int 
  * each row's number of ancestors.  mask uint32 [n_tokens][mask_stride]: bit j % 32 of
  * word j / 32 is set where row j of the sequence is the row itself or an ancestor; the
  * words' other bits are clear.  mask_stride at least ceil(max_new / 32), at most 65536;
- * max_new: at least every sequence's rows, at most FP_TREE_MAX_ROWS.  Another parent
+ * max_new: at least every sequence's rows, at most FP_TREE_MAX_ROWS (0: nothing is
+ * done).  Another parent
  * is taken for -1 and sets *err = 1 (err may be NULL); so does a sequence of more than
  * max_new rows, whose rows behind those are left as they were. */
 int fp_op_tree_plan(const int32_t* parent, int n_tokens, int B, const int32_t* cu, int max_new, int32_t* depth,
@@ -416,9 +417,10 @@ int fp_op_kv_commit(const fp_kv_view* kv, int n_tokens, int B, const int32_t* cu
  * [B*W] (may be NULL): 1 where the parent had ended or the token is end_token, else 0.
  * end_token in [-1, V); -1: none (done must be NULL then).  With fewer than W candidates
  * the places left are parent -1, token -1, score -inf, done 0.  A logit that is NaN or
- * +inf (or beyond 2^127) in a row that is read, or such a score, leaves the hypothesis
- * without candidates and sets *err = 1 (err may be NULL).  Values are ordered by sums in pairs of fp32, the
- * normaliser good to about 2^-23.  new_score may be score, new_done done; no other
+ * +inf in a row that is read, a row whose largest is beyond 2^127 either way, or a score
+ * that is NaN or +inf leaves the hypothesis without candidates and sets *err = 1 (err may
+ * be NULL).  Values are ordered by sums in pairs of fp32, the
+ * normaliser good to 2^-19.  new_score may be score, new_done done; no other
  * overlap.  V to 2^30.  workspace: 256-byte aligned, at least
  * fp_op_beam_select_workspace_bytes(B, W, V) bytes (0: a shape that is refused); its
  * leading 64 KB are ticket counters that must be zero before the first call; every call
@@ -451,7 +453,7 @@ int fp_op_beam_reorder(int B, int W, int pages_per_seq, int page_size, const int
  * from[i] = -1 or rows[i] = 0: nothing.  No page may be written twice or both read and
  * written in a call.  A page id outside the pool or rows[i] outside [0, page_size] sets
  * *err = 1 (err may be NULL) and skips the copy.  Pools 16-byte aligned, else
- * FP_ERR_UNSUPPORTED.  (The view's page table is not read.) */
+ * FP_ERR_UNSUPPORTED.  (The view's page table is to be there, but is not read.) */
 int fp_op_kv_copy(const fp_kv_view* kv, int n, const int32_t* from, const int32_t* to, const int32_t* rows,
                   int32_t* err, void* stream);
 

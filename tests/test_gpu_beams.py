@@ -81,7 +81,8 @@ def _check(got, x, B, W, score, done=None, end=-1):
 
 
 SHAPES = [(1, 1, 1), (1, 1, 2), (3, 2, 3), (2, 4, 33), (1, 8, 1000), (5, 3, 4097), (2, 5, 16385), (32, 4, 32000),
-          (1, 8, 128001), (2, 32, 5000), (1, 32, 70001), (7, 16, 517), (1, 1, 300000), (1, 2, 600011), (40, 10, 999)]
+          (1, 8, 128001), (2, 32, 5000), (1, 32, 70001), (7, 16, 517), (1, 1, 300000), (1, 2, 600011), (40, 10, 999), (2, 8, 3),
+          (3, 32, 1), (600, 2, 90)]
 
 
 @pytest.mark.parametrize("B,W,V", SHAPES)
