@@ -342,9 +342,8 @@ int fp_op_verify_draft(const float* p, const float* q, int V, int n_tokens, int 
  * word j / 32 is set where row j of the sequence is the row itself or an ancestor; the
  * words' other bits are clear.  mask_stride at least ceil(max_new / 32), at most 65536;
  * max_new: at least every sequence's rows, at most FP_TREE_MAX_ROWS (0: nothing is
- * done).  Another parent
- * is taken for -1 and sets *err = 1 (err may be NULL); so does a sequence of more than
- * max_new rows, whose rows behind those are left as they were. */
+ * done).  Another parent is taken for -1 and sets *err = 1 (err may be NULL); so does a
+ * sequence of more than max_new rows, whose rows behind those are left as they were. */
 int fp_op_tree_plan(const int32_t* parent, int n_tokens, int B, const int32_t* cu, int max_new, int32_t* depth,
                     uint32_t* mask, int mask_stride, int32_t* err, void* stream);
 
@@ -433,7 +432,8 @@ size_t fp_op_beam_select_workspace_bytes(int B, int W, int V);
 
 /* Page tables that follow the chosen beams.  table_in int32 [B*W][pages_per_seq] is
  * what the beams had, len int32 [B] their cached positions, parent as
- * fp_op_beam_select writes it (-1: the beam stays as it is).  In table_out (another
+ * fp_op_beam_select writes it (-1: no hypothesis; the beam keeps its own full blocks, its
+ * part-filled one may be any that is left, and nothing is copied).  In table_out (another
  * buffer) a beam has its parent's pages for the full blocks of page_size positions, shared,
  * and its own for the blocks not begun.  The part-filled block (len[b] % page_size > 0)
  * needs a page of its own for every beam, as table_in must have it: the first of a beam's children

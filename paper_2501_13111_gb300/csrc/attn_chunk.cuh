@@ -37,20 +37,19 @@
 //   warps 12-15, or 12-19 (int8 cache) K and V tiles of the codes as bf16, exact (a byte permute
 //               gives fp32 2^15 + 128 + q, a subtraction q).  A key's K scale multiplies
 //               its score column, its V scale its column of P, both in fp32.  (Tiles of
-//               bf16(q s) took 54 us where this takes 63, 420 where 496, see below, but
-//               were further from the sums in 64 bits: 0.0040 against 0.0024, relative.)
+//               bf16(q s) took 54 us where this then took 63, 420 where 496, but were
+//               further from the sums in 64 bits: 0.0040 against 0.0024, relative.)
 // Measured (launches in a graph, heads of 128): 8 sequences of 5 rows to position 612, 32
-// heads, bf16 cache 23.7 us (2.6 TB/s); 32 of 5 rows to 2148, 64 heads on 8, int8 63 us
-// (1.8 TB/s); 4 chunks of 512 rows to 2048, 40 heads, bf16 69 us (834 TFLOP/s); 2 of 1024
-// rows to 8000, 64 heads on 8, int8 487 us (830 TFLOP/s).  Trees: 8 of up to 26 rows to 612,
-// 32 heads, bf16 24.9 us (3.0 TB/s); 32 of up to 16 rows to 2148, 64 heads on 8, int8 65.5 us
-// (1.9 TB/s), bf16 49 us (4.7 TB/s); 8 of up to 64 rows to 8000, 64 heads on 8, bf16 99 us (828
+// heads, bf16 cache 23.7 us (2.6 TB/s); 32 of 5 rows to 2148, 64 heads on 8, int8 60 us
+// (1.9 TB/s); 4 chunks of 512 rows to 2048, 40 heads, bf16 69 us (834 TFLOP/s); 2 of 1024
+// rows to 8000, 64 heads on 8, int8 447 us (904 TFLOP/s).  Trees: 8 of up to 26 rows to 612,
+// 32 heads, bf16 25.0 us (3.0 TB/s); 32 of up to 16 rows to 2148, 64 heads on 8, int8 62.5 us
+// (2.0 TB/s), bf16 49 us (4.7 TB/s); 8 of up to 64 rows to 8000, 64 heads on 8, bf16 99 us (828
 // TFLOP/s).  A step of two query tiles takes 3000 to 3800 cycles where its MMAs need 2150: a
 // group's scores wait for its P, P for the scores, and what is in between (1900 cycles) is as
 // long as the other group's products; with an int8
-// cache the scales' way from shared memory, which the MMAs keep busy, comes on top (chunk
-// int8 406 us with constants instead), and half a tile's softmax takes 2200 cycles, not 950,
-// beside the widening.  Small batches: 6 to 9 us pass between the launch and the first scores
+// cache the scales' way from shared memory, which the MMAs keep busy, comes on top, and half a
+// tile's softmax takes 1750 cycles, not 950, beside the widening.  Small batches: 6 to 9 us pass between the launch and the first scores
 // (the plan 1.9, the pages 1.1, the first tiles of all SMs at once 2.8), 2 us behind the last.
 // Slots behind the sequence's last position may hold anything: their scores are
 // masked, their V rows are zeroed before the product (int8 cache: read as zeros).

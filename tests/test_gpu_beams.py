@@ -299,6 +299,64 @@ def test_copy_reports_and_skips_bad_pages(fp):
         assert np.array_equal(host(c.dev[w], c.data[w].dtype).reshape(c.data[w].shape), c.data[w])
 
 
+def test_a_captured_step_of_beams(fp):
+    """Select, reorder, copy, twice, as one graph on one stream: replayed on other logits and lengths, the tables and the
+    pools are the oracle's of what the selection chose."""
+    torch = torch_mod()
+    B, W, V, pps, hd, Hkv = 3, 5, 3001, 7, 64, 2
+    R, pages = B * W, B * W * pps
+    c = Batch(fp, 1, hd, Hkv, Hkv, [(1, pages * 16 - 1)], 11)
+    pools = {w: c.dev[w].clone() for w in c.data}
+    x, score, lens = [empty((R, V), np.float32) for _ in range(2)], [empty(R, np.float32) for _ in range(3)], empty(B, np.int32)
+    par, tok = [empty(R, np.int32) for _ in range(2)], empty(R, np.int32)
+    tabs, lists, err = [empty((R, pps), np.int32) for _ in range(3)], [[empty(R, np.int32) for _ in range(3)] for _ in range(2)], empty(1, np.int32)
+    need = fp.fp_op_beam_select_workspace_bytes(B, W, V)
+    ws = empty(need + 256)
+    st = torch.cuda.Stream()
+    g = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g, stream=st):
+        s = st.cuda_stream
+        for i in range(2):
+            fp.fp_op_beam_select(ptr(x[i]), V, B, W, ptr(score[i]), None, -1, ptr(par[i]), ptr(tok), ptr(score[i + 1]), None,
+                                 (ptr(ws) + 255) // 256 * 256, need, ptr(err), s)
+            fp.fp_op_beam_reorder(B, W, pps, 16, ptr(lens), ptr(par[i]), ptr(tabs[i]), ptr(tabs[i + 1]),
+                                  *[ptr(o) for o in lists[i]], ptr(err), s)
+            fp.fp_op_kv_copy(c.view, R, *[ptr(o) for o in lists[i]], ptr(err), s)
+    for seed in range(4):
+        rng = np.random.default_rng(seed)
+        xs = rng.normal(size=(2, R, V)).astype(np.float32)
+        length = rng.integers(0, pps * 16, B).astype(np.int32)
+        table = rng.permutation(pages).reshape(R, pps).astype(np.int32)
+        first = (-5 * rng.random(R)).astype(np.float32)
+        for w in pools:
+            c.dev[w].copy_(pools[w])
+        for a, z in ((x[0], xs[0]), (x[1], xs[1]), (lens, length), (tabs[0], table), (score[0], first)):
+            a.copy_(torch.from_numpy(z))
+        g.replay()
+        torch.cuda.synchronize()
+        assert host(err, np.int32)[0] == 0
+        want = {w: v.copy() for w, v in c.data.items()}
+        for i in range(2):
+            chosen = host(par[i], np.int32).reshape(B, W)
+            sums = host(score[i], np.float32).astype(np.float64)
+            z = xs[i].astype(np.float64)
+            best = np.sort((sums[:, None] + z - np.log(np.exp(z).sum(1))[:, None]).reshape(B, W * V), 1)[:, ::-1][:, :W]
+            new = host(score[i + 1], np.float32).reshape(B, W)
+            assert np.all(np.abs(new - best) <= 2.0 ** -24 * np.abs(best) + LSE)
+            for b in range(B):
+                t, copies, _ = several.reorder(table.reshape(B, W, pps)[b], int(length[b]), chosen[b].tolist())
+                table.reshape(B, W, pps)[b] = t
+                assert [list(v) for v in copies] == np.stack([host(o, np.int32) for o in lists[i]], -1)[b * W:b * W + W].tolist()
+                for a, z1, n in copies:
+                    for w in want:
+                        if n:
+                            want[w][z1, :, :n] = want[w][a, :, :n]
+            assert np.array_equal(host(tabs[i + 1], np.int32).reshape(R, pps), table)
+        for w in want:
+            assert np.array_equal(host(c.dev[w], want[w].dtype).reshape(want[w].shape).view(np.uint8), want[w].view(np.uint8)), w
+
+
 @pytest.mark.parametrize("kvq", [0, 1])
 def test_a_search_as_it_is_used(fp, kvq):
     """Forty steps of two layers: append the beams' tokens, attend over each beam's own history, select, reorder, copy.
