@@ -182,6 +182,28 @@ def test_attention_large_trees_and_units_that_many_ctas_share(fp, kvq, hd, H, Hk
     assert not host(ws, np.uint8)[off:off + 65536].any()
 
 
+@pytest.mark.parametrize("kvq,hd,H,Hkv,B", [(0, 128, 8, 2, 33), (1, 128, 8, 2, 75), (1, 64, 4, 4, 1100), (0, 64, 4, 1, 1100)])
+def test_attention_of_many_sequences(fp, kvq, hd, H, Hkv, B):
+    """More sequences than a warp has lanes, and than the GPU has SMs; some without rows."""
+    rng = np.random.default_rng(B)
+    c = Trees(fp, kvq, hd, H, Hkv, [(int(rng.integers(0, 6)), int(rng.integers(0, 200))) for _ in range(B)], B)
+    q = c.queries(3)
+    got, err = c.attend(q)
+    assert err == 0
+    c.check(q, got)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+def test_attention_whatever_rows_are_announced(fp, hd):
+    """An int8 cache, trees of one query tile: the same rows whether the bound on a tree's rows is one tile or many."""
+    c = Trees(fp, 1, hd, 16, 2, [(16, 2000), (3, 40), (0, 5), (9, 700)], 9, words=32)
+    q = c.queries(4)
+    for most in (16, 17, 1024):
+        got, err = c.attend(q, max_new=most)
+        assert err == 0
+        c.check(q, got)
+
+
 @pytest.mark.parametrize("kvq", [0, 1])
 def test_attention_any_mask(fp, kvq):
     """Masks that no tree has: rows that see later rows, none of their own, all; bits behind the rows do not count."""
