@@ -418,8 +418,8 @@ int fp_op_kv_commit(const fp_kv_view* kv, int n_tokens, int B, const int32_t* cu
  * the places left are parent -1, token -1, score -inf, done 0.  A logit that is NaN or
  * +inf in a row that is read, a row whose largest is beyond 2^127 either way, or a score
  * that is NaN or +inf leaves the hypothesis without candidates and sets *err = 1 (err may
- * be NULL).  Values are ordered by sums in pairs of fp32, the
- * normaliser good to 2^-19.  new_score may be score, new_done done; no other
+ * be NULL).  Values are ordered by sums in pairs of fp32, the normaliser good to
+ * 2^-19, or to 2^-44 of the row's largest logit where that is more.  new_score may be score, new_done done; no other
  * overlap.  V to 2^30.  workspace: 256-byte aligned, at least
  * fp_op_beam_select_workspace_bytes(B, W, V) bytes (0: a shape that is refused); its
  * leading 64 KB are ticket counters that must be zero before the first call; every call

@@ -86,9 +86,9 @@ def select(logits, score, done, end):
         m = np.max(x)
         if m == -np.inf:
             continue
-        lse = m + np.log(np.sum(np.exp(x - m)))
+        z = np.log(np.sum(np.exp(x - m)))  # (against m: x - lse would lose z where m is far from zero)
         order = np.lexsort((np.arange(V), -x))[:W]
-        found += [(-(s + x[t] - lse), w, int(t)) for t in order if x[t] > -np.inf]
+        found += [(-(s + ((x[t] - m) - z)), w, int(t)) for t in order if x[t] > -np.inf]
     found.sort()
     out = [(w, t, -v, int(bool(done[w]) or t == end)) for v, w, t in found[:W]]
     return out + [(-1, -1, -np.inf, 0)] * (W - len(out)), good

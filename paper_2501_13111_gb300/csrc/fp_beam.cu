@@ -290,11 +290,13 @@ __global__ void __launch_bounds__(kBsThreads, 2) beam_select_kernel(const BsArgs
     if (!fine && p.k != -INFINITY && lane == 0 && a.err) atomicExch(a.err, 1);
     if (lane == 0) {
       const int e = (int)(__float_as_uint(p.s) >> 23) - 127 + 1;  // s = 2^e f, 1/2 <= f < 1
-      const float f = __uint_as_float((__float_as_uint(p.s) & 0x7fffffu) | 0x3f000000u), n = p.k + (float)e;
-      // n ln 2 as a pair (0.693147180559945309), its error carried along
+      const float f = __uint_as_float((__float_as_uint(p.s) & 0x7fffffu) | 0x3f000000u);
+      // n = k + e: a pair, as k may be of 2^30, where fp32 holds multiples of 128 (rows of such
+      // logits).  n ln 2 as a pair (0.693147180559945309), its error carried along
       constexpr float kHi = 0.693147182464599609375f, kLo = -1.904654299957767e-9f;
-      const float h = __fmul_rn(n, kHi);
-      const Pair lse = add(tidy(h, __fmaf_rn(n, kLo, __fmaf_rn(n, kHi, -h))), Pair{logf(f), 0.f});
+      const Pair n = sum2(p.k, (float)e);
+      const float h = __fmul_rn(n.hi, kHi);
+      const Pair lse = add(tidy(h, __fmaf_rn(n.hi, kLo, __fmaf_rn(n.hi, kHi, -h))), Pair{__fmaf_rn(n.lo, kHi, logf(f)), 0.f});
       s_off[w] = add(Pair{sc, 0.f}, Pair{-lse.hi, -lse.lo});
     }
     // the pieces' lists, those that count side by side; each one's place is the number of
