@@ -410,16 +410,18 @@ int fp_op_kv_commit(const fp_kv_view* kv, int n_tokens, int B, const int32_t* cu
  * log-probabilities; -inf: there is none).  A group's candidates are (w, t) with the
  * value score[w] + logits[w][t] - log sum_s exp(logits[w][s]); the W largest, in falling
  * order, ties to the lowest w, then t: parent int32 [B*W] their w, token int32 [B*W]
- * their t, new_score fp32 [B*W] their values.  A logit of -inf bans its token.  done
+ * their t, new_score fp32 [B*W] their values.  A logit of -inf bans its token (a low
+ * finite one, down to the least, all but does: it is a candidate with its value, none
+ * where that is below the least fp32).  done
  * int32 [B*W] (NULL: none): where it is not 0 the hypothesis has ended; its logits are
  * not read, its one candidate is end_token with its score as it is.  new_done int32
  * [B*W] (may be NULL): 1 where the parent had ended or the token is end_token, else 0.
  * end_token in [-1, V); -1: none (done must be NULL then).  With fewer than W candidates
  * the places left are parent -1, token -1, score -inf, done 0.  A logit that is NaN or
- * +inf in a row that is read, a row whose largest is beyond 2^127 either way, or a score
- * that is NaN or +inf leaves the hypothesis without candidates and sets *err = 1 (err may
- * be NULL).  Values are ordered by sums in pairs of fp32, the normaliser good to
- * 2^-19, or to 2^-44 of the row's largest logit where that is more.  new_score may be score, new_done done; no other
+ * +inf in a row that is read, or a score that is NaN or +inf leaves the hypothesis
+ * without candidates and sets *err = 1 (err may be NULL).  Values are ordered by sums in
+ * pairs of fp32, the normaliser good to 2^-19, or to 2^-44 of the row's largest logit
+ * where that is up to 2^30 and 2^-44 of it is more.  new_score may be score, new_done done; no other
  * overlap.  V to 2^30.  workspace: 256-byte aligned, at least
  * fp_op_beam_select_workspace_bytes(B, W, V) bytes (0: a shape that is refused); its
  * leading 64 KB are ticket counters that must be zero before the first call; every call

@@ -10,6 +10,8 @@ import numpy as np
 
 from oracle import chunk
 
+LEAST = 2.0 ** 128 - 2.0 ** 103  # from here on down a score rounds to fp32's -inf
+
 
 def plan(parent):
     """Depth of each row and the set of rows it sees (itself and its ancestors); an impossible parent: none."""
@@ -77,7 +79,7 @@ def select(logits, score, done, end):
             good = False
             continue
         if done[w]:
-            found.append((-s, w, end))
+            found.append((-s, w, 0, end))
             continue
         x = np.asarray(logits[w], np.float64)
         if np.any(np.isnan(x)) or np.any(x == np.inf):
@@ -88,9 +90,12 @@ def select(logits, score, done, end):
             continue
         z = np.log(np.sum(np.exp(x - m)))  # (against m: x - lse would lose z where m is far from zero)
         order = np.lexsort((np.arange(V), -x))[:W]
-        found += [(-(s + ((x[t] - m) - z)), w, int(t)) for t in order if x[t] > -np.inf]
+        for i, t in enumerate(order):
+            v = s + ((x[t] - m) - z)
+            if x[t] > -np.inf and v > -LEAST:
+                found.append((-v, w, i, int(t)))  # (a beam's order is its logits', where v does not tell them apart)
     found.sort()
-    out = [(w, t, -v, int(bool(done[w]) or t == end)) for v, w, t in found[:W]]
+    out = [(w, t, -v, int(bool(done[w]) or t == end)) for v, w, _, t in found[:W]]
     return out + [(-1, -1, -np.inf, 0)] * (W - len(out)), good
 
 

@@ -16,8 +16,12 @@ namespace fpk {
 // of the group to finish merges each beam's pieces, then the beams.
 // Two candidates of different beams must fall as 64 bits would have them, so scores are
 // pairs of fp32.  The normaliser: with an integer reference k (the maximum's log2,
-// rounded up), sum_i 2^(x_i log2 e - k) in fp32, one rounding an exponent; pieces with
+// rounded up), sum_i 2^(x_i log2 e - k) in fp32, one rounding an exponent; sets with
 // other references are scaled exactly; lse = (k + exponent of s) ln 2 + log(significand of s).
+// Every warp has the reference of its own values, so that a set of banned tokens (any finite
+// value, down to the least) must not disturb the others: where the maximum m is beyond 2^30, k
+// would be too coarse, or infinite.  There fp32's neighbours are 128 apart, so that only the
+// values equal to m count: s is their number, and m itself the reference.
 // Sorting is by counting: a value's place is the number of larger ones, found by comparisons
 // that wait for nothing.  (One maximum after the other took 12 us where this takes 10.)  A
 // piece's candidates are the few values that reach the W-th largest of 32 groups' maxima; of
@@ -50,17 +54,20 @@ FP_DEV float bs_ex2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-// 2^d, d <= 0 an integer
+// 2^d, d <= 0; an integer from -126 on
 FP_DEV float bs_pow2(float d) { return d < -126.f ? 0.f : __uint_as_float((uint32_t)(127 + (int)d) << 23); }
 
-// A set's reference and its sum against it (-inf: nothing in it)
+// A set's reference r and its sum against it (-inf: nothing in it).  r is k / 2, or m where that is
+// beyond kBsFar: half of k = m log2 e stays below, so one order serves both, and of two sets that
+// are not both near the lower one's factor is 2^-126 or less: 0.
+constexpr float kBsFar = 0x1p30f;
 struct BsSum {
-  float k, s;
+  float r, s;
 };
 FP_DEV BsSum bs_add(BsSum a, BsSum b) {
-  const float k = fmaxf(a.k, b.k);
-  if (k == -INFINITY) return {k, a.s + b.s};
-  return {k, a.s * bs_pow2(a.k - k) + b.s * bs_pow2(b.k - k)};
+  const float r = fmaxf(a.r, b.r);
+  if (r == -INFINITY) return {r, a.s + b.s};
+  return {r, a.s * bs_pow2(2.f * (a.r - r)) + b.s * bs_pow2(2.f * (b.r - r))};
 }
 
 struct BsArgs {
@@ -106,6 +113,7 @@ __global__ void __launch_bounds__(kBsThreads, 2) beam_select_kernel(const BsArgs
     } beam;
   } s_u;
   __shared__ Pair s_off[FP_BEAM_MAX];                             // score - lse of a beam
+  __shared__ float s_ref[FP_BEAM_MAX];                            // (both against this)
   __shared__ unsigned long long s_row[FP_BEAM_MAX][FP_BEAM_MAX];  // its candidates
   constexpr int PIECE = kBsThreads * ITEMS * 4;
   pdl_trigger();
@@ -161,10 +169,13 @@ __global__ void __launch_bounds__(kBsThreads, 2) beam_select_kernel(const BsArgs
       }
       m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
       {
-        // x log2 e in two parts (1.4426950408889634)
+        // x log2 e in two parts (1.4426950408889634).  Far away the exponent is x/2 + (x/2 - m): 0
+        // for m, -64 or less for others (a factor of 0 would turn -inf into a NaN)
         constexpr float kHi = 1.44269502162933349609375f, kLo = 1.92596299e-8f;
-        const float k = m == -INFINITY ? 0.f : ceilf(m * kHi);
-        const float2 hi2 = make_float2(kHi, kHi), lo2 = make_float2(kLo, kLo), k2 = make_float2(-k, -k);
+        const bool far = !(m > -kBsFar && m <= kBsFar);
+        const float hi = far ? 0.5f : kHi, lo = far ? 0.5f : kLo;
+        const float k = m == -INFINITY ? 0.f : far ? m : ceilf(m * kHi);
+        const float2 hi2 = make_float2(hi, hi), lo2 = make_float2(lo, lo), k2 = make_float2(-k, -k);
         float2 s[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i)
@@ -174,7 +185,7 @@ __global__ void __launch_bounds__(kBsThreads, 2) beam_select_kernel(const BsArgs
             s[y / 2] = fp_add2(s[y / 2], make_float2(bs_ex2(e.x), bs_ex2(e.y)));
           }
         const float t = warp_sum((s[0].x + s[0].y) + (s[1].x + s[1].y));
-        sum = bs_add(sum, {m == -INFINITY && t == 0.f ? -INFINITY : k, t});
+        sum = bs_add(sum, {m == -INFINITY && t == 0.f ? -INFINITY : far ? k : 0.5f * k, t});
       }
       __syncthreads();
       const uint32_t bar = s_bar;
@@ -238,8 +249,8 @@ __global__ void __launch_bounds__(kBsThreads, 2) beam_select_kernel(const BsArgs
       BsSum p = lane < kBsWarps ? s_sum[lane] : BsSum{-INFINITY, 0.f};
 #pragma unroll
       for (int o = kBsWarps / 2; o > 0; o >>= 1)
-        p = bs_add(p, {__shfl_xor_sync(0xffffffffu, p.k, o), __shfl_xor_sync(0xffffffffu, p.s, o)});
-      if (lane == 0) a.sums[blockIdx.x] = make_float2(p.k, p.s);
+        p = bs_add(p, {__shfl_xor_sync(0xffffffffu, p.r, o), __shfl_xor_sync(0xffffffffu, p.s, o)});
+      if (lane == 0) a.sums[blockIdx.x] = make_float2(p.r, p.s);
       if (lane < W) a.best[(long long)blockIdx.x * W + lane] = s_list[list][lane];
     }
   }
@@ -280,24 +291,27 @@ __global__ void __launch_bounds__(kBsThreads, 2) beam_select_kernel(const BsArgs
       if (lane == 0) {
         if (real) s_row[w][0] = 1ull << 32 | (uint32_t)~a.end;
         s_off[w] = {sc, 0.f};
+        s_ref[w] = 0.f;
       }
       continue;
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1)
-      p = bs_add(p, {__shfl_xor_sync(0xffffffffu, p.k, o), __shfl_xor_sync(0xffffffffu, p.s, o)});
+      p = bs_add(p, {__shfl_xor_sync(0xffffffffu, p.r, o), __shfl_xor_sync(0xffffffffu, p.s, o)});
     const bool fine = p.s > 0.f && p.s < INFINITY;  // (a NaN or +inf among the logits: neither)
-    if (!fine && p.k != -INFINITY && lane == 0 && a.err) atomicExch(a.err, 1);
+    if (!fine && p.r != -INFINITY && lane == 0 && a.err) atomicExch(a.err, 1);
     if (lane == 0) {
       const int e = (int)(__float_as_uint(p.s) >> 23) - 127 + 1;  // s = 2^e f, 1/2 <= f < 1
       const float f = __uint_as_float((__float_as_uint(p.s) & 0x7fffffu) | 0x3f000000u);
       // n = k + e: a pair, as k may be of 2^30, where fp32 holds multiples of 128 (rows of such
       // logits).  n ln 2 as a pair (0.693147180559945309), its error carried along
       constexpr float kHi = 0.693147182464599609375f, kLo = -1.904654299957767e-9f;
-      const Pair n = sum2(p.k, (float)e);
+      const bool far = fabsf(p.r) >= kBsFar;
+      const Pair n = sum2(far ? 0.f : 2.f * p.r, (float)e);
       const float h = __fmul_rn(n.hi, kHi);
       const Pair lse = add(tidy(h, __fmaf_rn(n.hi, kLo, __fmaf_rn(n.hi, kHi, -h))), Pair{__fmaf_rn(n.lo, kHi, logf(f)), 0.f});
       s_off[w] = add(Pair{sc, 0.f}, Pair{-lse.hi, -lse.lo});
+      s_ref[w] = far ? p.r : 0.f;
     }
     // the pieces' lists, those that count side by side; each one's place is the number of
     // larger ones
@@ -326,8 +340,8 @@ __global__ void __launch_bounds__(kBsThreads, 2) beam_select_kernel(const BsArgs
     __syncwarp();
   }
   __syncthreads();
-  // the beams' lists in the same way: scores as pairs (0: none), ties to the lowest beam and, in
-  // a beam, the order of its list
+  // the beams' lists in the same way: scores as pairs (0: none, as where a sum falls below the least
+  // fp32), ties to the lowest beam and, in a beam, the order of its list
   int valid = 0;
   for (int i = threadIdx.x; i < W * W; i += kBsThreads) {
     const int w = i / W;
@@ -335,9 +349,14 @@ __global__ void __launch_bounds__(kBsThreads, 2) beam_select_kernel(const BsArgs
     unsigned long long score = 0;
     if (k != 0) {
       Pair v = s_off[w];
-      if (k >> 32 != 1) v = add(sum2(bs_value((uint32_t)(k >> 32)), v.hi), Pair{v.lo, 0.f});
-      score = (unsigned long long)bs_ordered(v.hi + 0.f) << 32 | bs_ordered(v.lo + 0.f);
-      ++valid;
+      if (k >> 32 != 1) {
+        const Pair x = sum2(bs_value((uint32_t)(k >> 32)), -s_ref[w]);
+        v = add(sum2(x.hi, v.hi), Pair{v.lo, x.lo});
+      }
+      if (v.hi > -INFINITY) {
+        score = (unsigned long long)bs_ordered(v.hi + 0.f) << 32 | bs_ordered(v.lo + 0.f);
+        ++valid;
+      }
     }
     s_u.beam.score[w][i - w * W] = score;
   }

@@ -32,7 +32,7 @@ def _compare(got, x, B, W, score, done=None, end=-1, err=0):
         want, good = several.select(x[r], score[r], done[r], end)
         assert good
         top = np.abs(np.max(np.where(np.isnan(x[r]), -np.inf, x[r]), -1).astype(np.float64))
-        most = max([m for m in top if m < 2.0 ** 30], default=0.0)
+        most = max([m for m in top if m <= 2.0 ** 30], default=0.0)
         tol = max(LSE, 2.0 ** -44 * most)
         for c, (pw, pt, ps, pd) in enumerate(want):
             o = b * W + c
