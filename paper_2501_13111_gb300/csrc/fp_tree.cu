@@ -86,7 +86,8 @@ __global__ void __launch_bounds__(kCmWarps * 32)
       int before = __shfl_up_sync(0xffffffffu, from, 1);
       if (lane == 0) before = last;
       last = __shfl_sync(0xffffffffu, from, 31);
-      const unsigned ends = __ballot_sync(0xffffffffu, from < 0), wrong = __ballot_sync(0xffffffffu, from >= 0 && (from <= before || from >= n));
+      const unsigned ends = __ballot_sync(0xffffffffu, from == -1),
+                     wrong = __ballot_sync(0xffffffffu, from != -1 && (from < 0 || from <= before || from >= n));
       const int count = min(32, min(ends ? __ffs(ends) - 1 : 32, wrong ? __ffs(wrong) - 1 : 32));
       if (wrong && (!ends || __ffs(wrong) < __ffs(ends)) && lane == 0 && err) atomicExch(err, 1);
       // pool rows of head h (-1: no such place)
