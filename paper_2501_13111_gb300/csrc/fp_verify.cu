@@ -241,9 +241,9 @@ constexpr int kVfCTAs = 8, kVfThreads = 512, kVfWarps = kVfThreads / 32, kVfRuns
 
 // Of the lanes whose weight counts, the first whose sum is past the border; rounding at
 // the very end, an r of 1 or more or a NaN leaves none: the last then.  -1: no weight at all.
-FP_DEV int holder(Pair upto, float w, Pair border) {
-  const unsigned has = __ballot_sync(0xffffffffu, w > 0.f), past = __ballot_sync(0xffffffffu, w > 0.f && greater(upto, border));
-  return past ? __ffs(past) - 1 : 31 - __clz(has);
+FP_DEV int holder(Pair upto, float w, Border border) {
+  const unsigned has = __ballot_sync(0xffffffffu, w > 0.f), over = __ballot_sync(0xffffffffu, w > 0.f && past(upto, border));
+  return over ? __ffs(over) - 1 : 31 - __clz(has);
 }
 
 // The weight of token t: p, less q where there is one, without token `gone`; none below zero.
@@ -337,7 +337,7 @@ __global__ void __cluster_dims__(kVfCTAs, 1, 1) __launch_bounds__(kVfThreads)
     auto leave = cluster.barrier_arrive();  // (a CTA stays until the others have read its total)
     const bool drawable = total.hi > 0.f && total.hi < INFINITY;
     if (drawable) {
-      const Pair border = times(total, rb);
+      const Border border = border_at(total, rb);
       if (holder(all, lane < kVfCTAs ? theirs.hi : 0.f, border) == rank) {
         const Pair before = rank ? shfl(all, rank - 1) : Pair{0.f, 0.f};
         const Pair to = add(before, upto);
@@ -359,7 +359,7 @@ __global__ void __cluster_dims__(kVfCTAs, 1, 1) __launch_bounds__(kVfThreads)
             const Pair wu = add(at, scan<32>(w, lane));
             const int l = holder(wu, w.hi, border);
             if (l >= 0) token = t0 + l;
-            if (__any_sync(0xffffffffu, w.hi > 0.f && greater(wu, border))) break;
+            if (__any_sync(0xffffffffu, w.hi > 0.f && past(wu, border))) break;
             at = shfl(wu, 31);
           }
           if (lane == 0) {
@@ -450,7 +450,7 @@ __global__ void __cluster_dims__(kVfCTAs, 1, 1) __launch_bounds__(kVfThreads)
     const Pair total = shfl(all, kVfCTAs - 1);
     const bool drawable = total.hi > 0.f && total.hi < INFINITY;
     if (drawable) {
-      const Pair border = times(total, r);
+      const Border border = border_at(total, r);
       if (holder(all, lane < kVfCTAs ? theirs.hi : 0.f, border) == rank) {
         const Pair before = rank ? shfl(all, rank - 1) : Pair{0.f, 0.f};
         const Pair to = add(before, upto);
@@ -472,7 +472,7 @@ __global__ void __cluster_dims__(kVfCTAs, 1, 1) __launch_bounds__(kVfThreads)
             const Pair wu = add(at, scan<32>(w, lane));
             const int l = holder(wu, w.hi, border);
             if (l >= 0) token = t0 + l;
-            if (__any_sync(0xffffffffu, w.hi > 0.f && greater(wu, border))) break;
+            if (__any_sync(0xffffffffu, w.hi > 0.f && past(wu, border))) break;
             at = shfl(wu, 31);
           }
           int child = -1;
@@ -634,17 +634,18 @@ __global__ void __launch_bounds__(kTdThreads, 3)
       const Pair theirs = lane < C ? *cluster.map_shared_rank(&s_cta, lane) : Pair{0.f, 0.f}, all = scan<kTdMaxCTAs>(theirs, lane);
       total = shfl(all, kTdMaxCTAs - 1);
       cluster.barrier_arrive();
-      here = holder(all, lane < C ? theirs.hi : 0.f, times(total, r)) == rank;
+      here = holder(all, lane < C ? theirs.hi : 0.f, border_at(total, r)) == rank;
       if (rank) before = shfl(all, rank - 1);
     }
     const Pair to = add(before, upto);
-    here = here && holder(to, lane < kTdWarps ? mine.hi : 0.f, times(total, r)) == warp;
+    here = here && holder(to, lane < kTdWarps ? mine.hi : 0.f, border_at(total, r)) == warp;
     if (warp) before = shfl(to, warp - 1);
   }
   const bool drawable = total.hi > 0.f && total.hi < INFINITY;
   if (!drawable && rank == 0 && (T == 1 ? lane : threadIdx.x) == 0) out[row] = -1;
   if (drawable && here) {
-    const Pair border = times(total, r), pu = add(before, chunks);
+    const Border border = border_at(total, r);
+    const Pair pu = add(before, chunks);
     const int c = holder(pu, chunk.hi, border);
     Pair at = c ? shfl(pu, c - 1) : before;
     int token = -1;
@@ -662,19 +663,19 @@ __global__ void __launch_bounds__(kTdThreads, 3)
           const float v[4] = {f4.x, f4.y, f4.z, f4.w};
           Pair f = from;
           int t = -1;
-          bool past = false;
+          bool over = false;
 #pragma unroll
           for (int y = 0; y < 4; ++y)
-            if (v[y] > 0.f && !past) {
+            if (v[y] > 0.f && !over) {
               f = add(f, Pair{v[y], 0.f});
               t = y;
-              past = greater(f, border);
+              over = past(f, border);
             }
           token = 4 * g - skew + t;
         }
         token = __shfl_sync(0xffffffffu, token, l);
       }
-      if (__any_sync(0xffffffffu, w.hi > 0.f && greater(wu, border))) break;
+      if (__any_sync(0xffffffffu, w.hi > 0.f && past(wu, border))) break;
       at = shfl(wu, 31);
     }
     if (lane == 0) out[row] = token;

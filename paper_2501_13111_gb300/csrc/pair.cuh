@@ -32,6 +32,18 @@ FP_DEV bool greater(Pair a, Pair b) {
   const Pair d = sum2(a.hi, -b.hi);
   return __fadd_rn(d.hi, __fadd_rn(d.lo, __fsub_rn(a.lo, b.lo))) > 0.f;
 }
+// r of a whole sum, 0 <= r < 1, and whether a running sum is past it.  The product's error is as
+// small as 2^-48 of it, so both sides are taken times 2^96 where it could underflow (sums of
+// weights near the least fp32).
+struct Border {
+  Pair at;
+  float by;
+};
+FP_DEV Border border_at(Pair total, float r) {
+  const float by = total.hi < 0x1p20f ? 0x1p96f : 1.f;
+  return {times(Pair{total.hi * by, total.lo * by}, r), by};
+}
+FP_DEV bool past(Pair upto, Border b) { return greater(Pair{upto.hi * b.by, upto.lo * b.by}, b.at); }
 FP_DEV Pair shfl(Pair v, int l) { return {__shfl_sync(0xffffffffu, v.hi, l), __shfl_sync(0xffffffffu, v.lo, l)}; }
 
 // Two fp32 lanes at once: a + b, a b + c.
