@@ -40,10 +40,10 @@
 //               bf16(q s) took 54 us where this then took 63, 420 where 496, but were
 //               further from the sums in 64 bits: 0.0040 against 0.0024, relative.)
 // Measured (launches in a graph, heads of 128): 8 sequences of 5 rows to position 612, 32
-// heads, bf16 cache 23.7 us (2.6 TB/s); 32 of 5 rows to 2148, 64 heads on 8, int8 60 us
+// heads, bf16 cache 23.4 us (2.6 TB/s); 32 of 5 rows to 2148, 64 heads on 8, int8 60 us
 // (1.9 TB/s); 4 chunks of 512 rows to 2048, 40 heads, bf16 67 us (861 TFLOP/s); 2 of 1024
 // rows to 8000, 64 heads on 8, int8 433 us (933 TFLOP/s).  Trees: 8 of up to 26 rows to 612,
-// 32 heads, bf16 24.6 us (3.0 TB/s); 32 of up to 16 rows to 2148, 64 heads on 8, int8 62.8 us
+// 32 heads, bf16 24.6 us (3.0 TB/s); 32 of up to 16 rows to 2148, 64 heads on 8, int8 63 us
 // (2.0 TB/s), bf16 48 us (4.8 TB/s); 8 of up to 64 rows to 8000, 64 heads on 8, bf16 95.5 us (858
 // TFLOP/s).  A step of two query tiles takes 3000 to 3800 cycles where its MMAs need 2150: a
 // group's scores wait for its P, P for the scores, and what is in between (1900 cycles) is as

@@ -26,9 +26,9 @@ namespace fpk {
 // that wait for nothing.  (One maximum after the other took 12 us where this takes 10.)  A
 // piece's candidates are the few values that reach the W-th largest of 32 groups' maxima; of
 // sorted lists, ordered by their heads, entry e of the r-th counts only if r + e < W.
-// Measured: 32 groups of 4 beams, 32000 tokens 10.2 us (1.6 TB/s), 1 of 8, 128001 tokens
-// 10.1.  Bound by latency: loads 2.5 us, exponentials 0.7, candidates 1.5, the group's ticket 1.2,
-// lists 1.5, beams 1.
+// Measured: 32 groups of 4 beams, 32000 tokens 10.5 us (1.6 TB/s), 1 of 8, 128001 tokens
+// 10.2 (10.3 and 10.1 with one form of reference, wrong beside such bans).  Bound by latency:
+// loads 2.5 us, exponentials 0.7, candidates 1.5, the group's ticket 1.2, lists 1.5, beams 1.
 constexpr int kBsThreads = 512, kBsWarps = kBsThreads / 32, kBsItems = 8;
 constexpr int kBsPiece = kBsThreads * kBsItems * 4;  // values held at once
 constexpr int kBsSplits = 32;                        // pieces of a row, at most

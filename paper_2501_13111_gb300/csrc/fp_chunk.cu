@@ -42,8 +42,10 @@ FP_DEV uint2 codes8(const float* x, float s) {
 // Four CTAs an SM, for the loads in flight: 64 registers, a few of 74 spilled (three: 68 us,
 // five: 71).
 // TREE: a row's place in the cache is pos[b] + i, what it is rotated by pos[b] + depth[row].
-// 32 trees of up to 16 rows, 64 heads on 8, int8, 7.3 us; 8 of up to 64, 40 heads, bf16 6.7: three
-// chains of loads (sequence, position and depth, page and cosines) one behind the other.
+// 32 trees of up to 16 rows (391), 64 heads on 8, int8, 7.3 us; 8 of up to 64 (380), 40 heads, bf16
+// 6.7, where their bytes take about 3: three chains of loads (sequence, position and depth, page and
+// cosines) one behind the other, then three or four turns over the heads, each of which waits
+// for loads that went out a turn before.
 template <int HD, bool KV8, bool TREE>
 __global__ void __launch_bounds__(256, 4)
     rope_kv_chunk_kernel(const uint16_t* qkv, int row_stride, int n_tokens, int B, int H, fp_kv_view kv,
